@@ -182,6 +182,49 @@ gpt2_status gpt2_adamw_step(gpt2_model* m, int64_t step, float* lr_out,
 gpt2_status gpt2_adamw_step_noalloc(gpt2_model* m, int64_t step, float* lr_out,
                                     float* d_grad_norm_out);
 
+/* Orthogonalised update. A matrix G goes to the result of `iterations`
+ * Newton-Schulz products: X = G / |G|_F (0 for G = 0), then
+ *   A = X X^T,  X <- 3.4445 X + (-4.7750 A + 2.0315 A^2) X
+ * (the shorter side's Gram matrix: a G taller than wide goes as its
+ * transpose). Five of them bring every singular value that is not small
+ * against the norm near 1. Operands are kept to 22 bits or more, sums in fp32.
+ *
+ * gpt2_orthogonalise: d_x, d_y fp32 [count, rows, cols], the matrices one
+ * after another, each its own problem; d_y may be d_x, and overlaps it in no
+ * other way. iterations 1..32. d_workspace: gpt2_orthogonalise_size bytes,
+ * 256-byte aligned, scratch of this call until its kernels have run, so that
+ * calls (or captured graphs) that may run at the same time need one each. A
+ * matrix that holds a NaN or an infinity comes out as NaN. Any rows, cols and
+ * count from 1, below 2^31 elements a matrix. */
+gpt2_status gpt2_orthogonalise_size(int32_t rows, int32_t cols,
+                                    int32_t count, size_t* bytes_out);
+gpt2_status gpt2_orthogonalise(const float* d_x, float* d_y, int32_t rows,
+                               int32_t cols, int32_t count, int32_t iterations,
+                               void* d_workspace, size_t workspace_bytes,
+                               void* hip_stream);
+
+/* Optimizer step as gpt2_adamw_step (same gradient norm, clipping, schedule
+ * and arguments) in which the matrices of the blocks take an orthogonalised
+ * update with momentum; the embedding tables, biases and LayerNorm parameters
+ * take AdamW. With g the clipped gradient of one matrix W [r, c] (q, k and v
+ * are three matrices) and M its momentum, kept in adam_m (adam_v is unused):
+ *   M = momentum M + g,  U = g + momentum M (nesterov) or M,
+ *   W -= lr (weight_decay W + scale sqrt(max(r, c)) orthogonalised(U)).
+ * A scale of 0.2 gives updates of about AdamW's size, so both can take one
+ * schedule. d_workspace: gpt2_muon_size bytes, 256-byte aligned, scratch as
+ * for gpt2_orthogonalise. INVALID_ARG for momentum outside [0, 1), iterations
+ * outside 1..32 or a scale that is not positive. */
+typedef struct gpt2_muon {
+  float momentum;       /* 0.95 */
+  int32_t nesterov;     /* 1 */
+  int32_t iterations;   /* 5 */
+  float scale;          /* 0.2 */
+} gpt2_muon;
+gpt2_status gpt2_muon_size(const gpt2_config* cfg, size_t* bytes_out);
+gpt2_status gpt2_muon_step(gpt2_model* m, int64_t step, const gpt2_muon* how,
+                           void* d_workspace, size_t workspace_bytes,
+                           float* lr_out, float* d_grad_norm_out);
+
 /* Loss of the last forward with targets ("Optimisation and precision": loss
  * in fp32, the mean over the B*T positions): *loss_out (host) receives the
  * mean; d_token_losses (device fp32 [B*T], row-major [B, T], optional)

@@ -53,6 +53,11 @@ class Buffers(ctypes.Structure):
                                                "params_bf16", "activations", "workspace")]
 
 
+class Muon(ctypes.Structure):
+    _fields_ = [("momentum", ctypes.c_float), ("nesterov", ctypes.c_int32), ("iterations", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
 _lib = None
 
 
@@ -77,6 +82,10 @@ def lib():
         "gpt2_backward": (I32, [P, I32]),
         "gpt2_adamw_step": (I32, [P, I64, ctypes.POINTER(F32), P]),
         "gpt2_adamw_step_noalloc": (I32, [P, I64, ctypes.POINTER(F32), P]),
+        "gpt2_orthogonalise_size": (I32, [I32, I32, I32, ctypes.POINTER(ctypes.c_size_t)]),
+        "gpt2_orthogonalise": (I32, [P, P, I32, I32, I32, I32, P, ctypes.c_size_t, P]),
+        "gpt2_muon_size": (I32, [cfgp, ctypes.POINTER(ctypes.c_size_t)]),
+        "gpt2_muon_step": (I32, [P, I64, ctypes.POINTER(Muon), P, ctypes.c_size_t, ctypes.POINTER(F32), P]),
         "gpt2_loss": (I32, [P, ctypes.POINTER(F32), P]),
         "gpt2_evaluate": (I32, [P, P, P, ctypes.POINTER(F32), P]),
         "gpt2_lr_at": (F32, [cfgp, I64]),
@@ -160,6 +169,38 @@ def kind_table(cfg: Config):
         off, shape = tt[f"h.0.{n}"]
         kinds[k] = (off, (L,) + shape)
     return kinds
+
+
+def orthogonalise(x, iterations=5, out=None, workspace=None):
+    """Newton-Schulz orthogonalisation of one fp32 matrix [rows, cols] or a
+    batch [count, rows, cols] (gpt2_orthogonalise) on the current stream of
+    x's device. out: a tensor like x, or x itself. workspace: a uint8 tensor
+    of at least orthogonalise_size bytes; allocated for the call by default."""
+    import torch
+    if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dtype == torch.float32 and x.dim() in (2, 3)
+            and x.is_contiguous() and x.numel()):
+        raise ValueError("orthogonalise takes a contiguous fp32 device tensor [rows, cols] or [count, rows, cols]")
+    out = torch.empty_like(x) if out is None else out
+    if out.dtype != x.dtype or out.shape != x.shape or out.device != x.device or not out.is_contiguous():
+        raise ValueError("out must be a contiguous tensor of x's shape, type and device")
+    rows, cols = x.shape[-2:]
+    count = x.shape[0] if x.dim() == 3 else 1
+    with torch.cuda.device(x.device):
+        if workspace is None:
+            workspace = torch.empty(orthogonalise_size(rows, cols, count), dtype=torch.uint8, device=x.device)
+        elif workspace.dtype != torch.uint8 or workspace.device != x.device or not workspace.is_contiguous():
+            raise ValueError("the workspace must be a contiguous uint8 tensor on x's device")
+        _check(lib().gpt2_orthogonalise(x.data_ptr(), out.data_ptr(), rows, cols, count, int(iterations),
+                                        workspace.data_ptr(), workspace.numel(),
+                                        torch.cuda.current_stream().cuda_stream))
+    return out
+
+
+def orthogonalise_size(rows, cols, count=1) -> int:
+    """Workspace bytes of orthogonalise."""
+    n = ctypes.c_size_t()
+    _check(lib().gpt2_orthogonalise_size(rows, cols, count, ctypes.byref(n)))
+    return n.value
 
 
 class GPT2:
@@ -253,6 +294,21 @@ class GPT2:
         ptr = ctypes.c_void_p(norm_out.data_ptr()) if norm_out is not None else ctypes.c_void_p(0)
         fn = self.L.gpt2_adamw_step_noalloc if noalloc else self.L.gpt2_adamw_step
         _check(fn(self.handle, int(step), ctypes.byref(lr), ptr), self.handle)
+        return lr.value
+
+    def muon_step(self, step: int, norm_out=None, momentum=0.95, nesterov=True, iterations=5, scale=0.2):
+        """Clip, an orthogonalised update with momentum for the blocks'
+        matrices and AdamW for the rest (gpt2_muon_step). Its workspace is
+        allocated on the first call and kept."""
+        if getattr(self, "muon_workspace", None) is None:
+            n = ctypes.c_size_t()
+            _check(self.L.gpt2_muon_size(ctypes.byref(self.cfg), ctypes.byref(n)))
+            self.muon_workspace = self.torch.empty(n.value, dtype=self.torch.uint8, device=self.device)
+        lr = ctypes.c_float()
+        how = Muon(float(momentum), int(bool(nesterov)), int(iterations), float(scale))
+        _check(self.L.gpt2_muon_step(self.handle, int(step), ctypes.byref(how), self.muon_workspace.data_ptr(),
+                                     self.muon_workspace.numel(), ctypes.byref(lr),
+                                     norm_out.data_ptr() if norm_out is not None else None), self.handle)
         return lr.value
 
     def loss(self, token_losses=None) -> float:

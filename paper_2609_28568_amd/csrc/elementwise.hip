@@ -529,6 +529,10 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {
   long lo = 0;
   for (int sg = 0; sg < a.seg.count; ++sg) {
     const long hi = a.seg.end[sg];
+    if (a.seg.decay[sg] < 0) {   // another optimizer's
+      lo = hi;
+      continue;
+    }
     const float wd = a.seg.decay[sg] ? a.weight_decay : 0.0f;
     const unsigned first = hi - lo < stride ? (unsigned)((lo >> 10) % gridDim.x) : 0u;
     const unsigned vb = blockIdx.x >= first ? blockIdx.x - first : blockIdx.x + gridDim.x - first;

@@ -1231,10 +1231,28 @@ gpt2_status gpt2_backward(gpt2_model* m, int32_t accumulate) {
 
 namespace {
 
+// The matrices of the blocks, which gpt2_muon_step orthogonalises: the q, k, v
+// and attention output projections, then the MLP's two. The pointers are left
+// for the step to fill in.
+constexpr int MUON_KINDS[] = {K_QKVW, K_ATTPROJW, K_FCW, K_FCPROJW};
+void muon_groups(const Dims& d, OrthoArgs* a) {
+  const int C = d.C, F = d.F;
+  const int shape[4][3] = {{C, C, 3 * d.L}, {C, C, d.L}, {F, C, d.L}, {C, F, d.L}};
+  a->ngroups = 4;
+  for (int k = 0; k < 4; ++k) {
+    OrthoGroup& g = a->g[k];
+    g.rows = shape[k][0];
+    g.cols = g.ld = shape[k][1];
+    g.count = shape[k][2];
+    g.stride = (long)g.rows * g.cols;
+  }
+}
+
 // The optimizer step with its scratch (sum-of-squares partials, norm and clip
-// coefficient) at the given device addresses.
+// coefficient) at the given device addresses; with muon the matrices of the
+// blocks take that update instead.
 gpt2_status adamw_step_with(gpt2_model* m, int64_t step, float* lr_out, float* d_grad_norm_out, float* parts,
-                            float* nc) {
+                            float* nc, const gpt2_muon* muon = nullptr, void* muon_ws = nullptr) {
   const gpt2_config& c = m->cfg;
   const long n = (long)m->n_params;
   float* grads = static_cast<float*>(m->buf.grads_f32);
@@ -1264,7 +1282,34 @@ gpt2_status adamw_step_with(gpt2_model* m, int64_t step, float* lr_out, float* d
     a.seg.end[k] = (long)(m->koff[k] + m->kn[k]);
     a.seg.decay[k] = kDecay[k] ? 1 : 0;
   }
-  TRY(m->run(GPT2_K_OPTIMIZER, 0.0, 30.0 * n, [&] { return launch_adamw(a, m->stream); }));
+  if (muon) {
+    OrthoArgs o{};
+    muon_groups(m->d, &o);
+    double skipped = 0.0;
+    for (int k = 0; k < o.ngroups; ++k) {
+      const int kind = MUON_KINDS[k];
+      a.seg.decay[kind] = -1;
+      skipped += (double)m->kn[kind];
+      OrthoGroup& g = o.g[k];
+      g.x = m->gf(kind);
+      g.y = m->pf(kind);
+      g.mom = static_cast<float*>(m->buf.adam_m) + m->koff[kind];
+      g.p_bf16 = m->pb(kind);
+      g.scale = muon->scale * std::sqrt((float)std::max(g.rows, g.cols));
+    }
+    o.iterations = muon->iterations;
+    o.workspace = muon_ws;
+    o.update = 1;
+    o.nesterov = muon->nesterov != 0;
+    o.momentum = muon->momentum;
+    o.lr = a.lr;
+    o.weight_decay = a.weight_decay;
+    o.norm_coef = nc;
+    TRY(m->run(GPT2_K_OPTIMIZER, ortho_flops(o), 22.0 * skipped, [&] { return launch_orthogonalise(o, m->stream); }));
+    TRY(m->run(GPT2_K_OPTIMIZER, 0.0, 30.0 * (n - skipped), [&] { return launch_adamw(a, m->stream); }));
+  } else {
+    TRY(m->run(GPT2_K_OPTIMIZER, 0.0, 30.0 * n, [&] { return launch_adamw(a, m->stream); }));
+  }
   if (lr_out) *lr_out = (float)lr;
   m->have_grads = false;
   return GPT2_OK;
@@ -1295,6 +1340,81 @@ gpt2_status gpt2_adamw_step_noalloc(gpt2_model* m, int64_t step, float* lr_out, 
   float* scratch = nullptr;
   TRY(noalloc_scratch(&scratch));
   return adamw_step_with(m, step, lr_out, d_grad_norm_out, scratch, scratch + nc_off);
+}
+
+gpt2_status gpt2_orthogonalise_size(int32_t rows, int32_t cols, int32_t count, size_t* bytes_out) {
+  OrthoGroup g{};
+  g.rows = rows; g.cols = cols; g.count = count;
+  const size_t bytes = ortho_layout(&g, 1);
+  if (!bytes || !bytes_out) {
+    g_last_error = bytes ? "bytes_out is NULL"
+                         : "rows, cols and count must be positive, a matrix (padded to multiples of 64) below 2^31 elements";
+    return GPT2_ERR_INVALID_ARG;
+  }
+  *bytes_out = bytes;
+  return GPT2_OK;
+}
+
+gpt2_status gpt2_orthogonalise(const float* d_x, float* d_y, int32_t rows, int32_t cols, int32_t count,
+                               int32_t iterations, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+  size_t need = 0;
+  if (gpt2_status st = gpt2_orthogonalise_size(rows, cols, count, &need)) return st;
+  const char* why = nullptr;
+  if (!d_x || !d_y || !d_workspace) why = "x, y or the workspace is NULL";
+  else if ((reinterpret_cast<uintptr_t>(d_x) | reinterpret_cast<uintptr_t>(d_y)) % 4) why = "x or y is not aligned";
+  else if (reinterpret_cast<uintptr_t>(d_workspace) % 256) why = "the workspace is not 256-byte aligned";
+  else if (workspace_bytes < need) why = "the workspace is smaller than gpt2_orthogonalise_size says";
+  else if (iterations < 1 || iterations > 32) why = "iterations must be in 1..32";
+  if (why) {
+    g_last_error = why;
+    return GPT2_ERR_INVALID_ARG;
+  }
+  OrthoArgs a{};
+  a.ngroups = 1;
+  a.g[0].x = d_x;
+  a.g[0].y = d_y;
+  a.g[0].rows = rows;
+  a.g[0].cols = a.g[0].ld = cols;
+  a.g[0].count = count;
+  a.g[0].stride = (long)rows * cols;
+  a.iterations = iterations;
+  a.workspace = d_workspace;
+  const hipError_t e = launch_orthogonalise(a, static_cast<hipStream_t>(hip_stream));
+  if (e == hipSuccess) return GPT2_OK;
+  g_last_error = hipGetErrorString(e);
+  return GPT2_ERR_DEVICE;
+}
+
+gpt2_status gpt2_muon_size(const gpt2_config* cfg, size_t* bytes_out) {
+  const char* why = validate(cfg);
+  if (!why && !bytes_out) why = "bytes_out is NULL";
+  size_t bytes = 0;
+  if (!why) {
+    OrthoArgs o{};
+    muon_groups(dims_of(*cfg), &o);
+    bytes = ortho_layout(o.g, o.ngroups);
+    if (!bytes) why = "a block's matrices are too large";
+  }
+  if (why) {
+    g_last_error = why;
+    return GPT2_ERR_INVALID_ARG;
+  }
+  *bytes_out = bytes;
+  return GPT2_OK;
+}
+
+gpt2_status gpt2_muon_step(gpt2_model* m, int64_t step, const gpt2_muon* how, void* d_workspace,
+                           size_t workspace_bytes, float* lr_out, float* d_grad_norm_out) {
+  if (!m) return GPT2_ERR_INVALID_ARG;
+  if (step < 0) return m->fail(GPT2_ERR_INVALID_ARG, "step must be >= 0");
+  if (const char* why = muon_invalid(how)) return m->fail(GPT2_ERR_INVALID_ARG, why);
+  size_t need = 0;
+  if (gpt2_muon_size(&m->cfg, &need) != GPT2_OK) return m->fail(GPT2_ERR_INVALID_ARG, g_last_error);
+  if (!d_workspace || reinterpret_cast<uintptr_t>(d_workspace) % 256 || workspace_bytes < need)
+    return m->fail(GPT2_ERR_INVALID_ARG, "the workspace is NULL, not 256-byte aligned, or smaller than gpt2_muon_size says");
+  if (!m->have_grads) return m->fail(GPT2_ERR_STATE, "optimizer step with no gradient");
+  return adamw_step_with(m, step, lr_out, d_grad_norm_out, m->wsf(m->ws.sumsq), m->wsf(m->ws.normcoef), how,
+                         d_workspace);
 }
 
 gpt2_status gpt2_loss(gpt2_model* m, float* loss_out, float* d_token_losses) {

@@ -359,7 +359,7 @@ hipError_t launch_clip_coef(const float* parts, int nparts, float clip, float* n
 
 struct AdamSegments {
   long end[16];    // exclusive end offset (elements) of each segment
-  int decay[16];   // 1 where weight decay applies
+  int decay[16];   // 1 where weight decay applies; -1: the segment is left as it is
   int count;
 };
 struct AdamArgs {
@@ -375,6 +375,42 @@ struct AdamArgs {
   AdamSegments seg;
 };
 hipError_t launch_adamw(const AdamArgs& a, hipStream_t s);
+
+// ---------------------------------------------------------------- orthogonalised updates
+constexpr int ORTHO_GROUPS = 12;   // shapes in one call
+constexpr int ORTHO_PARTS = 32;    // partial sums of squares per matrix
+
+// `count` matrices of one shape, `stride` elements apart, row stride ld. The
+// second block is filled in by ortho_layout and the launcher.
+struct OrthoGroup {
+  const float* x;      // the matrices (with update: their gradients)
+  float* y;            // the results (with update: the parameters)
+  float* mom;          // update: the momenta
+  bf16_t* p_bf16;      // update: the parameters' bf16 copy
+  long stride;
+  int rows, cols, ld, count;
+  float scale;         // update: the factor of the orthogonalised matrix
+
+  int mp, np, tall, vec;
+  long x_off[2], a_off, p_off;
+};
+struct OrthoArgs {
+  OrthoGroup g[ORTHO_GROUPS];
+  int ngroups, iterations;
+  void* workspace;     // ortho_layout bytes, 256-byte aligned
+  // with update: m = momentum m + coef x, u = coef x + momentum m (nesterov) or m,
+  // y -= lr (weight_decay y + scale orthogonalised(u)); otherwise y = orthogonalised(x)
+  int update, nesterov;
+  float momentum, lr, weight_decay;
+  const float* norm_coef;   // [1] clip coefficient
+};
+size_t ortho_layout(OrthoGroup* g, int ngroups);   // workspace bytes; 0: a shape out of range
+hipError_t launch_orthogonalise(const OrthoArgs& a, hipStream_t s);
+// FLOPs of the products (half of the symmetric ones)
+double ortho_flops(const OrthoArgs& a);
+struct gpt2_muon;
+// Why the settings of an orthogonalised update are refused, or null
+const char* muon_invalid(const gpt2_muon* how);
 
 // ---------------------------------------------------------------- no-alloc scratch
 // Floats of the static scratch array the allocation-free entry points use

@@ -20,7 +20,7 @@
 #include <string>
 #include <vector>
 
-#include "../../include/qwen3.h"
+#include "../../include/qwen3_prompt.h"
 #include "kernels.h"
 #include "probe.h"
 
@@ -531,6 +531,55 @@ double attn_fwd_flops(const Dims& d) {
   return 4.0 * d.B * d.H * d.hd * ((double)d.T * (d.T + 1) / 2.0);
 }
 
+// Norm of the adapter gradients and the clip coefficient, into normcoef; the
+// norm also to d_grad_norm_out if given.
+gpt2_status clip_norm(qwen3_model* m, float* d_grad_norm_out) {
+  const long n = (long)m->n_lora;
+  const float* grads = static_cast<const float*>(m->buf.lora_grads);
+  float* parts = m->wf(m->ws.sumsq);
+  float* nc = m->wf(m->ws.normcoef);
+  const int OPT = QWEN3_K_OPTIMIZER;
+  TRY(m->run(OPT, 0.0, 4.0 * n, [&] { return launch_sumsq(grads, n, parts, m->stream); }));
+  // the kernel writes the caller's copy of the norm too, where it can reach it
+  const bool direct = d_grad_norm_out && on_this_device(d_grad_norm_out);
+  TRY(m->run(OPT, 0.0, 4.0 * sumsq_parts(), [&] {
+    return launch_clip_coef(parts, sumsq_parts(), m->cfg.grad_clip, nc, m->stream, direct ? d_grad_norm_out : nullptr);
+  }));
+  if (d_grad_norm_out && !direct)
+    TRY(hipMemcpyAsync(d_grad_norm_out, nc, sizeof(float), hipMemcpyDeviceToDevice, m->stream));
+  return GPT2_OK;
+}
+
+// The adapters' matrices for the orthogonalised update: of every projection
+// its A, the r real rows of its block, and its B, whole (RP columns: the
+// padding is zero, and a zero column stays one through every product). m null:
+// shapes only.
+void muon_groups(const Dims& d, OrthoArgs* a, qwen3_model* m, const gpt2_muon* how) {
+  size_t off = 0;
+  auto add = [&](size_t at, long stride, int rows, int cols, int count) {
+    OrthoGroup& g = a->g[a->ngroups++];
+    g.rows = rows;
+    g.cols = g.ld = cols;
+    g.count = count;
+    g.stride = stride;
+    if (!m) return;
+    g.x = static_cast<const float*>(m->buf.lora_grads) + at;
+    g.y = static_cast<float*>(m->buf.lora_f32) + at;
+    g.mom = static_cast<float*>(m->buf.adam_m) + at;
+    g.p_bf16 = static_cast<bf16_t*>(m->buf.lora_bf16) + at;
+    g.scale = how->scale * std::sqrt((float)std::max(rows, cols == RP ? d.r : cols));
+  };
+  for (int g = 0; g < G_N; ++g) {
+    if (!(d.groups & (1 << g))) continue;
+    const GroupGeom gg = group_geom(d, g);
+    add(off, (long)RP * gg.in, d.r, gg.in, d.L * gg.n);
+    off += (size_t)d.L * gg.n * RP * gg.in;
+    for (int j = 0, row = 0; j < gg.n; row += gg.out[j], ++j)
+      add(off + (size_t)row * RP, (long)gg.out_total * RP, gg.out[j], RP, d.L);
+    off += (size_t)d.L * gg.out_total * RP;
+  }
+}
+
 gpt2_status fail(qwen3_model* m, gpt2_status st, const std::string& why) {
   if (m) m->err = why;
   g_err = why;
@@ -825,17 +874,9 @@ gpt2_status qwen3_adamw_step(qwen3_model* m, int64_t step, float* d_grad_norm_ou
   const qwen3_config& c = m->cfg;
   const long n = (long)m->n_lora;
   float* grads = static_cast<float*>(m->buf.lora_grads);
-  float* parts = m->wf(m->ws.sumsq);
   float* nc = m->wf(m->ws.normcoef);
   const int OPT = QWEN3_K_OPTIMIZER;
-  TRY(m->run(OPT, 0.0, 4.0 * n, [&] { return launch_sumsq(grads, n, parts, m->stream); }));
-  // the kernel writes the caller's copy of the norm too, where it can reach it
-  const bool direct = d_grad_norm_out && on_this_device(d_grad_norm_out);
-  TRY(m->run(OPT, 0.0, 4.0 * sumsq_parts(), [&] {
-    return launch_clip_coef(parts, sumsq_parts(), c.grad_clip, nc, m->stream, direct ? d_grad_norm_out : nullptr);
-  }));
-  if (d_grad_norm_out && !direct)
-    TRY(hipMemcpyAsync(d_grad_norm_out, nc, sizeof(float), hipMemcpyDeviceToDevice, m->stream));
+  if (gpt2_status st = clip_norm(m, d_grad_norm_out)) return st;
   AdamArgs a{};
   a.p = static_cast<float*>(m->buf.lora_f32);
   a.g = grads;
@@ -852,6 +893,43 @@ gpt2_status qwen3_adamw_step(qwen3_model* m, int64_t step, float* d_grad_norm_ou
   a.seg.end[0] = n;
   a.seg.decay[0] = 1;   // the configured decay applies to every adapter tensor (all are 2-D)
   TRY(m->run(OPT, 0.0, 30.0 * n, [&] { return launch_adamw(a, m->stream); }));
+  m->have_grads = false;
+  return GPT2_OK;
+}
+
+gpt2_status qwen3_muon_size(const qwen3_config* cfg, size_t* bytes_out) {
+  if (const char* why = validate(cfg)) return fail(nullptr, GPT2_ERR_INVALID_ARG, why);
+  if (!bytes_out) return fail(nullptr, GPT2_ERR_INVALID_ARG, "bytes_out is NULL");
+  OrthoArgs o{};
+  muon_groups(dims_of(*cfg), &o, nullptr, nullptr);
+  const size_t bytes = ortho_layout(o.g, o.ngroups);
+  if (!bytes) return fail(nullptr, GPT2_ERR_INVALID_ARG, "an adapter's matrices are too large");
+  *bytes_out = bytes;
+  return GPT2_OK;
+}
+
+gpt2_status qwen3_muon_step(qwen3_model* m, const gpt2_muon* how, void* d_workspace, size_t workspace_bytes,
+                            float* d_grad_norm_out) {
+  if (!m) return fail(nullptr, GPT2_ERR_INVALID_ARG, "null model");
+  if (const char* why = muon_invalid(how)) return fail(m, GPT2_ERR_INVALID_ARG, why);
+  size_t need = 0;
+  if (qwen3_muon_size(&m->cfg, &need) != GPT2_OK) return fail(m, GPT2_ERR_INVALID_ARG, g_err);
+  if (!d_workspace || reinterpret_cast<uintptr_t>(d_workspace) % 256 || workspace_bytes < need)
+    return fail(m, GPT2_ERR_INVALID_ARG,
+                "the workspace is NULL, not 256-byte aligned, or smaller than qwen3_muon_size says");
+  if (!m->have_grads) return fail(m, GPT2_ERR_STATE, "optimizer step needs a backward");
+  if (gpt2_status st = clip_norm(m, d_grad_norm_out)) return st;
+  OrthoArgs o{};
+  muon_groups(m->d, &o, m, how);
+  o.iterations = how->iterations;
+  o.workspace = d_workspace;
+  o.update = 1;
+  o.nesterov = how->nesterov != 0;
+  o.momentum = how->momentum;
+  o.lr = m->cfg.lr;
+  o.weight_decay = m->cfg.weight_decay;
+  o.norm_coef = m->wf(m->ws.normcoef);
+  TRY(m->run(QWEN3_K_OPTIMIZER, ortho_flops(o), 22.0 * m->n_lora, [&] { return launch_orthogonalise(o, m->stream); }));
   m->have_grads = false;
   return GPT2_OK;
 }

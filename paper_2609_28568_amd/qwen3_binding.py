@@ -1,5 +1,5 @@
-"""ctypes binding of the Qwen3-shaped adapter step (include/qwen3.h) in
-libgpt2_mi355x.so.
+"""ctypes binding of the Qwen3-shaped adapter step (include/qwen3.h and
+include/qwen3_prompt.h) in libgpt2_mi355x.so.
 
 Argument marshalling only: torch supplies the device buffers and the stream,
 every step runs in the library's HIP kernels. Also maps the per-projection
@@ -12,7 +12,7 @@ import ctypes
 
 import numpy as np
 
-from .binding import LibError, lib as _lib_gpt2
+from .binding import LibError, Muon, lib as _lib_gpt2
 
 RP = 64   # padded adapter rank of the library
 # kernel classes of the timing probes (QWEN3_K_* in include/qwen3.h)
@@ -62,6 +62,8 @@ def lib():
         "qwen3_forward": (I32, [P, P, P]),
         "qwen3_backward": (I32, [P]),
         "qwen3_adamw_step": (I32, [P, ctypes.c_int64, P]),
+        "qwen3_muon_size": (I32, [ctypes.POINTER(Qwen3Config), ctypes.POINTER(ctypes.c_size_t)]),
+        "qwen3_muon_step": (I32, [P, ctypes.POINTER(Muon), P, ctypes.c_size_t, P]),
         "qwen3_loss": (I32, [P, ctypes.POINTER(F32), P]),
         "qwen3_set_fusion": (I32, [P, I32, I32]),
         "qwen3_destroy": (None, [P]),
@@ -262,6 +264,20 @@ class Qwen3:
     def adamw_step(self, step: int, norm_out=None):
         ptr = ctypes.c_void_p(norm_out.data_ptr() if norm_out is not None else 0)
         _check(lib().qwen3_adamw_step(self.h, step, ptr), self.h)
+
+    def muon_step(self, norm_out=None, momentum=0.95, nesterov=True, iterations=5, scale=0.2):
+        """Clip and an orthogonalised update with momentum of every adapter
+        matrix (qwen3_muon_step). Its workspace is allocated on the first call
+        and kept."""
+        if getattr(self, "muon_workspace", None) is None:
+            n = ctypes.c_size_t()
+            _check(lib().qwen3_muon_size(ctypes.byref(self.cfg), ctypes.byref(n)))
+            self.muon_workspace = self.torch.empty(n.value, dtype=self.torch.uint8,
+                                                   device=self.bufs["workspace"].device)
+        how = Muon(float(momentum), int(bool(nesterov)), int(iterations), float(scale))
+        _check(lib().qwen3_muon_step(self.h, ctypes.byref(how), self.muon_workspace.data_ptr(),
+                                     self.muon_workspace.numel(),
+                                     norm_out.data_ptr() if norm_out is not None else None), self.h)
 
     def loss(self, token_losses=None) -> float:
         v = ctypes.c_float()
