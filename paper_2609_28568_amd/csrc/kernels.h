@@ -376,6 +376,21 @@ struct AdamArgs {
 };
 hipError_t launch_adamw(const AdamArgs& a, hipStream_t s);
 
+// ---------------------------------------------------------------- rotary positions with several axes
+// Rows q [H*hd] | k [Hkv*hd] | v [Hkv*hd] of `tokens` tokens; positions
+// [axes][tokens]; gains null: no norm. Forward: in = the rows. Backward: in =
+// their gradients, raw = the rows. Values pass through. out may be in.
+struct RotaryArgs {
+  int tokens, H, Hkv, hd;
+  float eps;
+  const int32_t* positions;
+  const bf16_t *q_norm, *k_norm;
+  double freq[128];    // turns per unit of position of each pair, theta^(-2i/hd) / 2 pi
+  uint8_t axis[128];   // each pair's axis
+};
+hipError_t launch_rotary(const RotaryArgs& a, const bf16_t* in, const bf16_t* raw, bf16_t* out, int backward,
+                         hipStream_t s);
+
 // ---------------------------------------------------------------- orthogonalised updates
 constexpr int ORTHO_GROUPS = 12;   // shapes in one call
 constexpr int ORTHO_PARTS = 32;    // partial sums of squares per matrix

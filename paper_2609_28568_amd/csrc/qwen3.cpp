@@ -302,6 +302,9 @@ struct qwen3_model {
   size_t base_off[B_NKIND];
   bool have_targets = false, have_grads = false;
   int swiglu_fused = 1;   // QWEN3_FUSION_SWIGLU mode
+  // positions of the next forward, and of the last one (positions null: the
+  // default tables)
+  RotaryArgs rotary{}, rotary_used{};
   std::string err;
   ProbeSet<QWEN3_K_COUNT> probes;
 
@@ -580,6 +583,67 @@ void muon_groups(const Dims& d, OrthoArgs* a, qwen3_model* m, const gpt2_muon* h
   }
 }
 
+// Checks axes and sections and fills in the pairs' axes and frequencies.
+const char* rotary_axes(RotaryArgs* a, int hd, int n_axes, const int32_t* sections, int interleaved, double theta) {
+  if (hd != 32 && hd != 64 && hd != 128 && hd != 256) return "head_dim must be 32, 64, 128 or 256";
+  if (n_axes < 1 || n_axes > 4 || !sections) return "n_axes must be in 1..4, with a section for each";
+  if (!(theta > 0.0) || !std::isfinite(theta)) return "theta must be positive";
+  const int half = hd / 2;
+  int sum = 0;
+  for (int k = 0; k < n_axes; ++k) {
+    if (sections[k] < 0 || sections[k] > half) return "a section is out of range";
+    if (interleaved && k > 0 && sections[k] > 0 && k + n_axes * (sections[k] - 1) >= half)
+      return "an interleaved section does not fit the head";
+    sum += sections[k];
+  }
+  if (sum != half) return "the sections must sum to head_dim / 2";
+  a->hd = hd;
+  for (int i = 0, k = 0, left = sections[0]; i < half; ++i) {
+    if (interleaved) {
+      k = i % n_axes;
+      if (i / n_axes >= sections[k]) k = 0;
+    } else {
+      while (left == 0) left = sections[++k];
+      --left;
+    }
+    a->axis[i] = (uint8_t)k;
+    a->freq[i] = std::pow(theta, -2.0 * i / hd) / (2.0 * 3.14159265358979323846);
+  }
+  return nullptr;
+}
+
+const char* rotary_args(const qwen3_rotary* r, const void* in, const void* raw, const int32_t* pos, const void* qn,
+                        const void* kn, const void* out, RotaryArgs* a) {
+  if (!r) return "null rotary description";
+  if (r->n_tokens < 0 || r->n_tokens > (1 << 30) || r->n_head < 1 || r->n_kv_head < 1 || r->n_head > (1 << 20) || r->n_kv_head > (1 << 20))
+    return "n_tokens, n_head or n_kv_head out of range";
+  if (const char* why = rotary_axes(a, r->head_dim, r->n_axes, r->sections, r->interleaved, r->theta)) return why;
+  if (!(r->rms_eps >= 0.0f)) return "rms_eps must not be negative";
+  if (!qn != !kn) return "q_norm and k_norm go together";
+  if (r->n_tokens == 0) return nullptr;
+  if (!in || !out || !pos || (qn && !raw)) return "null argument";
+  const uintptr_t all = reinterpret_cast<uintptr_t>(in) | reinterpret_cast<uintptr_t>(out) |
+                        reinterpret_cast<uintptr_t>(qn) | reinterpret_cast<uintptr_t>(kn) |
+                        (qn ? reinterpret_cast<uintptr_t>(raw) : 0);
+  if (all % 16 || reinterpret_cast<uintptr_t>(pos) % 4) return "a pointer is not aligned";
+  a->tokens = r->n_tokens;
+  a->H = r->n_head;
+  a->Hkv = r->n_kv_head;
+  a->eps = r->rms_eps;
+  a->positions = pos;
+  a->q_norm = static_cast<const bf16_t*>(qn);
+  a->k_norm = static_cast<const bf16_t*>(kn);
+  return nullptr;
+}
+
+// layer l's gains
+RotaryArgs layer_rotary(qwen3_model* m, int l) {
+  RotaryArgs a = m->rotary_used;
+  a.q_norm = m->base(B_QNORM) + (size_t)l * m->d.hd;
+  a.k_norm = m->base(B_KNORM) + (size_t)l * m->d.hd;
+  return a;
+}
+
 gpt2_status fail(qwen3_model* m, gpt2_status st, const std::string& why) {
   if (m) m->err = why;
   g_err = why;
@@ -697,6 +761,7 @@ gpt2_status qwen3_forward(qwen3_model* m, const int32_t* d_inputs, const int32_t
   const int BT = (int)d.BT, BTL = (int)d.BTL;
   const int FWD = QWEN3_K_GEMM_FWD, NORM = QWEN3_K_NORM, OTHER = QWEN3_K_OTHER;
   const double rowb = 2.0 * d.BT * d.C;   // bytes of one bf16 [BT, C] activation
+  m->rotary_used = m->rotary;
   TRY(m->run(OTHER, 0.0, 2.0 * rowb + 4.0 * d.BT,
              [&] { return launch_embed_gather(d_inputs, m->base(B_EMBED), m->res(0), d.BT, d.C, m->stream); }));
   bool in_norm_done = false;   // formed with the previous layer's output
@@ -718,6 +783,8 @@ gpt2_status qwen3_forward(qwen3_model* m, const int32_t* d_inputs, const int32_t
     TRY(proj_fwd(m, G_QKV, l, h, m->base(B_QKV) + (size_t)l * d.QKVD * d.C, raw, d.QKVD, nullptr));
     AttnArgs aa = attn_args(m, l);
     TRY(m->run(NORM, 0.0, 4.0 * d.BT * d.QKVD + 4.0 * d.BT * (d.H + d.Hkv), [&] {
+      if (m->rotary_used.positions)
+        return launch_rotary(layer_rotary(m, l), raw, raw, const_cast<bf16_t*>(aa.qkv), 0, m->stream);
       return launch_qknorm_rope_fwd(raw, m->base(B_QNORM) + (size_t)l * d.hd, m->base(B_KNORM) + (size_t)l * d.hd,
                                     m->wf(m->ws.cosT), m->wf(m->ws.sinT), const_cast<bf16_t*>(aa.qkv),
                                     m->af(m->act.rq + l * m->act.s_rq), m->af(m->act.rk + l * m->act.s_rk), BT, d.T,
@@ -846,6 +913,8 @@ gpt2_status qwen3_backward(qwen3_model* m) {
     TRY(m->run(QWEN3_K_ATTN_BWD, 2.0 * attn_fwd_flops(d), 0.0, [&] { return launch_attention_bwd(aa, m->stream); }));
     bf16_t* draw = m->wb(m->ws.draw + l * m->ws.s_draw);
     TRY(m->run(NORM, 0.0, 6.0 * d.BT * d.QKVD + 4.0 * d.BT * (d.H + d.Hkv), [&] {
+      if (m->rotary_used.positions)
+        return launch_rotary(layer_rotary(m, l), m->wb(m->ws.dpacked), raw, draw, 1, m->stream);
       return launch_qknorm_rope_bwd(m->wb(m->ws.dpacked), raw, m->base(B_QNORM) + (size_t)l * d.hd,
                                     m->base(B_KNORM) + (size_t)l * d.hd, m->wf(m->ws.cosT), m->wf(m->ws.sinT),
                                     m->af(m->act.rq + l * m->act.s_rq), m->af(m->act.rk + l * m->act.s_rk), draw, BT,
@@ -894,6 +963,45 @@ gpt2_status qwen3_adamw_step(qwen3_model* m, int64_t step, float* d_grad_norm_ou
   a.seg.decay[0] = 1;   // the configured decay applies to every adapter tensor (all are 2-D)
   TRY(m->run(OPT, 0.0, 30.0 * n, [&] { return launch_adamw(a, m->stream); }));
   m->have_grads = false;
+  return GPT2_OK;
+}
+
+gpt2_status qwen3_rotary_forward(const qwen3_rotary* r, const void* d_qkv, const int32_t* d_positions,
+                                 const void* d_q_norm, const void* d_k_norm, void* d_out, void* hip_stream) {
+  RotaryArgs a{};
+  if (const char* why = rotary_args(r, d_qkv, d_qkv, d_positions, d_q_norm, d_k_norm, d_out, &a))
+    return fail(nullptr, GPT2_ERR_INVALID_ARG, why);
+  const bf16_t* x = static_cast<const bf16_t*>(d_qkv);
+  const hipError_t e = launch_rotary(a, x, x, static_cast<bf16_t*>(d_out), 0, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? GPT2_OK : fail(nullptr, GPT2_ERR_DEVICE, hipGetErrorString(e));
+}
+
+gpt2_status qwen3_rotary_backward(const qwen3_rotary* r, const void* d_dout, const void* d_qkv,
+                                  const int32_t* d_positions, const void* d_q_norm, const void* d_k_norm,
+                                  void* d_dqkv, void* hip_stream) {
+  RotaryArgs a{};
+  if (const char* why = rotary_args(r, d_dout, d_qkv, d_positions, d_q_norm, d_k_norm, d_dqkv, &a))
+    return fail(nullptr, GPT2_ERR_INVALID_ARG, why);
+  const hipError_t e = launch_rotary(a, static_cast<const bf16_t*>(d_dout), static_cast<const bf16_t*>(d_qkv),
+                                     static_cast<bf16_t*>(d_dqkv), 1, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? GPT2_OK : fail(nullptr, GPT2_ERR_DEVICE, hipGetErrorString(e));
+}
+
+gpt2_status qwen3_set_positions(qwen3_model* m, const int32_t* d_positions, int32_t n_axes, const int32_t* sections,
+                                int32_t interleaved) {
+  if (!m) return fail(nullptr, GPT2_ERR_INVALID_ARG, "null model");
+  RotaryArgs a{};
+  if (d_positions) {
+    if (const char* why = rotary_axes(&a, m->d.hd, n_axes, sections, interleaved, m->cfg.rope_theta))
+      return fail(m, GPT2_ERR_INVALID_ARG, why);
+    if (reinterpret_cast<uintptr_t>(d_positions) % 4) return fail(m, GPT2_ERR_INVALID_ARG, "positions are not aligned");
+    a.tokens = (int)m->d.BT;
+    a.H = m->d.H;
+    a.Hkv = m->d.Hkv;
+    a.eps = m->cfg.rms_eps;
+    a.positions = d_positions;
+  }
+  m->rotary = a;
   return GPT2_OK;
 }
 

@@ -43,6 +43,12 @@ class Qwen3Buffers(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in _BUFS]
 
 
+class Rotary(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_tokens", "n_head", "n_kv_head", "head_dim", "n_axes")] + [
+        ("sections", ctypes.c_int32 * 4), ("interleaved", ctypes.c_int32), ("theta", ctypes.c_float),
+        ("rms_eps", ctypes.c_float)]
+
+
 _lib = None
 
 
@@ -62,6 +68,9 @@ def lib():
         "qwen3_forward": (I32, [P, P, P]),
         "qwen3_backward": (I32, [P]),
         "qwen3_adamw_step": (I32, [P, ctypes.c_int64, P]),
+        "qwen3_rotary_forward": (I32, [ctypes.POINTER(Rotary), P, P, P, P, P, P]),
+        "qwen3_rotary_backward": (I32, [ctypes.POINTER(Rotary), P, P, P, P, P, P, P]),
+        "qwen3_set_positions": (I32, [P, P, I32, ctypes.POINTER(I32), I32]),
         "qwen3_muon_size": (I32, [ctypes.POINTER(Qwen3Config), ctypes.POINTER(ctypes.c_size_t)]),
         "qwen3_muon_step": (I32, [P, ctypes.POINTER(Muon), P, ctypes.c_size_t, P]),
         "qwen3_loss": (I32, [P, ctypes.POINTER(F32), P]),
@@ -177,6 +186,68 @@ def unpack_lora(packed: dict, targets, r: int, out_widths: dict) -> dict:
     return {k: v for k, v in res.items() if k[:-2] in targets}
 
 
+def _device_rows(t, name, dtype, like=None, shape=None):
+    """A contiguous device tensor of the dtype, on like's device, or ValueError."""
+    import torch
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()
+            and (like is None or t.device == like.device) and (shape is None or tuple(t.shape) == tuple(shape))):
+        raise ValueError(f"{name} must be a contiguous {dtype} device tensor"
+                         + (f" of shape {tuple(shape)}" if shape is not None else "")
+                         + (" on the other tensors' device" if like is not None else ""))
+    return t
+
+
+def _rotary_args(qkv, positions, n_head, n_kv_head, sections, theta, q_norm, k_norm, eps, interleaved):
+    import torch
+    if not isinstance(qkv, torch.Tensor) or qkv.dim() != 2 or n_head < 1 or n_kv_head < 1:
+        raise ValueError("rows of q | k | v [tokens, (n_head + 2 n_kv_head) head_dim]")
+    _device_rows(qkv, "q | k | v", torch.bfloat16)
+    n, width = qkv.shape
+    hd = width // (n_head + 2 * n_kv_head)
+    if hd * (n_head + 2 * n_kv_head) != width or not 1 <= len(sections) <= 4:
+        raise ValueError("the rows' width must be (n_head + 2 n_kv_head) head_dim, with 1 to 4 sections")
+    _device_rows(positions, "positions", torch.int32, qkv, (len(sections), n))
+    for name, g in (("q_norm", q_norm), ("k_norm", k_norm)):
+        if g is not None:
+            _device_rows(g, name, torch.bfloat16, qkv, (hd,))
+    return Rotary(n, n_head, n_kv_head, hd, len(sections), (ctypes.c_int32 * 4)(*sections), int(bool(interleaved)),
+                  theta, eps)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def rotary(qkv, positions, *, n_head, n_kv_head, sections, theta=1e6, q_norm=None, k_norm=None, eps=1e-6,
+           interleaved=False, out=None):
+    """Head norm (with gains q_norm and k_norm) and rotary embedding of the
+    query and key heads of qkv, bf16 [tokens, (n_head + 2 n_kv_head) head_dim],
+    at positions int32 [axes, tokens]; sections: pairs per axis
+    (qwen3_rotary_forward). On the current stream; out may be qkv."""
+    import torch
+    r = _rotary_args(qkv, positions, n_head, n_kv_head, sections, theta, q_norm, k_norm, eps, interleaved)
+    out = torch.empty_like(qkv) if out is None else _device_rows(out, "out", torch.bfloat16, qkv, qkv.shape)
+    with torch.cuda.device(qkv.device):
+        _check(lib().qwen3_rotary_forward(ctypes.byref(r), qkv.data_ptr(), positions.data_ptr(), _ptr(q_norm),
+                                          _ptr(k_norm), out.data_ptr(), torch.cuda.current_stream().cuda_stream))
+    return out
+
+
+def rotary_backward(dout, qkv, positions, *, n_head, n_kv_head, sections, theta=1e6, q_norm=None, k_norm=None,
+                    eps=1e-6, interleaved=False, out=None):
+    """The gradient of rotary's qkv from that of its result
+    (qwen3_rotary_backward); out may be dout."""
+    import torch
+    r = _rotary_args(qkv, positions, n_head, n_kv_head, sections, theta, q_norm, k_norm, eps, interleaved)
+    _device_rows(dout, "dout", torch.bfloat16, qkv, qkv.shape)
+    out = torch.empty_like(qkv) if out is None else _device_rows(out, "out", torch.bfloat16, qkv, qkv.shape)
+    with torch.cuda.device(qkv.device):
+        _check(lib().qwen3_rotary_backward(ctypes.byref(r), dout.data_ptr(), qkv.data_ptr(), positions.data_ptr(),
+                                           _ptr(q_norm), _ptr(k_norm), out.data_ptr(),
+                                           torch.cuda.current_stream().cuda_stream))
+    return out
+
+
 class Qwen3:
     """One model instance on a torch-owned set of device buffers."""
 
@@ -264,6 +335,17 @@ class Qwen3:
     def adamw_step(self, step: int, norm_out=None):
         ptr = ctypes.c_void_p(norm_out.data_ptr() if norm_out is not None else 0)
         _check(lib().qwen3_adamw_step(self.h, step, ptr), self.h)
+
+    def set_positions(self, positions=None, sections=(64,), interleaved=False):
+        """Positions int32 [axes, B*T] of the tokens from the next forward on,
+        with the pairs per axis (qwen3_set_positions); None: the default."""
+        if positions is not None:
+            _device_rows(positions, "positions", self.torch.int32, self.bufs["workspace"],
+                         (len(sections), self.cfg.B * self.cfg.T))
+        sec = (ctypes.c_int32 * len(sections))(*sections)
+        _check(lib().qwen3_set_positions(self.h, _ptr(positions), len(sections), sec, int(bool(interleaved))), self.h)
+        # the forward and the backward read them; a backward may still take the ones before
+        self._positions = (positions, getattr(self, "_positions", (None,))[0])
 
     def muon_step(self, norm_out=None, momentum=0.95, nesterov=True, iterations=5, scale=0.2):
         """Clip and an orthogonalised update with momentum of every adapter

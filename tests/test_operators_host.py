@@ -73,3 +73,53 @@ def test_muon_sizes():
     assert qb.lib().qwen3_muon_size(ctypes.byref(q), ctypes.byref(n)) == 0 and n.value > 0
     assert qb.lib().qwen3_muon_size(ctypes.byref(q), None) == INVALID
     assert qb.lib().qwen3_muon_step(None, None, None, 0, None) == INVALID
+
+
+# ---- rotary positions with several axes
+
+def rotary_desc(**over):
+    d = dict(n_tokens=8, n_head=4, n_kv_head=2, head_dim=128, n_axes=3, sections=(16, 24, 24), interleaved=0,
+             theta=1e6, rms_eps=1e-6)
+    d.update(over)
+    d["sections"] = (ctypes.c_int32 * 4)(*d["sections"])
+    return qb.Rotary(**d)
+
+
+@pytest.mark.parametrize("over,why", [
+    (dict(n_tokens=-1), "n_tokens"), (dict(n_head=0), "n_head"), (dict(n_kv_head=0), "n_kv_head"),
+    (dict(head_dim=96), "head_dim"), (dict(n_axes=0), "n_axes"), (dict(n_axes=5), "n_axes"),
+    (dict(sections=(16, 24, 25)), "sum"), (dict(sections=(16, 24, 23)), "sum"), (dict(sections=(-1, 41, 24)), "range"),
+    (dict(sections=(0, 40, 24), interleaved=1), "fit"), (dict(theta=0.0), "theta"), (dict(theta=float("inf")), "theta"),
+    (dict(rms_eps=-1.0), "rms_eps"), (dict(rms_eps=float("nan")), "rms_eps")])
+def test_rotary_refuses_descriptions(over, why):
+    d = rotary_desc(**over)
+    L = qb.lib()
+    for call in (lambda: L.qwen3_rotary_forward(ctypes.byref(d), 4096, 4096, 4096, 4096, 8192, None),
+                 lambda: L.qwen3_rotary_backward(ctypes.byref(d), 4096, 4096, 4096, 4096, 4096, 8192, None)):
+        assert call() == INVALID
+        assert why in L.qwen3_last_error(None).decode()
+
+
+@pytest.mark.parametrize("args,why", [
+    ((0, 4096, 4096, 4096, 8192), "null"), ((4096, 0, 4096, 4096, 8192), "null"), ((4096, 4096, 4096, 4096, 0), "null"),
+    ((4096, 4096, 0, 4096, 8192), "together"), ((4096, 4096, 4096, 0, 8192), "together"),
+    ((4104, 4096, 4096, 4096, 8192), "aligned"), ((4096, 4098, 4096, 4096, 8192), "aligned"),
+    ((4096, 4096, 4098, 4096, 8192), "aligned"), ((4096, 4096, 4096, 4096, 8200), "aligned")])
+def test_rotary_refuses_pointers(args, why):
+    L, d = qb.lib(), rotary_desc()
+    assert L.qwen3_rotary_forward(ctypes.byref(d), *args, None) == INVALID
+    assert why in L.qwen3_last_error(None).decode()
+    assert L.qwen3_rotary_forward(None, *args, None) == INVALID
+
+
+def test_rotary_without_tokens_does_nothing():
+    d = rotary_desc(n_tokens=0)
+    assert qb.lib().qwen3_rotary_forward(ctypes.byref(d), None, None, None, None, None, None) == 0
+
+
+def test_rotary_binding_refuses_tensors():
+    torch = pytest.importorskip("torch")
+    x, pos = torch.zeros(4, 8 * 128, dtype=torch.bfloat16), torch.zeros(1, 4, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        qb.rotary(x, pos, n_head=4, n_kv_head=2, sections=(64,))   # not on a device
+    assert qb.lib().qwen3_set_positions(None, None, 1, None, 0) == INVALID
