@@ -1,6 +1,7 @@
 /*
  * qwen3_prompt.h - further entry points of the Qwen3-shaped adapter step
  * (qwen3.h, whose conventions hold here): rotary positions with several axes,
+ * attention over sequences that share a prefix (answers to one prompt), both
  * alone and in the step, and the orthogonalised optimizer step. Calls without
  * a model take the stream to enqueue on; it belongs to the current device, and
  * so do the pointers. qwen3_last_error(NULL) says why such a call failed.
@@ -60,6 +61,70 @@ gpt2_status qwen3_rotary_backward(const qwen3_rotary* r, const void* d_dout,
 gpt2_status qwen3_set_positions(qwen3_model* m, const int32_t* d_positions,
                                 int32_t n_axes, const int32_t* sections,
                                 int32_t interleaved);
+
+/* Attention over packed sequences that share one prefix, such as answers to
+ * one prompt, whose keys and values are then there, and read, once. The rows
+ * are tokens: prefix_len of the prefix, then n_seq sequences one after another
+ * of seq_lens[i] >= 0 tokens. A token sees itself, what precedes it in its own
+ * sequence, and the whole prefix (a token of the prefix: what precedes it
+ * there). Query head h reads key/value head h / (n_head / n_kv_head); scores
+ * are scaled by 1/sqrt(head_dim). prefix_len 0 is packed causal attention,
+ * n_seq 0 one causal sequence.
+ * prefix_queries 1: every token has a query. 0: only the sequences' tokens have
+ * (the prefix was processed before); out, lse and dout then hold their rows
+ * only, and the prefix' queries are not read. */
+typedef struct qwen3_prefix_config {
+  int32_t n_head, n_kv_head, head_dim;   /* head_dim 64 or 128 */
+  int32_t prefix_len, n_seq;
+  int32_t prefix_queries;
+} qwen3_prefix_config;
+
+typedef struct qwen3_prefix qwen3_prefix;   /* opaque host-side handle */
+
+/* A layout and its device buffer, d_plan: qwen3_prefix_size bytes, 256-byte
+ * aligned, the caller's, holding the layout's tables and the calls' scratch.
+ * Laid out once per set of lengths and used by any number of calls, one at a
+ * time: calls (or captured graphs) that may run at the same time take a layout
+ * each. create writes the tables through hip_stream and synchronises it; it
+ * cannot be captured. INVALID_ARG for lengths or sizes out of range (no
+ * query at all; rows beyond 4 GiB), a NULL or unaligned buffer. */
+gpt2_status qwen3_prefix_size(const qwen3_prefix_config* cfg,
+                              const int32_t* seq_lens, size_t* bytes_out);
+gpt2_status qwen3_prefix_create(const qwen3_prefix_config* cfg,
+                                const int32_t* seq_lens, void* d_plan,
+                                size_t plan_bytes, void* hip_stream,
+                                qwen3_prefix** out);
+/* d_qkv bf16 [tokens, (n_head + 2 n_kv_head) * head_dim]; d_out bf16 [rows,
+ * n_head * head_dim], rows the tokens with queries; d_lse fp32 [n_head, rows],
+ * the log-sum-exp of the scaled scores; d_qkv, d_out 16-byte aligned. */
+gpt2_status qwen3_prefix_forward(const qwen3_prefix* p, const void* d_qkv,
+                                 void* d_out, float* d_lse, void* hip_stream);
+/* The gradient of d_qkv to d_dqkv (written whole, not d_qkv itself; zero where
+ * a prefix has no queries) from d_dout, that of d_out, and the forward's d_qkv,
+ * d_out and d_lse. A key's gradient sums over its group's query heads and, in
+ * the prefix, over all sequences, in fp32 and in a fixed order. */
+gpt2_status qwen3_prefix_backward(const qwen3_prefix* p, const void* d_qkv,
+                                  const void* d_out, const float* d_lse,
+                                  const void* d_dout, void* d_dqkv,
+                                  void* hip_stream);
+void qwen3_prefix_destroy(qwen3_prefix* p);
+
+/* The step's tokens as one prefix and sequences over it, from the next
+ * qwen3_forward on: the model's B must be 1 and prefix_len plus the sequences'
+ * lengths its T. Attention is as above, and unless qwen3_set_positions gives
+ * others, a sequence's positions go on from the prefix' end. The prefix' last
+ * token has one target only: let every sequence begin with the prompt's last
+ * token and loss_from begin behind the prefix, and each answer's first token
+ * is predicted within its own sequence. d_plan: qwen3_layout_size bytes,
+ * 256-byte aligned, the caller's to keep while the layout is in use (by the
+ * next forwards, and a backward that follows one). Synchronises the stream.
+ * d_plan NULL goes back to B sequences of T tokens. */
+gpt2_status qwen3_layout_size(const qwen3_model* m, int32_t prefix_len,
+                              int32_t n_seq, const int32_t* seq_lens,
+                              size_t* bytes_out);
+gpt2_status qwen3_set_layout(qwen3_model* m, int32_t prefix_len, int32_t n_seq,
+                             const int32_t* seq_lens, void* d_plan,
+                             size_t plan_bytes);
 
 /* Optimizer step with an orthogonalised update (gpt2.h, gpt2_muon) in place
  * of AdamW: clip as qwen3_adamw_step does, then for every projection's A

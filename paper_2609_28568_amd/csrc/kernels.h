@@ -376,6 +376,42 @@ struct AdamArgs {
 };
 hipError_t launch_adamw(const AdamArgs& a, hipStream_t s);
 
+// ---------------------------------------------------------------- attention over a shared prefix
+// What one workgroup of a key/value head does: of the forward and dQ kernels,
+// rows row..row+127 (token and head of the group, token by token, among the
+// tokens with queries) against tiles f0..f1-1 of 64 keys, the first npre from
+// key 0 on and the others from key `own` on; of the dK/dV kernel, keys
+// row..row+127 against tiles f0..f1-1 of the walk over the tokens t0..t1-1 of
+// one query head of the group after another. slot -1: the result; otherwise the
+// place of its partial result.
+struct PrefixItem {
+  int32_t row, f0, f1, slot;
+  int32_t npre, own;   // forward, dQ
+  int32_t t0, t1;      // dK/dV
+};
+// Partial results slot..slot+parts-1 of rows (or keys) row..row+127 make one.
+struct PrefixJoin {
+  int32_t row, slot, parts, unused;
+};
+struct PrefixArgs {
+  int N, P, q0, nq, H, Hkv, hd;   // tokens; of the prefix; first with a query, and how many
+  const bf16_t* qkv;              // [N][(H + 2 Hkv) hd]
+  bf16_t* out;                    // [nq][H hd]
+  float* lse;                     // [H][nq]
+  const bf16_t* dout;
+  bf16_t* dqkv;
+  float* dsum;                    // [H][nq], scratch of the backward
+  float* part;                    // partial results
+  const int32_t *first, *end;     // per token, see prefix.hip
+  const PrefixItem *items, *kitems;
+  const PrefixJoin *joins, *kjoins;
+  int nitems, njoins, nkitems, nkjoins;
+};
+// floats of a partial result of one key/value head: forward (0), dQ (1), dK/dV (2)
+size_t prefix_part_floats(int hd, int which);
+hipError_t launch_prefix_fwd(const PrefixArgs& a, hipStream_t s);
+hipError_t launch_prefix_bwd(const PrefixArgs& a, hipStream_t s);
+
 // ---------------------------------------------------------------- rotary positions with several axes
 // Rows q [H*hd] | k [Hkv*hd] | v [Hkv*hd] of `tokens` tokens; positions
 // [axes][tokens]; gains null: no norm. Forward: in = the rows. Backward: in =

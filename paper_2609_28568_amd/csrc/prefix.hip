@@ -1,0 +1,617 @@
+// Attention over packed sequences that share one prefix. Rows of q|k|v are
+// tokens: the prefix 0..P-1, then the sequences one after another. Token t sees
+// token j <= t of the prefix, and of its own sequence:
+//
+//   j <= t and (j < P or first[t] <= j),   first[t] = first token of t's sequence
+//
+// or, from the key's side, j <= t < end[j], end[j] = the token after j's
+// sequence (all tokens, for a key of the prefix). The prefix' keys are walked
+// once for all sequences: a workgroup's 128 rows are any 128 consecutive rows,
+// whatever sequences they belong to, so even sequences of one token fill its
+// MFMA tiles, and every key tile it loads serves them all.
+//
+// Rows of the forward and dQ kernels are (token, query head of a group) pairs,
+// token by token, so a group's heads share the loads of its key head too. The
+// dK/dV kernel walks the tokens of one query head after another.
+//
+// Which workgroup walks what is laid down by the host once per layout, in items
+// (prefix.cpp): rows and a range of tiles. Long walks are dealt to several
+// workgroups where the items are few, with fp32 partial results joined by a
+// second launch in a fixed order.
+//
+// The tile arithmetic is attention.hip's: S^T = K Q^T with one row per lane,
+// probabilities handed to the next MFMA from the accumulator registers.
+#include <type_traits>
+
+#include "attn_tile.h"
+#include "common.h"
+#include "kernels.h"
+
+namespace {
+
+// Item decoding: blocks run through the key/value heads of an item, then the
+// next item, so that with 8 of them each keeps to one XCD's L2.
+struct Where {
+  PrefixItem it;
+  int j;   // key/value head
+};
+DEV Where where(const PrefixArgs& a, const PrefixItem* items) {
+  const int b = blockIdx.x;
+  Where w;
+  w.it = items[b / a.Hkv];
+  w.j = b % a.Hkv;
+  return w;
+}
+
+// One row (token, query head) of the forward and dQ kernels: the lane's own,
+// rows past the end taken as the last one.
+struct Row {
+  int t, rq, h;      // token; its place among the tokens with queries; query head
+  int first;         // first key of its own sequence it sees (none in the prefix)
+  int t0, t1;        // tokens of the wave's first and last row
+  int first0, first1;   // smallest and largest first key among the wave's rows in sequences
+  bool on;
+};
+DEV Row row_of(const PrefixArgs& a, int row, int j, int lane) {
+  const int G = a.H / a.Hkv, rows = a.nq * G;
+  const int r = min(row + (lane & 31), rows - 1);
+  Row o;
+  o.on = row + (lane & 31) < rows;
+  o.rq = r / G;
+  o.h = j * G + r - o.rq * G;
+  o.t = a.q0 + o.rq;
+  o.first = a.first[o.t];
+  o.t0 = __builtin_amdgcn_readfirstlane(o.t);
+  o.t1 = __builtin_amdgcn_readlane(o.t, 31);
+  o.first0 = o.t0 >= a.P ? __builtin_amdgcn_readfirstlane(o.first) : a.P;
+  o.first1 = __builtin_amdgcn_readlane(o.first, 31);
+  return o;
+}
+
+// What a wave's rows see of the tile of 64 keys at kv0.
+enum Sight { NONE, SOME, ALL };
+DEV Sight sight(const PrefixArgs& a, const Row& r, int kv0, bool own) {
+  if (!own) return kv0 > r.t1 ? NONE : kv0 + TILE - 1 <= min(r.t0, a.P - 1) ? ALL : SOME;
+  if (r.t1 < a.P || kv0 > r.t1 || kv0 + TILE - 1 < r.first0) return NONE;
+  return r.t0 >= a.P && kv0 >= r.first1 && kv0 + TILE - 1 <= r.t0 ? ALL : SOME;
+}
+
+// Keys lo..hi of the segment that a lane's row sees.
+DEV void seen(const PrefixArgs& a, const Row& r, bool own, int& lo, int& hi) {
+  lo = own ? (r.t >= a.P ? r.first : r.t + 1) : 0;
+  hi = own ? r.t : min(r.t, a.P - 1);
+}
+
+// Key and value tiles of an item's walk, double-buffered: tile f < it.npre is
+// keys 64 f.. of the prefix, the others follow from it.own on.
+template <int HD>
+struct KeyWalk {
+  using S = Shape<HD>;
+  v4i32 rs;
+  uint32_t koff, voff;
+  int ld, npre, own;
+  DEV void init(const PrefixArgs& a, const Where& w) {
+    ld = (a.H + 2 * a.Hkv) * HD;
+    rs = make_rsrc(a.qkv, (uint32_t)((size_t)a.N * ld * 2));
+    koff = (uint32_t)((a.H + w.j) * HD * 2);
+    voff = koff + (uint32_t)(a.Hkv * HD * 2);
+    npre = w.it.npre;
+    own = w.it.own;
+  }
+  DEV bool is_own(int f) const { return f >= npre; }
+  DEV int key0(int f) const { return f < npre ? f * TILE : own + (f - npre) * TILE; }
+  DEV void issue(int f, lds_char_t* st, int wave, int lane) const {
+    constexpr int U = HD / 8, INSTR = TILE * U / 64;
+    const uint32_t r0 = (uint32_t)key0(f);
+#pragma unroll
+    for (int i = 0; i < INSTR / 4; ++i) {
+      const int ins = wave + 4 * i, u = ins * 64 + lane;
+      const int row = u / U, c = unit<HD>(row, u % U) - row * U;   // the XOR is its own inverse
+      const uint32_t off = ((r0 + (uint32_t)row) * (uint32_t)ld + (uint32_t)(c * 8)) * 2u;
+      dma16(rs, koff + off, lds_addr(st + ins * 1024));
+      dma16(rs, voff + off, lds_addr(st + S::TBA + ins * 1024));
+    }
+  }
+};
+
+DEV size_t part_at(const PrefixArgs& a, int slot, int j, size_t floats) {
+  return ((size_t)slot * a.Hkv + j) * floats;
+}
+constexpr size_t fwd_part(int hd) { return (size_t)BQ * (hd + 2); }    // O [128][hd], max [128], sum [128]
+constexpr size_t dq_part(int hd) { return (size_t)BQ * hd; }
+constexpr size_t dkdv_part(int hd) { return (size_t)2 * BQ * hd; }     // dK, dV [128][hd]
+
+template <int HD>
+__global__ __launch_bounds__(256, 2) void prefix_fwd_kernel(PrefixArgs a) {
+  using S = Shape<HD>;
+  __shared__ __attribute__((aligned(1024))) char smem_raw[2 * 2 * S::TBA];   // 2 stages x (K, V)
+  lds_char_t* smem = (lds_char_t*)smem_raw;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lq = lane & 31, g = lane >> 5;
+  const Where w = where(a, a.items);
+  const Row r = row_of(a, w.it.row + 32 * wave, w.j, lane);
+  KeyWalk<HD> keys;
+  keys.init(a, w);
+
+  bf16x8 qf[S::KS];
+  const bf16_t* q = a.qkv + (size_t)r.t * keys.ld + r.h * HD;
+#pragma unroll
+  for (int s = 0; s < S::KS; ++s) qf[s] = as_bf16x8(*reinterpret_cast<const uint4*>(q + 16 * s + 8 * g));
+  floatx16 o[S::DT];
+#pragma unroll
+  for (int d = 0; d < S::DT; ++d) zero(o[d]);
+  float m_run = -INFINITY, l_run = 0.0f;
+  const float sc = LOG2E / sqrtf((float)HD);
+
+  auto stage = [&](int f) { return smem + ((f - w.it.f0) & 1) * 2 * S::TBA; };
+  keys.issue(w.it.f0, stage(w.it.f0), wave, lane);
+  for (int f = w.it.f0; f < w.it.f1; ++f) {
+    wait_vmcnt<0>();
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // this wave's reads of the stage that the next loads overwrite are done
+    block_barrier();
+    if (f + 1 < w.it.f1) keys.issue(f + 1, stage(f + 1), wave, lane);
+    const int kv0 = keys.key0(f);
+    const bool own = keys.is_own(f);
+    const Sight see = sight(a, r, kv0, own);
+    if (see == NONE) continue;
+    const lds_char_t* Ks = stage(f);
+    const lds_char_t* Vs = Ks + S::TBA;
+
+    floatx16 s[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      zero(s[t]);
+#pragma unroll
+      for (int k = 0; k < S::KS; ++k) s[t] = mfma32(read_row<HD>(Ks, 32 * t + lq, 2 * k + g), qf[k], s[t]);
+    }
+    float mt = -INFINITY;
+    auto mask_max = [&](auto masked) {
+      int lo, hi;
+      seen(a, r, own, lo, hi);
+      lo -= kv0 + 4 * g;
+      hi -= kv0 + 4 * g;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float x = s[t][e];
+          const int k = 32 * t + acc_row(e, 0);
+          if constexpr (decltype(masked)::value) x = k >= lo && k <= hi ? x : -INFINITY;
+          s[t][e] = x;
+          mt = fmaxf(mt, x);
+        }
+    };
+    if (see == SOME) mask_max(std::true_type{});
+    else mask_max(std::false_type{});
+    mt = max32(mt) * sc;
+    const bool grow = mt > m_run + RESCALE_SLACK;
+    if (__ballot(grow) != 0) {
+      const float alpha = grow ? fast_exp2(m_run - mt) : 1.0f;
+      m_run = grow ? mt : m_run;
+      l_run *= alpha;
+#pragma unroll
+      for (int d = 0; d < S::DT; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[d][e] *= alpha;
+    }
+    // a row that has seen nothing yet (its keys come later) has no maximum
+    const float shift = m_run == -INFINITY ? 0.0f : m_run;
+    float rsum = 0.0f;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float p = fast_exp2(fmaf(s[t][e], sc, -shift));
+        s[t][e] = p;
+        rsum += p;
+      }
+    l_run += sum32(rsum);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh) {
+        const bf16x8 pf = acc_slots(s[t], hh);
+#pragma unroll
+        for (int d = 0; d < S::DT; ++d) o[d] = mfma32(read_tr<HD>(Vs, 32 * d, 32 * t + 16 * hh, lane), pf, o[d]);
+      }
+  }
+
+  if (!r.on) return;
+  if (w.it.slot >= 0) {
+    float* part = a.part + part_at(a, w.it.slot, w.j, fwd_part(HD));
+    const int row = 32 * wave + lq;
+#pragma unroll
+    for (int d = 0; d < S::DT; ++d)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        *reinterpret_cast<float4*>(part + (size_t)row * HD + 32 * d + 8 * c + 4 * g) =
+            make_float4(o[d][4 * c], o[d][4 * c + 1], o[d][4 * c + 2], o[d][4 * c + 3]);
+    if (g == 0) {
+      part[(size_t)BQ * HD + row] = m_run;
+      part[(size_t)BQ * HD + BQ + row] = l_run;
+    }
+    return;
+  }
+  const float inv = 1.0f / l_run;
+  bf16_t* out = a.out + ((size_t)r.rq * a.H + r.h) * HD;
+#pragma unroll
+  for (int d = 0; d < S::DT; ++d)
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      *reinterpret_cast<uint2*>(out + 32 * d + 8 * c + 4 * g) =
+          make_uint2(pack2(o[d][4 * c] * inv, o[d][4 * c + 1] * inv),
+                     pack2(o[d][4 * c + 2] * inv, o[d][4 * c + 3] * inv));
+  if (g == 0) a.lse[(size_t)r.h * a.nq + r.rq] = (m_run + log2f(l_run)) * LN2;
+}
+
+// The parts of a row merged: HD/8 lanes a row, 8 elements each.
+template <int HD>
+__global__ __launch_bounds__(256) void prefix_fwd_join_kernel(PrefixArgs a) {
+  constexpr int LANES = HD / 8, ROWS = 256 / LANES;
+  const int b = blockIdx.x, j = b % a.Hkv;
+  const PrefixJoin jn = a.joins[b / a.Hkv];
+  const int G = a.H / a.Hkv, row = blockIdx.y * ROWS + threadIdx.x / LANES, c = threadIdx.x % LANES * 8;
+  const int rr = jn.row + row;
+  if (rr >= a.nq * G) return;
+  float m = -INFINITY;
+  for (int k = 0; k < jn.parts; ++k)
+    m = fmaxf(m, a.part[part_at(a, jn.slot + k, j, fwd_part(HD)) + (size_t)BQ * HD + row]);
+  float l = 0.0f, o[8] = {};
+#pragma unroll 4
+  for (int k = 0; k < jn.parts; ++k) {
+    const float* part = a.part + part_at(a, jn.slot + k, j, fwd_part(HD));
+    const float f = fast_exp2(part[(size_t)BQ * HD + row] - m);
+    const float4 x = *reinterpret_cast<const float4*>(part + (size_t)row * HD + c);
+    const float4 y = *reinterpret_cast<const float4*>(part + (size_t)row * HD + c + 4);
+    l += f * part[(size_t)BQ * HD + BQ + row];
+    o[0] += f * x.x; o[1] += f * x.y; o[2] += f * x.z; o[3] += f * x.w;
+    o[4] += f * y.x; o[5] += f * y.y; o[6] += f * y.z; o[7] += f * y.w;
+  }
+  const float inv = 1.0f / l;
+  const int rq = rr / G, h = j * G + rr - rq * G;
+  *reinterpret_cast<uint4*>(a.out + ((size_t)rq * a.H + h) * HD + c) =
+      make_uint4(pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv), pack2(o[4] * inv, o[5] * inv),
+                 pack2(o[6] * inv, o[7] * inv));
+  if (c == 0) a.lse[(size_t)h * a.nq + rq] = (m + log2f(l)) * LN2;
+}
+
+// D = rowsum(dO * O) of every row with a query, HD/8 lanes each; a prefix
+// without queries takes a zero gradient there.
+template <int HD>
+__global__ __launch_bounds__(256) void prefix_dsum_kernel(PrefixArgs a) {
+  constexpr int LANES = HD / 8;
+  const long i = ((long)blockIdx.x * 256 + threadIdx.x) / LANES;
+  const int c = threadIdx.x % LANES * 8, ld = (a.H + 2 * a.Hkv) * HD;
+  if (i >= (long)a.N * a.H) return;
+  const int t = (int)(i / a.H), h = (int)(i % a.H);
+  if (t < a.q0) {
+    *reinterpret_cast<uint4*>(a.dqkv + (size_t)t * ld + h * HD + c) = make_uint4(0, 0, 0, 0);
+    return;
+  }
+  const size_t at = ((size_t)(t - a.q0) * a.H + h) * HD + c;
+  const uint4 d = *reinterpret_cast<const uint4*>(a.dout + at), o = *reinterpret_cast<const uint4*>(a.out + at);
+  float s = lo_f(d.x) * lo_f(o.x) + hi_f(d.x) * hi_f(o.x) + lo_f(d.y) * lo_f(o.y) + hi_f(d.y) * hi_f(o.y);
+  s += lo_f(d.z) * lo_f(o.z) + hi_f(d.z) * hi_f(o.z) + lo_f(d.w) * lo_f(o.w) + hi_f(d.w) * hi_f(o.w);
+#pragma unroll
+  for (int m = LANES / 2; m; m >>= 1) s += __shfl_xor(s, m);
+  if (c == 0) a.dsum[(size_t)h * a.nq + t - a.q0] = s;
+}
+
+// dQ of 128 rows, walking the forward's tiles: dS = P (dO V^T - D), dQ = dS K.
+template <int HD>
+__global__ __launch_bounds__(256, 2) void prefix_dq_kernel(PrefixArgs a) {
+  using S = Shape<HD>;
+  __shared__ __attribute__((aligned(1024))) char smem_raw[2 * 2 * S::TBA];   // 2 stages x (K, V)
+  lds_char_t* smem = (lds_char_t*)smem_raw;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lq = lane & 31, g = lane >> 5;
+  const Where w = where(a, a.items);
+  const Row r = row_of(a, w.it.row + 32 * wave, w.j, lane);
+  KeyWalk<HD> keys;
+  keys.init(a, w);
+
+  bf16x8 qf[S::KS], df[S::KS];
+  const bf16_t* q = a.qkv + (size_t)r.t * keys.ld + r.h * HD;
+  const bf16_t* dout = a.dout + ((size_t)r.rq * a.H + r.h) * HD;
+#pragma unroll
+  for (int s = 0; s < S::KS; ++s) {
+    qf[s] = as_bf16x8(*reinterpret_cast<const uint4*>(q + 16 * s + 8 * g));
+    df[s] = as_bf16x8(*reinterpret_cast<const uint4*>(dout + 16 * s + 8 * g));
+  }
+  const float lse2 = a.lse[(size_t)r.h * a.nq + r.rq] * LOG2E, dsum = a.dsum[(size_t)r.h * a.nq + r.rq];
+  floatx16 dq[S::DT];
+#pragma unroll
+  for (int d = 0; d < S::DT; ++d) zero(dq[d]);
+  const float scale = 1.0f / sqrtf((float)HD);
+  const float sc = scale * LOG2E;
+
+  auto stage = [&](int f) { return smem + ((f - w.it.f0) & 1) * 2 * S::TBA; };
+  keys.issue(w.it.f0, stage(w.it.f0), wave, lane);
+  for (int f = w.it.f0; f < w.it.f1; ++f) {
+    wait_vmcnt<0>();
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // this wave's reads of the stage that the next loads overwrite are done
+    block_barrier();
+    if (f + 1 < w.it.f1) keys.issue(f + 1, stage(f + 1), wave, lane);
+    const int kv0 = keys.key0(f);
+    const bool own = keys.is_own(f);
+    const Sight see = sight(a, r, kv0, own);
+    if (see == NONE) continue;
+    const lds_char_t* Ks = stage(f);
+    const lds_char_t* Vs = Ks + S::TBA;
+    int lo, hi;
+    seen(a, r, own, lo, hi);
+
+    floatx16 ds[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      floatx16 p;
+      zero(p);
+      zero(ds[t]);
+#pragma unroll
+      for (int k = 0; k < S::KS; ++k) {
+        p = mfma32(read_row<HD>(Ks, 32 * t + lq, 2 * k + g), qf[k], p);
+        ds[t] = mfma32(read_row<HD>(Vs, 32 * t + lq, 2 * k + g), df[k], ds[t]);
+      }
+      auto probs = [&](auto masked) {
+        const int at = kv0 + 32 * t + 4 * g;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float pv = fast_exp2(p[e] * sc - lse2);
+          if constexpr (decltype(masked)::value) pv = acc_row(e, 0) >= lo - at && acc_row(e, 0) <= hi - at ? pv : 0.0f;
+          ds[t][e] = pv * (ds[t][e] - dsum);
+        }
+      };
+      if (see == SOME) probs(std::true_type{});
+      else probs(std::false_type{});
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh) {
+        const bf16x8 sf = acc_slots(ds[t], hh);
+#pragma unroll
+        for (int d = 0; d < S::DT; ++d) dq[d] = mfma32(read_tr<HD>(Ks, 32 * d, 32 * t + 16 * hh, lane), sf, dq[d]);
+      }
+  }
+
+  if (!r.on) return;
+  if (w.it.slot >= 0) {
+    float* part = a.part + part_at(a, w.it.slot, w.j, dq_part(HD)) + (size_t)(32 * wave + lq) * HD;
+#pragma unroll
+    for (int d = 0; d < S::DT; ++d)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        *reinterpret_cast<float4*>(part + 32 * d + 8 * c + 4 * g) =
+            make_float4(dq[d][4 * c], dq[d][4 * c + 1], dq[d][4 * c + 2], dq[d][4 * c + 3]);
+    return;
+  }
+  bf16_t* dst = a.dqkv + (size_t)r.t * keys.ld + r.h * HD;
+#pragma unroll
+  for (int d = 0; d < S::DT; ++d)
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      *reinterpret_cast<uint2*>(dst + 32 * d + 8 * c + 4 * g) =
+          make_uint2(pack2(dq[d][4 * c] * scale, dq[d][4 * c + 1] * scale),
+                     pack2(dq[d][4 * c + 2] * scale, dq[d][4 * c + 3] * scale));
+}
+
+// The parts of 128 rows added up: dQ rows (token, head of the group), or dK and
+// dV rows of a key/value head.
+template <int HD, bool KEYS>
+__global__ __launch_bounds__(256) void prefix_sum_join_kernel(PrefixArgs a) {
+  constexpr int LANES = HD / 8, ROWS = 256 / LANES;
+  constexpr size_t PART = KEYS ? dkdv_part(HD) : dq_part(HD);
+  const int b = blockIdx.x, j = b % a.Hkv, ld = (a.H + 2 * a.Hkv) * HD;
+  const PrefixJoin jn = (KEYS ? a.kjoins : a.joins)[b / a.Hkv];
+  const int G = a.H / a.Hkv, c = threadIdx.x % LANES * 8;
+  const int row = blockIdx.y * ROWS + threadIdx.x / LANES;   // dV's rows follow dK's
+  const bool is_v = KEYS && row >= BQ;
+  const int rr = jn.row + (is_v ? row - BQ : row);
+  if (rr >= (KEYS ? (jn.row < a.P ? a.P : a.N) : a.nq * G)) return;
+  float o[8] = {};
+#pragma unroll 4
+  for (int k = 0; k < jn.parts; ++k) {
+    const float* part = a.part + part_at(a, jn.slot + k, j, PART) + (size_t)row * HD + c;
+    const float4 x = *reinterpret_cast<const float4*>(part), y = *reinterpret_cast<const float4*>(part + 4);
+    o[0] += x.x; o[1] += x.y; o[2] += x.z; o[3] += x.w;
+    o[4] += y.x; o[5] += y.y; o[6] += y.z; o[7] += y.w;
+  }
+  const float f = is_v ? 1.0f : 1.0f / sqrtf((float)HD);
+  const int rq = rr / G;
+  const size_t at = KEYS ? (size_t)rr * ld + (a.H + j + (is_v ? a.Hkv : 0)) * HD
+                         : (size_t)(a.q0 + rq) * ld + (j * G + rr - rq * G) * HD;
+  *reinterpret_cast<uint4*>(a.dqkv + at + c) =
+      make_uint4(pack2(o[0] * f, o[1] * f), pack2(o[2] * f, o[3] * f), pack2(o[4] * f, o[5] * f),
+                 pack2(o[6] * f, o[7] * f));
+}
+
+// dK, dV of 128 keys with eight waves, as attention.hip's: wave w owns keys
+// 32 (w % 4)..+31 and the query half w / 4 of every tile of 64 queries; the
+// keys' rows stay in LDS. Query tile f of the walk is tile f % nt of the tokens
+// it.t0..it.t1-1, head f / nt of the group.
+template <int HD>
+__global__ __launch_bounds__(512, 1) void prefix_dkdv_kernel(PrefixArgs a) {
+  using S = Shape<HD>;
+  constexpr int KVB = BQ * HD * 2;             // one 128-row block of K or V
+  constexpr int STAGE = 2 * S::TBA + 1024;     // Q tile, dO tile, lse and D rows
+  constexpr int SMEM_T = 2 * KVB + 2 * STAGE;
+  constexpr int NACC = 2 * S::DT * 16;         // dK and dV registers per lane
+  constexpr int SMEM = SMEM_T > 4 * NACC * 64 * 4 ? SMEM_T : 4 * NACC * 64 * 4;
+  __shared__ __attribute__((aligned(1024))) char smem_raw[SMEM];
+  lds_char_t* smem = (lds_char_t*)smem_raw;
+  lds_char_t* Ks = smem;
+  lds_char_t* Vs = smem + KVB;
+  lds_char_t* stages = smem + 2 * KVB;
+  const Where w = where(a, a.kitems);
+  const int H = a.H, C = H * HD, Hkv = a.Hkv, ld = (H + 2 * Hkv) * HD, G = H / Hkv, j = w.j;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kw = wave & 3, th = wave >> 2;   // key group, query half
+  const int lk = lane & 31, g = lane >> 5;
+  const int k0 = w.it.row, kend = k0 < a.P ? a.P : a.N;
+  const int kv0w = k0 + kw * 32, kv = kv0w + lk;
+  // queries kv..end-1 see key kv
+  const int end = a.end[min(kv, kend - 1)];
+  const int end0 = __builtin_amdgcn_readfirstlane(end), end1 = __builtin_amdgcn_readlane(end, 31);
+  const v4i32 rq = make_rsrc(a.qkv, (uint32_t)((size_t)a.N * ld * 2));
+  const v4i32 rd = make_rsrc(a.dout, (uint32_t)((size_t)a.nq * C * 2));
+  const v4i32 rl = make_rsrc(a.lse, (uint32_t)((size_t)H * a.nq * 4));
+  const v4i32 rD = make_rsrc(a.dsum, (uint32_t)((size_t)H * a.nq * 4));
+
+  floatx16 dk[S::DT], dv[S::DT];
+#pragma unroll
+  for (int d = 0; d < S::DT; ++d) {
+    zero(dk[d]);
+    zero(dv[d]);
+  }
+  const float scale = 1.0f / sqrtf((float)HD);
+  const float sc = scale * LOG2E;
+  const int nt = (w.it.t1 - w.it.t0 + TILE - 1) / TILE;
+  auto issue = [&](int f) {
+    lds_char_t* st = stages + ((f - w.it.f0) & 1) * STAGE;
+    const int gi = f / nt, h = j * G + gi;
+    const int t = w.it.t0 + (f - gi * nt) * TILE, rt = t - a.q0;
+    issue_rows8<HD>(rq, (uint32_t)(h * HD) * 2u, t, ld, st, wave, lane);
+    issue_rows8<HD>(rd, (uint32_t)(h * HD) * 2u, rt, C, st + S::TBA, wave, lane);
+    // the tile's 64 log-sum-exp and D values (256 bytes each): 16 lanes
+    if (wave == 0 && lane < 16) {
+      const uint32_t off = ((uint32_t)h * (uint32_t)a.nq + (uint32_t)rt) * 4u + 16u * lane;
+      dma16(rl, off, lds_addr(st + 2 * S::TBA));
+      dma16(rD, off, lds_addr(st + 2 * S::TBA + 256));
+    }
+  };
+  if (w.it.f0 < w.it.f1) {
+    const uint32_t koff = (uint32_t)((H + j) * HD) * 2u, voff = koff + (uint32_t)(Hkv * HD) * 2u;
+    issue_rows8<HD>(rq, koff, k0, ld, Ks, wave, lane);
+    issue_rows8<HD>(rq, koff, k0 + TILE, ld, Ks + S::TB, wave, lane);
+    issue_rows8<HD>(rq, voff, k0, ld, Vs, wave, lane);
+    issue_rows8<HD>(rq, voff, k0 + TILE, ld, Vs + S::TB, wave, lane);
+    issue(w.it.f0);
+  }
+  for (int f = w.it.f0; f < w.it.f1; ++f) {
+    wait_vmcnt<0>();
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // this wave's reads of the stage that the next loads overwrite are done
+    block_barrier();
+    if (f + 1 < w.it.f1) issue(f + 1);
+    const int qh0 = w.it.t0 + f % nt * TILE + 32 * th;   // this wave's first query
+    if (qh0 + 31 < kv0w || qh0 >= end1) continue;   // none of its queries sees its keys
+    const lds_char_t* Qs = stages + ((f - w.it.f0) & 1) * STAGE;
+    const lds_char_t* Ds = Qs + S::TBA;
+    const lds_char_t* lr = Qs + 2 * S::TBA;   // lse [64] then D [64], fp32
+    const bool some = qh0 < kv0w + 31 || qh0 + 32 > end0 || kv0w + 32 > kend;
+
+    floatx16 p, ds;
+    zero(p);
+    zero(ds);
+#pragma unroll
+    for (int k = 0; k < S::KS; ++k) {
+      p = mfma32(read_row<HD>(Qs, 32 * th + lk, 2 * k + g), read_row<HD>(Ks, 32 * kw + lk, 2 * k + g), p);
+      ds = mfma32(read_row<HD>(Ds, 32 * th + lk, 2 * k + g), read_row<HD>(Vs, 32 * kw + lk, 2 * k + g), ds);
+    }
+    auto probs = [&](auto masked) {
+#pragma unroll
+      for (int c4 = 0; c4 < 4; ++c4) {
+        const int qi = 8 * c4 + 4 * g;   // 4 consecutive queries of the half
+        const v4f32 l4 = *reinterpret_cast<const lds_v4f32_t*>(lr + 4 * (32 * th + qi));
+        const v4f32 d4 = *reinterpret_cast<const lds_v4f32_t*>(lr + 256 + 4 * (32 * th + qi));
+        const int qlo = kv - qh0 - qi, qhi = (kv < kend ? end : 0) - qh0 - qi;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = 4 * c4 + e;
+          float pv = fast_exp2(p[i] * sc - l4[e] * LOG2E);
+          float dd = ds[i] - d4[e];
+          if constexpr (decltype(masked)::value) {
+            // rows past the last query hold no log-sum-exp or D of this head: both factors go
+            const bool in = e >= qlo && e < qhi;
+            pv = in ? pv : 0.0f;
+            dd = in ? dd : 0.0f;
+          }
+          p[i] = pv;
+          ds[i] = pv * dd;
+        }
+      }
+    };
+    if (some) probs(std::true_type{});
+    else probs(std::false_type{});
+#pragma unroll
+    for (int hh = 0; hh < 2; ++hh) {
+      const bf16x8 pf = acc_slots(p, hh), sf = acc_slots(ds, hh);
+#pragma unroll
+      for (int d = 0; d < S::DT; ++d) {
+        dv[d] = mfma32(read_tr<HD>(Ds, 32 * d, 32 * th + 16 * hh, lane), pf, dv[d]);
+        dk[d] = mfma32(read_tr<HD>(Qs, 32 * d, 32 * th + 16 * hh, lane), sf, dk[d]);
+      }
+    }
+  }
+
+  // the second query half's waves hand their partial sums to the first's
+  __syncthreads();
+  lds_v4f32_t* red = (lds_v4f32_t*)smem_raw + kw * (NACC / 4) * 64 + lane;
+  if (th == 1) {
+#pragma unroll
+    for (int d = 0; d < S::DT; ++d)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        red[((2 * d) * 4 + c) * 64] = v4f32{dk[d][4 * c], dk[d][4 * c + 1], dk[d][4 * c + 2], dk[d][4 * c + 3]};
+        red[((2 * d + 1) * 4 + c) * 64] = v4f32{dv[d][4 * c], dv[d][4 * c + 1], dv[d][4 * c + 2], dv[d][4 * c + 3]};
+      }
+  }
+  __syncthreads();
+  if (th == 1 || kv >= kend) return;
+  bf16_t* dst = a.dqkv + (size_t)kv * ld + (H + j) * HD;
+  float* part = w.it.slot >= 0 ? a.part + part_at(a, w.it.slot, j, dkdv_part(HD)) + (size_t)(32 * kw + lk) * HD : nullptr;
+#pragma unroll
+  for (int d = 0; d < S::DT; ++d)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const v4f32 ok = red[((2 * d) * 4 + c) * 64], ov = red[((2 * d + 1) * 4 + c) * 64];
+      const int dd = 32 * d + 8 * c + 4 * g;
+      const float4 k4 = make_float4(dk[d][4 * c] + ok.x, dk[d][4 * c + 1] + ok.y, dk[d][4 * c + 2] + ok.z,
+                                    dk[d][4 * c + 3] + ok.w);
+      const float4 v4 = make_float4(dv[d][4 * c] + ov.x, dv[d][4 * c + 1] + ov.y, dv[d][4 * c + 2] + ov.z,
+                                    dv[d][4 * c + 3] + ov.w);
+      if (part) {
+        *reinterpret_cast<float4*>(part + dd) = k4;
+        *reinterpret_cast<float4*>(part + (size_t)BQ * HD + dd) = v4;
+      } else {
+        *reinterpret_cast<uint2*>(dst + dd) =
+            make_uint2(pack2(k4.x * scale, k4.y * scale), pack2(k4.z * scale, k4.w * scale));
+        *reinterpret_cast<uint2*>(dst + Hkv * HD + dd) = make_uint2(pack2(v4.x, v4.y), pack2(v4.z, v4.w));
+      }
+    }
+}
+
+template <int HD>
+hipError_t fwd_t(const PrefixArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(prefix_fwd_kernel<HD>, dim3(a.nitems * a.Hkv), dim3(256), 0, s, a);
+  if (a.njoins)
+    hipLaunchKernelGGL(prefix_fwd_join_kernel<HD>, dim3(a.njoins * a.Hkv, BQ * HD / 2048), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+template <int HD>
+hipError_t bwd_t(const PrefixArgs& a, hipStream_t s) {
+  const long lanes = (long)a.N * a.H * (HD / 8);
+  hipLaunchKernelGGL(prefix_dsum_kernel<HD>, dim3((unsigned)((lanes + 255) / 256)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL(prefix_dq_kernel<HD>, dim3(a.nitems * a.Hkv), dim3(256), 0, s, a);
+  if (a.njoins)
+    hipLaunchKernelGGL((prefix_sum_join_kernel<HD, false>), dim3(a.njoins * a.Hkv, BQ * HD / 2048), dim3(256), 0, s, a);
+  hipLaunchKernelGGL(prefix_dkdv_kernel<HD>, dim3(a.nkitems * a.Hkv), dim3(512), 0, s, a);
+  if (a.nkjoins)
+    hipLaunchKernelGGL((prefix_sum_join_kernel<HD, true>), dim3(a.nkjoins * a.Hkv, 2 * BQ * HD / 2048), dim3(256), 0, s,
+                       a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t prefix_part_floats(int hd, int which) {
+  return which == 0 ? fwd_part(hd) : which == 1 ? dq_part(hd) : dkdv_part(hd);
+}
+
+hipError_t launch_prefix_fwd(const PrefixArgs& a, hipStream_t s) {
+  return a.hd == 64 ? fwd_t<64>(a, s) : a.hd == 128 ? fwd_t<128>(a, s) : hipErrorInvalidValue;
+}
+
+hipError_t launch_prefix_bwd(const PrefixArgs& a, hipStream_t s) {
+  return a.hd == 64 ? bwd_t<64>(a, s) : a.hd == 128 ? bwd_t<128>(a, s) : hipErrorInvalidValue;
+}

@@ -22,6 +22,7 @@
 
 #include "../../include/qwen3_prompt.h"
 #include "kernels.h"
+#include "prefix.h"
 #include "probe.h"
 
 namespace {
@@ -305,6 +306,8 @@ struct qwen3_model {
   // positions of the next forward, and of the last one (positions null: the
   // default tables)
   RotaryArgs rotary{}, rotary_used{};
+  // likewise the layout (null: B sequences of T tokens)
+  std::shared_ptr<qwen3_prefix> layout, layout_used;
   std::string err;
   ProbeSet<QWEN3_K_COUNT> probes;
 
@@ -529,9 +532,28 @@ AttnArgs attn_args(qwen3_model* m, int l) {
   return a;
 }
 
-double attn_fwd_flops(const Dims& d) {
+PrefixArgs prefix_args(qwen3_model* m, const AttnArgs& aa) {
+  PrefixArgs a = m->layout_used->args;
+  a.qkv = aa.qkv;
+  a.out = aa.out;
+  a.lse = aa.lse;
+  a.dout = aa.dout;
+  a.dsum = aa.dsum;
+  a.dqkv = aa.dqkv;
+  return a;
+}
+
+double attn_fwd_flops(const qwen3_model* m) {
+  const Dims& d = m->d;
+  if (m->layout_used) return 4.0 * d.H * d.hd * m->layout_used->pairs;
   // causal: q.k and p.v over the key positions j <= i only
   return 4.0 * d.B * d.H * d.hd * ((double)d.T * (d.T + 1) / 2.0);
+}
+
+gpt2_status fail(qwen3_model* m, gpt2_status st, const std::string& why) {
+  if (m) m->err = why;
+  g_err = why;
+  return st;
 }
 
 // Norm of the adapter gradients and the clip coefficient, into normcoef; the
@@ -636,6 +658,20 @@ const char* rotary_args(const qwen3_rotary* r, const void* in, const void* raw, 
   return nullptr;
 }
 
+// the step's tokens at the given positions
+gpt2_status positions_of(qwen3_model* m, const int32_t* d_positions, int n_axes, const int32_t* sections,
+                         int interleaved, RotaryArgs* a) {
+  if (const char* why = rotary_axes(a, m->d.hd, n_axes, sections, interleaved, m->cfg.rope_theta))
+    return fail(m, GPT2_ERR_INVALID_ARG, why);
+  if (reinterpret_cast<uintptr_t>(d_positions) % 4) return fail(m, GPT2_ERR_INVALID_ARG, "positions are not aligned");
+  a->tokens = (int)m->d.BT;
+  a->H = m->d.H;
+  a->Hkv = m->d.Hkv;
+  a->eps = m->cfg.rms_eps;
+  a->positions = d_positions;
+  return GPT2_OK;
+}
+
 // layer l's gains
 RotaryArgs layer_rotary(qwen3_model* m, int l) {
   RotaryArgs a = m->rotary_used;
@@ -644,13 +680,10 @@ RotaryArgs layer_rotary(qwen3_model* m, int l) {
   return a;
 }
 
-gpt2_status fail(qwen3_model* m, gpt2_status st, const std::string& why) {
-  if (m) m->err = why;
-  g_err = why;
-  return st;
-}
 
 }  // namespace
+
+void set_qwen3_error(const char* why) { g_err = why; }
 
 extern "C" {
 
@@ -761,7 +794,12 @@ gpt2_status qwen3_forward(qwen3_model* m, const int32_t* d_inputs, const int32_t
   const int BT = (int)d.BT, BTL = (int)d.BTL;
   const int FWD = QWEN3_K_GEMM_FWD, NORM = QWEN3_K_NORM, OTHER = QWEN3_K_OTHER;
   const double rowb = 2.0 * d.BT * d.C;   // bytes of one bf16 [BT, C] activation
+  m->layout_used = m->layout;
   m->rotary_used = m->rotary;
+  if (m->layout && !m->rotary.positions) {
+    const int32_t sections[] = {d.hd / 2};
+    if (gpt2_status st = positions_of(m, m->layout->positions, 1, sections, 0, &m->rotary_used)) return st;
+  }
   TRY(m->run(OTHER, 0.0, 2.0 * rowb + 4.0 * d.BT,
              [&] { return launch_embed_gather(d_inputs, m->base(B_EMBED), m->res(0), d.BT, d.C, m->stream); }));
   bool in_norm_done = false;   // formed with the previous layer's output
@@ -790,7 +828,9 @@ gpt2_status qwen3_forward(qwen3_model* m, const int32_t* d_inputs, const int32_t
                                     m->af(m->act.rq + l * m->act.s_rq), m->af(m->act.rk + l * m->act.s_rk), BT, d.T,
                                     d.H, d.Hkv, d.hd, m->cfg.rms_eps, m->stream);
     }));
-    TRY(m->run(QWEN3_K_ATTN_FWD, attn_fwd_flops(d), 0.0, [&] { return launch_attention_fwd(aa, m->stream); }));
+    TRY(m->run(QWEN3_K_ATTN_FWD, attn_fwd_flops(m), 0.0, [&] {
+      return m->layout_used ? launch_prefix_fwd(prefix_args(m, aa), m->stream) : launch_attention_fwd(aa, m->stream);
+    }));
     Slices sl;
     TRY(proj_fwd(m, G_O, l, aa.out, m->base(B_O) + (size_t)l * d.C * d.QD, xmid, d.C, m->res(l), &sl));
     // MLP sub-layer
@@ -910,7 +950,9 @@ gpt2_status qwen3_backward(qwen3_model* m) {
     AttnArgs aa = attn_args(m, l);
     bf16_t* datt = m->wb(m->ws.datt);
     TRY(proj_bwd(m, G_O, l, res_mid, d.C, m->base(B_O) + (size_t)l * d.C * d.QD, datt));
-    TRY(m->run(QWEN3_K_ATTN_BWD, 2.0 * attn_fwd_flops(d), 0.0, [&] { return launch_attention_bwd(aa, m->stream); }));
+    TRY(m->run(QWEN3_K_ATTN_BWD, 2.0 * attn_fwd_flops(m), 0.0, [&] {
+      return m->layout_used ? launch_prefix_bwd(prefix_args(m, aa), m->stream) : launch_attention_bwd(aa, m->stream);
+    }));
     bf16_t* draw = m->wb(m->ws.draw + l * m->ws.s_draw);
     TRY(m->run(NORM, 0.0, 6.0 * d.BT * d.QKVD + 4.0 * d.BT * (d.H + d.Hkv), [&] {
       if (m->rotary_used.positions)
@@ -991,17 +1033,38 @@ gpt2_status qwen3_set_positions(qwen3_model* m, const int32_t* d_positions, int3
                                 int32_t interleaved) {
   if (!m) return fail(nullptr, GPT2_ERR_INVALID_ARG, "null model");
   RotaryArgs a{};
-  if (d_positions) {
-    if (const char* why = rotary_axes(&a, m->d.hd, n_axes, sections, interleaved, m->cfg.rope_theta))
-      return fail(m, GPT2_ERR_INVALID_ARG, why);
-    if (reinterpret_cast<uintptr_t>(d_positions) % 4) return fail(m, GPT2_ERR_INVALID_ARG, "positions are not aligned");
-    a.tokens = (int)m->d.BT;
-    a.H = m->d.H;
-    a.Hkv = m->d.Hkv;
-    a.eps = m->cfg.rms_eps;
-    a.positions = d_positions;
-  }
+  if (d_positions)
+    if (gpt2_status st = positions_of(m, d_positions, n_axes, sections, interleaved, &a)) return st;
   m->rotary = a;
+  return GPT2_OK;
+}
+
+gpt2_status qwen3_layout_size(const qwen3_model* m, int32_t prefix_len, int32_t n_seq, const int32_t* seq_lens,
+                              size_t* bytes_out) {
+  if (!m) return fail(nullptr, GPT2_ERR_INVALID_ARG, "null model");
+  const qwen3_prefix_config c{m->d.H, m->d.Hkv, m->d.hd, prefix_len, n_seq, 1};
+  const gpt2_status st = qwen3_prefix_size(&c, seq_lens, bytes_out);
+  return st == GPT2_OK ? st : fail(const_cast<qwen3_model*>(m), st, std::string(g_err));
+}
+
+gpt2_status qwen3_set_layout(qwen3_model* m, int32_t prefix_len, int32_t n_seq, const int32_t* seq_lens, void* d_plan,
+                             size_t plan_bytes) {
+  if (!m) return fail(nullptr, GPT2_ERR_INVALID_ARG, "null model");
+  if (!d_plan) {
+    m->layout.reset();
+    return GPT2_OK;
+  }
+  if (m->d.B != 1) return fail(m, GPT2_ERR_INVALID_ARG, "a layout takes a model of one row of tokens, B = 1");
+  const qwen3_prefix_config c{m->d.H, m->d.Hkv, m->d.hd, prefix_len, n_seq, 1};
+  const std::string why = prefix_check(&c, seq_lens);
+  if (!why.empty()) return fail(m, GPT2_ERR_INVALID_ARG, why);
+  long n = prefix_len;
+  for (int i = 0; i < n_seq; ++i) n += seq_lens[i];
+  if (n != m->d.T) return fail(m, GPT2_ERR_INVALID_ARG, "the prefix and the sequences must make up the T tokens");
+  qwen3_prefix* p = nullptr;
+  if (gpt2_status st = qwen3_prefix_create(&c, seq_lens, d_plan, plan_bytes, m->stream, &p))
+    return fail(m, st, std::string(g_err));
+  m->layout.reset(p);
   return GPT2_OK;
 }
 

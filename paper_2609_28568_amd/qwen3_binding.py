@@ -49,6 +49,11 @@ class Rotary(ctypes.Structure):
         ("rms_eps", ctypes.c_float)]
 
 
+class PrefixConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_head", "n_kv_head", "head_dim", "prefix_len", "n_seq",
+                                              "prefix_queries")]
+
+
 _lib = None
 
 
@@ -71,6 +76,15 @@ def lib():
         "qwen3_rotary_forward": (I32, [ctypes.POINTER(Rotary), P, P, P, P, P, P]),
         "qwen3_rotary_backward": (I32, [ctypes.POINTER(Rotary), P, P, P, P, P, P, P]),
         "qwen3_set_positions": (I32, [P, P, I32, ctypes.POINTER(I32), I32]),
+        "qwen3_prefix_size": (I32, [ctypes.POINTER(PrefixConfig), ctypes.POINTER(I32),
+                                    ctypes.POINTER(ctypes.c_size_t)]),
+        "qwen3_prefix_create": (I32, [ctypes.POINTER(PrefixConfig), ctypes.POINTER(I32), P, ctypes.c_size_t, P,
+                                      ctypes.POINTER(P)]),
+        "qwen3_prefix_forward": (I32, [P, P, P, P, P]),
+        "qwen3_prefix_backward": (I32, [P, P, P, P, P, P, P]),
+        "qwen3_prefix_destroy": (None, [P]),
+        "qwen3_layout_size": (I32, [P, I32, I32, ctypes.POINTER(I32), ctypes.POINTER(ctypes.c_size_t)]),
+        "qwen3_set_layout": (I32, [P, I32, I32, ctypes.POINTER(I32), P, ctypes.c_size_t]),
         "qwen3_muon_size": (I32, [ctypes.POINTER(Qwen3Config), ctypes.POINTER(ctypes.c_size_t)]),
         "qwen3_muon_step": (I32, [P, ctypes.POINTER(Muon), P, ctypes.c_size_t, P]),
         "qwen3_loss": (I32, [P, ctypes.POINTER(F32), P]),
@@ -248,6 +262,73 @@ def rotary_backward(dout, qkv, positions, *, n_head, n_kv_head, sections, theta=
     return out
 
 
+class SharedPrefix:
+    """Attention over packed sequences that share one prefix
+    (qwen3_prefix_*): tokens of the prefix, then of each sequence. The layout
+    is made once and its calls run one at a time, on the current stream."""
+
+    def __init__(self, n_head, n_kv_head, head_dim, prefix_len, seq_lens, prefix_queries=True, device="cuda"):
+        import torch
+        self.torch = torch
+        self.h = ctypes.c_void_p()
+        lens = [int(n) for n in seq_lens]
+        cfg = PrefixConfig(n_head, n_kv_head, head_dim, prefix_len, len(lens), int(bool(prefix_queries)))
+        c_lens = (ctypes.c_int32 * len(lens))(*lens)
+        n = ctypes.c_size_t()
+        _check(lib().qwen3_prefix_size(ctypes.byref(cfg), c_lens, ctypes.byref(n)))
+        self.tokens = prefix_len + sum(lens)
+        self.rows = self.tokens if prefix_queries else sum(lens)
+        self.n_head, self.width, self.out_width = n_head, (n_head + 2 * n_kv_head) * head_dim, n_head * head_dim
+        self.plan = torch.empty(n.value, dtype=torch.uint8, device=device)
+        with torch.cuda.device(self.plan.device):
+            _check(lib().qwen3_prefix_create(ctypes.byref(cfg), c_lens, self.plan.data_ptr(), n.value,
+                                             torch.cuda.current_stream().cuda_stream, ctypes.byref(self.h)))
+
+    def close(self):
+        if self.h:
+            lib().qwen3_prefix_destroy(self.h)
+            self.h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _rows(self, t, name, shape, dtype=None):
+        return _device_rows(t, name, dtype or self.torch.bfloat16, self.plan, shape)
+
+    def forward(self, qkv, out=None, lse=None):
+        """(out [rows, n_head head_dim] bf16, lse [n_head, rows] fp32) of qkv
+        [tokens, (n_head + 2 n_kv_head) head_dim] bf16; rows: the tokens with
+        queries."""
+        torch = self.torch
+        self._rows(qkv, "q | k | v", (self.tokens, self.width))
+        shapes = (self.rows, self.out_width), (self.n_head, self.rows)
+        out = qkv.new_empty(shapes[0]) if out is None else self._rows(out, "out", shapes[0])
+        lse = (qkv.new_empty(shapes[1], dtype=torch.float32) if lse is None
+               else self._rows(lse, "lse", shapes[1], torch.float32))
+        with torch.cuda.device(qkv.device):
+            _check(lib().qwen3_prefix_forward(self.h, qkv.data_ptr(), out.data_ptr(), lse.data_ptr(),
+                                              torch.cuda.current_stream().cuda_stream))
+        return out, lse
+
+    def backward(self, dout, qkv, out, lse, dqkv=None):
+        """The gradient of qkv from dout, that of out, and the forward's qkv,
+        out and lse."""
+        torch = self.torch
+        self._rows(qkv, "q | k | v", (self.tokens, self.width))
+        self._rows(dout, "dout", (self.rows, self.out_width))
+        self._rows(out, "out", (self.rows, self.out_width))
+        self._rows(lse, "lse", (self.n_head, self.rows), torch.float32)
+        dqkv = torch.empty_like(qkv) if dqkv is None else self._rows(dqkv, "dqkv", (self.tokens, self.width))
+        with torch.cuda.device(qkv.device):
+            _check(lib().qwen3_prefix_backward(self.h, qkv.data_ptr(), out.data_ptr(), lse.data_ptr(),
+                                               dout.data_ptr(), dqkv.data_ptr(),
+                                               torch.cuda.current_stream().cuda_stream))
+        return dqkv
+
+
 class Qwen3:
     """One model instance on a torch-owned set of device buffers."""
 
@@ -262,6 +343,7 @@ class Qwen3:
         self.n_lora = sum(int(np.prod(s)) for _, s in self.lora_table.values())
         self.stream = torch.cuda.current_stream(device)
         b = Qwen3Buffers(**{n: t.data_ptr() for n, t in self.bufs.items()})
+        self._positions = self._plan = self._in_use = None
         self.h = ctypes.c_void_p()
         _check(lib().qwen3_init(ctypes.byref(cfg), ctypes.byref(b), ctypes.c_void_p(self.stream.cuda_stream),
                                 ctypes.byref(self.h)))
@@ -324,6 +406,8 @@ class Qwen3:
 
     def forward(self, ids, targets=None):
         torch = self.torch
+        # a backward takes its forward's positions and layout, whatever is set in between
+        self._in_use = (self._positions, self._plan)
         self._ids = ids.to(torch.int32).cuda().contiguous()
         self._tgt = None if targets is None else targets.to(torch.int32).cuda().contiguous()
         _check(lib().qwen3_forward(self.h, ctypes.c_void_p(self._ids.data_ptr()),
@@ -344,8 +428,22 @@ class Qwen3:
                          (len(sections), self.cfg.B * self.cfg.T))
         sec = (ctypes.c_int32 * len(sections))(*sections)
         _check(lib().qwen3_set_positions(self.h, _ptr(positions), len(sections), sec, int(bool(interleaved))), self.h)
-        # the forward and the backward read them; a backward may still take the ones before
-        self._positions = (positions, getattr(self, "_positions", (None,))[0])
+        self._positions = positions
+
+    def set_layout(self, prefix_len=0, seq_lens=None):
+        """The tokens as a prefix and sequences over it (qwen3_set_layout),
+        from the next forward on; without seq_lens: B sequences of T tokens."""
+        if seq_lens is None:
+            _check(lib().qwen3_set_layout(self.h, 0, 0, None, None, 0), self.h)
+            self._plan = None
+            return
+        lens = [int(n) for n in seq_lens]
+        c_lens = (ctypes.c_int32 * len(lens))(*lens)
+        n = ctypes.c_size_t()
+        _check(lib().qwen3_layout_size(self.h, prefix_len, len(lens), c_lens, ctypes.byref(n)), self.h)
+        plan = self.torch.empty(n.value, dtype=self.torch.uint8, device=self.bufs["workspace"].device)
+        _check(lib().qwen3_set_layout(self.h, prefix_len, len(lens), c_lens, plan.data_ptr(), n.value), self.h)
+        self._plan = plan
 
     def muon_step(self, norm_out=None, momentum=0.95, nesterov=True, iterations=5, scale=0.2):
         """Clip and an orthogonalised update with momentum of every adapter

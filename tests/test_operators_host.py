@@ -123,3 +123,48 @@ def test_rotary_binding_refuses_tensors():
     with pytest.raises(ValueError):
         qb.rotary(x, pos, n_head=4, n_kv_head=2, sections=(64,))   # not on a device
     assert qb.lib().qwen3_set_positions(None, None, 1, None, 0) == INVALID
+
+
+# ---- attention over a shared prefix
+
+def prefix_size(lens, **over):
+    c = dict(n_head=4, n_kv_head=2, head_dim=128, prefix_len=100, n_seq=len(lens), prefix_queries=1)
+    c.update(over)
+    n = ctypes.c_size_t()
+    arr = (ctypes.c_int32 * max(len(lens), 1))(*lens)
+    st = qb.lib().qwen3_prefix_size(ctypes.byref(qb.PrefixConfig(**c)), arr, ctypes.byref(n))
+    return st, n.value
+
+
+@pytest.mark.parametrize("lens,over,why", [
+    ([5], dict(n_head=0), "n_head"), ([5], dict(n_kv_head=3), "n_head"), ([5], dict(n_kv_head=0), "n_head"),
+    ([5], dict(head_dim=96), "head_dim"), ([5], dict(prefix_len=-1), "prefix_len"), ([5], dict(n_seq=-1), "n_seq"),
+    ([5, -1], {}, "negative"), ([0, 0], dict(prefix_queries=0), "query"), ([], dict(prefix_len=0), "query"),
+    ([1 << 30], {}, "32-bit"), ([1 << 30] * 9, {}, "32-bit")])
+def test_prefix_refuses_layouts(lens, over, why):
+    st, _ = prefix_size(lens, **over)
+    assert st == INVALID and why in qb.lib().qwen3_last_error(None).decode()
+
+
+def test_prefix_sizes():
+    st, n = prefix_size([10, 0, 3])
+    assert st == 0 and n >= 113 * 12
+    assert prefix_size([], prefix_len=7)[0] == 0
+    assert prefix_size([1] * 64, prefix_len=8192, prefix_queries=0)[0] == 0
+    assert qb.lib().qwen3_prefix_size(None, None, None) == INVALID
+
+
+def test_prefix_refuses_arguments():
+    L = qb.lib()
+    c = qb.PrefixConfig(4, 2, 128, 100, 1, 1)
+    lens, out = (ctypes.c_int32 * 1)(5), ctypes.c_void_p()
+    for d_plan, nbytes, why in ((0, 1 << 30, "NULL"), (4100, 1 << 30, "aligned"), (4096, 64, "smaller")):
+        assert L.qwen3_prefix_create(ctypes.byref(c), lens, d_plan, nbytes, None, ctypes.byref(out)) == INVALID
+        assert why in L.qwen3_last_error(None).decode() and not out
+    assert L.qwen3_prefix_create(ctypes.byref(c), lens, 4096, 1 << 30, None, None) == INVALID
+    assert L.qwen3_prefix_forward(None, 4096, 4096, 4096, None) == INVALID
+    assert L.qwen3_prefix_backward(None, 4096, 4096, 4096, 4096, 4096, None) == INVALID
+    L.qwen3_prefix_destroy(None)
+    n = ctypes.c_size_t()
+    assert L.qwen3_layout_size(None, 1, 1, lens, ctypes.byref(n)) == INVALID
+    assert L.qwen3_set_layout(None, 1, 1, lens, None, 0) == INVALID
