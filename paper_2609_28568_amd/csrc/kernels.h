@@ -429,7 +429,7 @@ hipError_t launch_rotary(const RotaryArgs& a, const bf16_t* in, const bf16_t* ra
 
 // ---------------------------------------------------------------- orthogonalised updates
 constexpr int ORTHO_GROUPS = 12;   // shapes in one call
-constexpr int ORTHO_PARTS = 32;    // partial sums of squares per matrix
+constexpr int ORTHO_PARTS = 64;    // partial sums of squares per matrix
 
 // `count` matrices of one shape, `stride` elements apart, row stride ld. The
 // second block is filled in by ortho_layout and the launcher.
