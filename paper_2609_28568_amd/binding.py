@@ -171,6 +171,16 @@ def kind_table(cfg: Config):
     return kinds
 
 
+def on_stream(device, fn, *args):
+    """fn(*args, stream) with the device current and its current stream; the
+    status is the caller's to check."""
+    import torch
+    if torch.cuda.current_device() == device.index:
+        return fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    with torch.cuda.device(device):
+        return fn(*args, torch.cuda.current_stream(device).cuda_stream)
+
+
 def orthogonalise(x, iterations=5, out=None, workspace=None):
     """Newton-Schulz orthogonalisation of one fp32 matrix [rows, cols] or a
     batch [count, rows, cols] (gpt2_orthogonalise) on the current stream of
@@ -185,14 +195,12 @@ def orthogonalise(x, iterations=5, out=None, workspace=None):
         raise ValueError("out must be a contiguous tensor of x's shape, type and device")
     rows, cols = x.shape[-2:]
     count = x.shape[0] if x.dim() == 3 else 1
-    with torch.cuda.device(x.device):
-        if workspace is None:
-            workspace = torch.empty(orthogonalise_size(rows, cols, count), dtype=torch.uint8, device=x.device)
-        elif workspace.dtype != torch.uint8 or workspace.device != x.device or not workspace.is_contiguous():
-            raise ValueError("the workspace must be a contiguous uint8 tensor on x's device")
-        _check(lib().gpt2_orthogonalise(x.data_ptr(), out.data_ptr(), rows, cols, count, int(iterations),
-                                        workspace.data_ptr(), workspace.numel(),
-                                        torch.cuda.current_stream().cuda_stream))
+    if workspace is None:
+        workspace = torch.empty(orthogonalise_size(rows, cols, count), dtype=torch.uint8, device=x.device)
+    elif workspace.dtype != torch.uint8 or workspace.device != x.device or not workspace.is_contiguous():
+        raise ValueError("the workspace must be a contiguous uint8 tensor on x's device")
+    _check(on_stream(x.device, lib().gpt2_orthogonalise, x.data_ptr(), out.data_ptr(), rows, cols, count,
+                     int(iterations), workspace.data_ptr(), workspace.numel()))
     return out
 
 

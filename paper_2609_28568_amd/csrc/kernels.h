@@ -406,6 +406,7 @@ struct PrefixArgs {
   const PrefixItem *items, *kitems;
   const PrefixJoin *joins, *kjoins;
   int nitems, njoins, nkitems, nkjoins;
+  int parts;                      // most parts of a join
 };
 // floats of a partial result of one key/value head: forward (0), dQ (1), dK/dV (2)
 size_t prefix_part_floats(int hd, int which);

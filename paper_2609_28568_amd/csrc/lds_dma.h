@@ -47,6 +47,18 @@ DEV void wait_vmcnt() {
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
 }
 
+// Wait until at most min(later, L) tiles of LOADS load instructions each are
+// still in flight (later is uniform across the wave).
+template <int L, int LOADS>
+DEV void wait_tiles(int later) {
+  if constexpr (L <= 0) {
+    wait_vmcnt<0>();
+  } else {
+    if (later >= L) wait_vmcnt<L * LOADS>();
+    else wait_tiles<L - 1, LOADS>(later);
+  }
+}
+
 // workgroup barrier without the memory fence of __syncthreads (which would
 // wait for the prefetches still in flight)
 DEV void block_barrier() { asm volatile("s_barrier" ::: "memory"); }

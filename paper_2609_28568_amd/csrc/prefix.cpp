@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <cstring>
+#include <functional>
 #include <new>
 #include <vector>
 
@@ -24,14 +25,14 @@ struct Tables {
   std::vector<PrefixJoin> joins, kjoins;
 };
 
-// Cut walks of `nt` tiles, longest first in `walks`, into items of about `per`
-// tiles where they are longer than that by half, and put the longest items
-// first, so that no long one starts last.
-void deal(std::vector<PrefixItem>& walks, int per, std::vector<PrefixItem>& items, std::vector<PrefixJoin>& joins,
-          int& slots) {
+int parts_of(int nt, int per) { return 2l * nt > 3l * per ? (nt + per - 1) / per : 1; }
+
+// Cut walks into items of about `per` tiles where they are longer than that by
+// half, and put the longest items first, so that no long one starts last.
+void deal(const std::vector<PrefixItem>& walks, int per, std::vector<PrefixItem>& items,
+          std::vector<PrefixJoin>& joins, int& slots) {
   for (const PrefixItem& w : walks) {
-    const int nt = w.f1;
-    const int parts = 2 * (long)nt > 3 * (long)per ? (nt + per - 1) / per : 1;
+    const int nt = w.f1, parts = parts_of(nt, per);
     if (parts > 1) joins.push_back({w.row, slots, parts, 0});
     for (int i = 0; i < parts; ++i) {
       PrefixItem it = w;
@@ -45,13 +46,59 @@ void deal(std::vector<PrefixItem>& walks, int per, std::vector<PrefixItem>& item
                    [](const PrefixItem& a, const PrefixItem& b) { return a.f1 - a.f0 > b.f1 - b.f0; });
 }
 
-// The length of items that fills the chip `rounds` times over with `walks` of
-// every key/value head, `wgs` workgroups at a time, and is worth an item's
-// start, its partial result and their joining.
-int item_tiles(const std::vector<PrefixItem>& walks, int Hkv, int wgs, int least) {
+// Microseconds that items of about `per` tiles take: each workgroup slot takes
+// the next longest item when it is free, an item costs its start and end and
+// its tiles, one that shares its walk also its partial result, and those are
+// joined by a launch that reads them all. Measured (forward, head size 128, one
+// walk of 129 tiles for each of 8 heads, per 5, 6, 8, 12, 16, 24, 40, 129: 21.9,
+// 21.3, 21.6, 23.3, 25.7, 30.9, 38.8, 117; this gives 21.3, 21.1, 21.5, 23.4,
+// 25.4, 30.7, 39.8, 118).
+constexpr int CUS = 256;
+struct Costs {
+  int slots;            // workgroups that run at a time
+  double tile;          // a tile of a workgroup with a CU to itself
+  double shared;        // ... with all slots taken, where those are two a CU
+  double part_bytes;    // of a partial result
+};
+double estimate(const std::vector<PrefixItem>& walks, int per, int Hkv, const Costs& c) {
+  std::vector<int> n;
+  long parts = 0;
+  for (const PrefixItem& w : walks) {
+    const int k = parts_of(w.f1, per);
+    if (k > 1) parts += k;
+    for (int i = 0; i < k; ++i) n.push_back((int)((long)w.f1 * (i + 1) / k - (long)w.f1 * i / k));
+  }
+  std::sort(n.rbegin(), n.rend());
+  const double wgs = (double)n.size() * Hkv;
+  const double tile = wgs <= CUS || c.slots == CUS ? c.tile : std::min(1.0, wgs / c.slots) * c.shared;
+  std::vector<double> heap(std::max(1, c.slots / Hkv), 0.0);   // when each of one head's slots is free
+  for (int t : n) {
+    std::pop_heap(heap.begin(), heap.end(), std::greater<double>());
+    heap.back() += 6.0 + t * tile;
+    std::push_heap(heap.begin(), heap.end(), std::greater<double>());
+  }
+  const double traffic = 2.0 * parts * Hkv * c.part_bytes / 4e6;   // written and read, at 4 TB/s
+  return *std::max_element(heap.begin(), heap.end()) + (parts ? 4.0 + traffic : 0.0);
+}
+
+// The length of items with the least estimate: whole walks, or what shares the
+// tiles out over a third of the slots to four times as many.
+int item_tiles(const std::vector<PrefixItem>& walks, int Hkv, const Costs& c) {
   long total = 0;
   for (const PrefixItem& w : walks) total += w.f1;
-  return (int)std::max((long)least, (total * Hkv + wgs - 1) / wgs);
+  int best = 1 << 30;
+  if (walks.size() > 16384) return best;   // plenty of items, and none much longer than the others
+  double least = estimate(walks, best, Hkv, c);
+  for (int r = 1; r <= 12; ++r) {
+    const long wgs = (long)c.slots * r / 3;
+    const int per = (int)std::max(2l, (total * Hkv + wgs - 1) / wgs);
+    const double t = estimate(walks, per, Hkv, c);
+    if (t < 0.97 * least) {
+      least = t;
+      best = per;
+    }
+  }
+  return best;
 }
 
 Tables lay_out(const qwen3_prefix_config& c, const int32_t* lens) {
@@ -85,7 +132,10 @@ Tables lay_out(const qwen3_prefix_config& c, const int32_t* lens) {
     w.f1 = w.npre + (tb >= t.P ? (tb + 1 - w.own + TILE - 1) / TILE : 0);
     walks.push_back(w);
   }
-  deal(walks, item_tiles(walks, c.n_kv_head, 512, 4), t.items, t.joins, t.fslots);
+  const bool narrow = c.head_dim == 64;
+  const double bytes[] = {4.0 * prefix_part_floats(c.head_dim, 0), 4.0 * prefix_part_floats(c.head_dim, 2)};
+  deal(walks, item_tiles(walks, c.n_kv_head, {2 * CUS, narrow ? 0.5 : 0.87, narrow ? 1.4 : 2.8, bytes[0]}), t.items,
+       t.joins, t.fslots);
 
   walks.clear();
   auto keys = [&](int from, int to) {
@@ -100,7 +150,7 @@ Tables lay_out(const qwen3_prefix_config& c, const int32_t* lens) {
   };
   keys(0, t.P);
   keys(t.P, t.N);
-  deal(walks, item_tiles(walks, c.n_kv_head, 512, 8), t.kitems, t.kjoins, t.kslots);
+  deal(walks, item_tiles(walks, c.n_kv_head, {CUS, narrow ? 1.2 : 1.85, 0.0, bytes[1]}), t.kitems, t.kjoins, t.kslots);
   return t;
 }
 
@@ -193,6 +243,7 @@ hipError_t prefix_make(const qwen3_prefix_config& c, const int32_t* lens, void* 
   a.part = static_cast<float*>(at(p.part));
   a.nitems = (int)t.items.size();
   a.njoins = (int)t.joins.size();
+  for (const PrefixJoin& j : t.joins) a.parts = std::max(a.parts, (int)j.parts);
   a.nkitems = (int)t.kitems.size();
   a.nkjoins = (int)t.kjoins.size();
   out->positions = static_cast<int32_t*>(at(p.pos));

@@ -29,6 +29,8 @@
 
 namespace {
 
+typedef float float2_t __attribute__((ext_vector_type(2)));
+
 // Item decoding: blocks run through the key/value heads of an item, then the
 // next item, so that with 8 of them each keeps to one XCD's L2.
 struct Where {
@@ -121,17 +123,27 @@ constexpr size_t fwd_part(int hd) { return (size_t)BQ * (hd + 2); }    // O [128
 constexpr size_t dq_part(int hd) { return (size_t)BQ * hd; }
 constexpr size_t dkdv_part(int hd) { return (size_t)2 * BQ * hd; }     // dK, dV [128][hd]
 
-template <int HD>
-__global__ __launch_bounds__(256, 2) void prefix_fwd_kernel(PrefixArgs a) {
+// Where items are too few for two workgroups a CU, GR groups of four waves walk
+// the item's tiles in turn and merge what they have at the end: a walk's time is
+// one wave's chain of products and exponentials, tile after tile.
+template <int HD, int GR>
+__global__ __launch_bounds__(256 * GR, GR == 1 ? 2 : 1) void prefix_fwd_kernel(PrefixArgs a) {
   using S = Shape<HD>;
-  __shared__ __attribute__((aligned(1024))) char smem_raw[2 * 2 * S::TBA];   // 2 stages x (K, V)
-  lds_char_t* smem = (lds_char_t*)smem_raw;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  constexpr int GROUP = 2 * 2 * S::TBA;   // 2 stages x (K, V)
+  constexpr int KEEP = S::DT * 4096 + 512;   // a wave's O, maxima and sums
+  static_assert(4 * (GR - 1) * KEEP <= GR * GROUP, "the groups' results fit their tiles' space");
+  __shared__ __attribute__((aligned(1024))) char smem_raw[GR * GROUP];
+  const int tid = threadIdx.x, lane = tid & 63, all = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = all & 3, group = all >> 2;
+  lds_char_t* smem = (lds_char_t*)smem_raw + group * GROUP;
   const int lq = lane & 31, g = lane >> 5;
   const Where w = where(a, a.items);
-  const Row r = row_of(a, w.it.row + 32 * wave, w.j, lane);
   KeyWalk<HD> keys;
   keys.init(a, w);
+  auto stage = [&](int f) { return smem + (f - w.it.f0) / GR % 2 * 2 * S::TBA; };
+  // under way while the rows are read
+  if (w.it.f0 + group < w.it.f1) keys.issue(w.it.f0 + group, stage(w.it.f0 + group), wave, lane);
+  const Row r = row_of(a, w.it.row + 32 * wave, w.j, lane);
 
   bf16x8 qf[S::KS];
   const bf16_t* q = a.qkv + (size_t)r.t * keys.ld + r.h * HD;
@@ -143,13 +155,13 @@ __global__ __launch_bounds__(256, 2) void prefix_fwd_kernel(PrefixArgs a) {
   float m_run = -INFINITY, l_run = 0.0f;
   const float sc = LOG2E / sqrtf((float)HD);
 
-  auto stage = [&](int f) { return smem + ((f - w.it.f0) & 1) * 2 * S::TBA; };
-  keys.issue(w.it.f0, stage(w.it.f0), wave, lane);
-  for (int f = w.it.f0; f < w.it.f1; ++f) {
+  for (int f0 = w.it.f0; f0 < w.it.f1; f0 += GR) {
+    const int f = f0 + group;
     wait_vmcnt<0>();
     __builtin_amdgcn_s_waitcnt(0xC07F);   // this wave's reads of the stage that the next loads overwrite are done
     block_barrier();
-    if (f + 1 < w.it.f1) keys.issue(f + 1, stage(f + 1), wave, lane);
+    if (f + GR < w.it.f1) keys.issue(f + GR, stage(f + GR), wave, lane);
+    if (f >= w.it.f1) continue;
     const int kv0 = keys.key0(f);
     const bool own = keys.is_own(f);
     const Sight see = sight(a, r, kv0, own);
@@ -216,6 +228,39 @@ __global__ __launch_bounds__(256, 2) void prefix_fwd_kernel(PrefixArgs a) {
       }
   }
 
+  if constexpr (GR > 1) {
+    // the other groups' results through LDS, joined in order
+    __syncthreads();
+    lds_char_t* keep = (lds_char_t*)smem_raw + ((group - 1) * 4 + wave) * KEEP + lane * 16;
+    if (group > 0) {
+#pragma unroll
+      for (int d = 0; d < S::DT; ++d)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          *reinterpret_cast<lds_v4f32_t*>(keep + (d * 4 + c) * 1024) =
+              v4f32{o[d][4 * c], o[d][4 * c + 1], o[d][4 * c + 2], o[d][4 * c + 3]};
+      *reinterpret_cast<LDS_AS float2_t*>(keep + S::DT * 4096 - lane * 8) = float2_t{m_run, l_run};
+    }
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int k = 0; k < GR - 1; ++k) {
+      const lds_char_t* from = keep + (k + 1) * 4 * KEEP;
+      const float2_t ml = *reinterpret_cast<const LDS_AS float2_t*>(from + S::DT * 4096 - lane * 8);
+      const float m = fmaxf(m_run, ml.x);
+      const float f0 = m_run == -INFINITY ? 0.0f : fast_exp2(m_run - m), f1 = ml.x == -INFINITY ? 0.0f : fast_exp2(ml.x - m);
+      m_run = m;
+      l_run = l_run * f0 + ml.y * f1;
+#pragma unroll
+      for (int d = 0; d < S::DT; ++d)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const v4f32 x = *reinterpret_cast<const lds_v4f32_t*>(from + (d * 4 + c) * 1024);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[d][4 * c + e] = o[d][4 * c + e] * f0 + x[e] * f1;
+        }
+    }
+  }
   if (!r.on) return;
   if (w.it.slot >= 0) {
     float* part = a.part + part_at(a, w.it.slot, w.j, fwd_part(HD));
@@ -244,26 +289,82 @@ __global__ __launch_bounds__(256, 2) void prefix_fwd_kernel(PrefixArgs a) {
   if (g == 0) a.lse[(size_t)r.h * a.nq + r.rq] = (m_run + log2f(l_run)) * LN2;
 }
 
-// The parts of a row merged: HD/8 lanes a row, 8 elements each.
+// The parts of a row merged, a wave a row: lane k first holds part k's maximum
+// and sum (the maximum's weight afterwards), then HD/8 lanes take the row's
+// elements, 8 each, and the groups of them the parts in turn.
 template <int HD>
 __global__ __launch_bounds__(256) void prefix_fwd_join_kernel(PrefixArgs a) {
+  constexpr int LANES = HD / 8, GROUPS = 64 / LANES;
+  const int lane = threadIdx.x & 63;
+  const int b = blockIdx.x, j = b % a.Hkv;
+  const PrefixJoin jn = a.joins[b / a.Hkv];
+  const int G = a.H / a.Hkv, row = blockIdx.y * 4 + (threadIdx.x >> 6), c = lane % LANES * 8;
+  const int rr = jn.row + row;
+  if (rr >= a.nq * G) return;
+  const float* part0 = a.part + part_at(a, jn.slot, j, fwd_part(HD));
+  const size_t step = (size_t)a.Hkv * fwd_part(HD);
+  float m = -INFINITY;
+  for (int k = lane; k < jn.parts; k += 64) m = fmaxf(m, part0[k * step + (size_t)BQ * HD + row]);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  float l = 0.0f, o[8] = {};
+  for (int k0 = 0; k0 < jn.parts; k0 += 64) {
+    float wgt = 0.0f;
+    if (k0 + lane < jn.parts) {
+      const float* p = part0 + (k0 + lane) * step + (size_t)BQ * HD;
+      wgt = fast_exp2(p[row] - m);
+      l += wgt * p[BQ + row];
+    }
+    const int n = min(64, jn.parts - k0);
+#pragma unroll 4
+    for (int k = 0; k < n; k += GROUPS) {
+      const int q = k + lane / LANES;
+      const float f = __shfl(wgt, min(q, 63));
+      if (q < n) {
+        const float* p = part0 + (k0 + q) * step + (size_t)row * HD + c;
+        const float4 x = *reinterpret_cast<const float4*>(p), y = *reinterpret_cast<const float4*>(p + 4);
+        o[0] += f * x.x; o[1] += f * x.y; o[2] += f * x.z; o[3] += f * x.w;
+        o[4] += f * y.x; o[5] += f * y.y; o[6] += f * y.z; o[7] += f * y.w;
+      }
+    }
+  }
+  l = wave_sum(l);
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+#pragma unroll
+    for (int s = LANES; s < 64; s <<= 1) o[e] += __shfl_xor(o[e], s);
+  if (lane >= LANES) return;
+  const float inv = 1.0f / l;
+  const int rq = rr / G, h = j * G + rr - rq * G;
+  *reinterpret_cast<uint4*>(a.out + ((size_t)rq * a.H + h) * HD + c) =
+      make_uint4(pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv), pack2(o[4] * inv, o[5] * inv),
+                 pack2(o[6] * inv, o[7] * inv));
+  if (c == 0) a.lse[(size_t)h * a.nq + rq] = (m + log2f(l)) * LN2;
+}
+
+// ... a row's HD/8 lanes taking its parts one after another, where rows are
+// many and parts few.
+template <int HD>
+__global__ __launch_bounds__(256) void prefix_fwd_join_few_kernel(PrefixArgs a) {
   constexpr int LANES = HD / 8, ROWS = 256 / LANES;
   const int b = blockIdx.x, j = b % a.Hkv;
   const PrefixJoin jn = a.joins[b / a.Hkv];
   const int G = a.H / a.Hkv, row = blockIdx.y * ROWS + threadIdx.x / LANES, c = threadIdx.x % LANES * 8;
   const int rr = jn.row + row;
   if (rr >= a.nq * G) return;
+  const float* part0 = a.part + part_at(a, jn.slot, j, fwd_part(HD));
+  const size_t step = (size_t)a.Hkv * fwd_part(HD);
   float m = -INFINITY;
-  for (int k = 0; k < jn.parts; ++k)
-    m = fmaxf(m, a.part[part_at(a, jn.slot + k, j, fwd_part(HD)) + (size_t)BQ * HD + row]);
+#pragma unroll 4
+  for (int k = 0; k < jn.parts; ++k) m = fmaxf(m, part0[k * step + (size_t)BQ * HD + row]);
   float l = 0.0f, o[8] = {};
 #pragma unroll 4
   for (int k = 0; k < jn.parts; ++k) {
-    const float* part = a.part + part_at(a, jn.slot + k, j, fwd_part(HD));
-    const float f = fast_exp2(part[(size_t)BQ * HD + row] - m);
-    const float4 x = *reinterpret_cast<const float4*>(part + (size_t)row * HD + c);
-    const float4 y = *reinterpret_cast<const float4*>(part + (size_t)row * HD + c + 4);
-    l += f * part[(size_t)BQ * HD + BQ + row];
+    const float* p = part0 + k * step;
+    const float f = fast_exp2(p[(size_t)BQ * HD + row] - m);
+    const float4 x = *reinterpret_cast<const float4*>(p + (size_t)row * HD + c);
+    const float4 y = *reinterpret_cast<const float4*>(p + (size_t)row * HD + c + 4);
+    l += f * p[(size_t)BQ * HD + BQ + row];
     o[0] += f * x.x; o[1] += f * x.y; o[2] += f * x.z; o[3] += f * x.w;
     o[4] += f * y.x; o[5] += f * y.y; o[6] += f * y.z; o[7] += f * y.w;
   }
@@ -298,17 +399,23 @@ __global__ __launch_bounds__(256) void prefix_dsum_kernel(PrefixArgs a) {
 }
 
 // dQ of 128 rows, walking the forward's tiles: dS = P (dO V^T - D), dQ = dS K.
-template <int HD>
-__global__ __launch_bounds__(256, 2) void prefix_dq_kernel(PrefixArgs a) {
+template <int HD, int GR>
+__global__ __launch_bounds__(256 * GR, GR == 1 ? 2 : 1) void prefix_dq_kernel(PrefixArgs a) {
   using S = Shape<HD>;
-  __shared__ __attribute__((aligned(1024))) char smem_raw[2 * 2 * S::TBA];   // 2 stages x (K, V)
-  lds_char_t* smem = (lds_char_t*)smem_raw;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  constexpr int GROUP = 2 * 2 * S::TBA, KEEP = S::DT * 4096;   // as the forward's
+  static_assert(4 * (GR - 1) * KEEP <= GR * GROUP, "the groups' results fit their tiles' space");
+  __shared__ __attribute__((aligned(1024))) char smem_raw[GR * GROUP];
+  const int tid = threadIdx.x, lane = tid & 63, all = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = all & 3, group = all >> 2;
+  lds_char_t* smem = (lds_char_t*)smem_raw + group * GROUP;
   const int lq = lane & 31, g = lane >> 5;
   const Where w = where(a, a.items);
-  const Row r = row_of(a, w.it.row + 32 * wave, w.j, lane);
   KeyWalk<HD> keys;
   keys.init(a, w);
+  auto stage = [&](int f) { return smem + (f - w.it.f0) / GR % 2 * 2 * S::TBA; };
+  // under way while the rows are read
+  if (w.it.f0 + group < w.it.f1) keys.issue(w.it.f0 + group, stage(w.it.f0 + group), wave, lane);
+  const Row r = row_of(a, w.it.row + 32 * wave, w.j, lane);
 
   bf16x8 qf[S::KS], df[S::KS];
   const bf16_t* q = a.qkv + (size_t)r.t * keys.ld + r.h * HD;
@@ -325,13 +432,13 @@ __global__ __launch_bounds__(256, 2) void prefix_dq_kernel(PrefixArgs a) {
   const float scale = 1.0f / sqrtf((float)HD);
   const float sc = scale * LOG2E;
 
-  auto stage = [&](int f) { return smem + ((f - w.it.f0) & 1) * 2 * S::TBA; };
-  keys.issue(w.it.f0, stage(w.it.f0), wave, lane);
-  for (int f = w.it.f0; f < w.it.f1; ++f) {
+  for (int f0 = w.it.f0; f0 < w.it.f1; f0 += GR) {
+    const int f = f0 + group;
     wait_vmcnt<0>();
     __builtin_amdgcn_s_waitcnt(0xC07F);   // this wave's reads of the stage that the next loads overwrite are done
     block_barrier();
-    if (f + 1 < w.it.f1) keys.issue(f + 1, stage(f + 1), wave, lane);
+    if (f + GR < w.it.f1) keys.issue(f + GR, stage(f + GR), wave, lane);
+    if (f >= w.it.f1) continue;
     const int kv0 = keys.key0(f);
     const bool own = keys.is_own(f);
     const Sight see = sight(a, r, kv0, own);
@@ -374,6 +481,30 @@ __global__ __launch_bounds__(256, 2) void prefix_dq_kernel(PrefixArgs a) {
       }
   }
 
+  if constexpr (GR > 1) {
+    __syncthreads();
+    lds_char_t* keep = (lds_char_t*)smem_raw + ((group - 1) * 4 + wave) * KEEP + lane * 16;
+    if (group > 0) {
+#pragma unroll
+      for (int d = 0; d < S::DT; ++d)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          *reinterpret_cast<lds_v4f32_t*>(keep + (d * 4 + c) * 1024) =
+              v4f32{dq[d][4 * c], dq[d][4 * c + 1], dq[d][4 * c + 2], dq[d][4 * c + 3]};
+    }
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int k = 1; k < GR; ++k)
+#pragma unroll
+      for (int d = 0; d < S::DT; ++d)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const v4f32 x = *reinterpret_cast<const lds_v4f32_t*>(keep + k * 4 * KEEP + (d * 4 + c) * 1024);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) dq[d][4 * c + e] += x[e];
+        }
+  }
   if (!r.on) return;
   if (w.it.slot >= 0) {
     float* part = a.part + part_at(a, w.it.slot, w.j, dq_part(HD)) + (size_t)(32 * wave + lq) * HD;
@@ -582,9 +713,14 @@ __global__ __launch_bounds__(512, 1) void prefix_dkdv_kernel(PrefixArgs a) {
 
 template <int HD>
 hipError_t fwd_t(const PrefixArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL(prefix_fwd_kernel<HD>, dim3(a.nitems * a.Hkv), dim3(256), 0, s, a);
-  if (a.njoins)
-    hipLaunchKernelGGL(prefix_fwd_join_kernel<HD>, dim3(a.njoins * a.Hkv, BQ * HD / 2048), dim3(256), 0, s, a);
+  const unsigned wgs = a.nitems * a.Hkv;
+  constexpr int GR = HD == 64 ? 4 : 2;   // as many as the registers allow
+  if (wgs <= 256) hipLaunchKernelGGL((prefix_fwd_kernel<HD, GR>), dim3(wgs), dim3(256 * GR), 0, s, a);
+  else hipLaunchKernelGGL((prefix_fwd_kernel<HD, 1>), dim3(wgs), dim3(256), 0, s, a);
+  if (!a.njoins) return hipGetLastError();
+  const unsigned joins = a.njoins * a.Hkv;
+  if (a.parts > 8) hipLaunchKernelGGL(prefix_fwd_join_kernel<HD>, dim3(joins, BQ / 4), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(prefix_fwd_join_few_kernel<HD>, dim3(joins, BQ * HD / 2048), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -592,7 +728,9 @@ template <int HD>
 hipError_t bwd_t(const PrefixArgs& a, hipStream_t s) {
   const long lanes = (long)a.N * a.H * (HD / 8);
   hipLaunchKernelGGL(prefix_dsum_kernel<HD>, dim3((unsigned)((lanes + 255) / 256)), dim3(256), 0, s, a);
-  hipLaunchKernelGGL(prefix_dq_kernel<HD>, dim3(a.nitems * a.Hkv), dim3(256), 0, s, a);
+  const unsigned wgs = a.nitems * a.Hkv;
+  if (wgs <= 256) hipLaunchKernelGGL((prefix_dq_kernel<HD, 2>), dim3(wgs), dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((prefix_dq_kernel<HD, 1>), dim3(wgs), dim3(256), 0, s, a);
   if (a.njoins)
     hipLaunchKernelGGL((prefix_sum_join_kernel<HD, false>), dim3(a.njoins * a.Hkv, BQ * HD / 2048), dim3(256), 0, s, a);
   hipLaunchKernelGGL(prefix_dkdv_kernel<HD>, dim3(a.nkitems * a.Hkv), dim3(512), 0, s, a);

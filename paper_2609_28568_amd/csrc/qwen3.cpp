@@ -620,7 +620,11 @@ const char* rotary_axes(RotaryArgs* a, int hd, int n_axes, const int32_t* sectio
   }
   if (sum != half) return "the sections must sum to head_dim / 2";
   a->hd = hd;
-  for (int i = 0, k = 0, left = sections[0]; i < half; ++i) {
+  // turns per unit of position, one step of the geometric series after another
+  // in 64 bits of significand (64 pow() took 3 us of a call)
+  const long double ratio = std::pow((long double)theta, -2.0L / hd);
+  long double f = 1.0L / (2.0L * 3.14159265358979323846264L);
+  for (int i = 0, k = 0, left = sections[0]; i < half; ++i, f *= ratio) {
     if (interleaved) {
       k = i % n_axes;
       if (i / n_axes >= sections[k]) k = 0;
@@ -629,7 +633,7 @@ const char* rotary_axes(RotaryArgs* a, int hd, int n_axes, const int32_t* sectio
       --left;
     }
     a->axis[i] = (uint8_t)k;
-    a->freq[i] = std::pow(theta, -2.0 * i / hd) / (2.0 * 3.14159265358979323846);
+    a->freq[i] = (double)f;
   }
   return nullptr;
 }

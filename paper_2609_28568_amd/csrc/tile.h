@@ -83,16 +83,4 @@ DEV bf16x8 read_frag(const lds_char_t* stage, int row_base, int s, int lane) {
   }
 }
 
-// Wait until at most min(later, L) tiles of LOADS load instructions each are
-// still in flight (later is uniform across the wave).
-template <int L, int LOADS>
-DEV void wait_tiles(int later) {
-  if constexpr (L <= 0) {
-    wait_vmcnt<0>();
-  } else {
-    if (later >= L) wait_vmcnt<L * LOADS>();
-    else wait_tiles<L - 1, LOADS>(later);
-  }
-}
-
 }  // namespace

@@ -9,10 +9,11 @@ layouts (q|k|v and gate|up stacked, adapter ranks zero-padded) and back.
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import numpy as np
 
-from .binding import LibError, Muon, lib as _lib_gpt2
+from .binding import LibError, Muon, lib as _lib_gpt2, on_stream
 
 RP = 64   # padded adapter rank of the library
 # kernel classes of the timing probes (QWEN3_K_* in include/qwen3.h)
@@ -204,28 +205,35 @@ def _device_rows(t, name, dtype, like=None, shape=None):
     """A contiguous device tensor of the dtype, on like's device, or ValueError."""
     import torch
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()
-            and (like is None or t.device == like.device) and (shape is None or tuple(t.shape) == tuple(shape))):
+            and (like is None or t.device == like.device) and (shape is None or t.shape == shape)):
         raise ValueError(f"{name} must be a contiguous {dtype} device tensor"
                          + (f" of shape {tuple(shape)}" if shape is not None else "")
                          + (" on the other tensors' device" if like is not None else ""))
     return t
 
 
+@functools.lru_cache(maxsize=256)
+def _rotary_desc(n, n_head, n_kv_head, width, sections, interleaved, theta, eps):
+    """The call's description, made once per shape, and head_dim."""
+    if n_head < 1 or n_kv_head < 1 or width % (n_head + 2 * n_kv_head) or not 1 <= len(sections) <= 4:
+        raise ValueError("rows of q | k | v are (n_head + 2 n_kv_head) head_dim wide, with 1 to 4 sections")
+    hd = width // (n_head + 2 * n_kv_head)
+    return ctypes.byref(Rotary(n, n_head, n_kv_head, hd, len(sections), (ctypes.c_int32 * 4)(*sections),
+                               int(bool(interleaved)), theta, eps)), hd
+
+
 def _rotary_args(qkv, positions, n_head, n_kv_head, sections, theta, q_norm, k_norm, eps, interleaved):
     import torch
-    if not isinstance(qkv, torch.Tensor) or qkv.dim() != 2 or n_head < 1 or n_kv_head < 1:
-        raise ValueError("rows of q | k | v [tokens, (n_head + 2 n_kv_head) head_dim]")
     _device_rows(qkv, "q | k | v", torch.bfloat16)
+    if qkv.dim() != 2:
+        raise ValueError("rows of q | k | v [tokens, (n_head + 2 n_kv_head) head_dim]")
     n, width = qkv.shape
-    hd = width // (n_head + 2 * n_kv_head)
-    if hd * (n_head + 2 * n_kv_head) != width or not 1 <= len(sections) <= 4:
-        raise ValueError("the rows' width must be (n_head + 2 n_kv_head) head_dim, with 1 to 4 sections")
+    r, hd = _rotary_desc(n, n_head, n_kv_head, width, tuple(sections), interleaved, theta, eps)
     _device_rows(positions, "positions", torch.int32, qkv, (len(sections), n))
     for name, g in (("q_norm", q_norm), ("k_norm", k_norm)):
         if g is not None:
             _device_rows(g, name, torch.bfloat16, qkv, (hd,))
-    return Rotary(n, n_head, n_kv_head, hd, len(sections), (ctypes.c_int32 * 4)(*sections), int(bool(interleaved)),
-                  theta, eps)
+    return r
 
 
 def _ptr(t):
@@ -241,9 +249,8 @@ def rotary(qkv, positions, *, n_head, n_kv_head, sections, theta=1e6, q_norm=Non
     import torch
     r = _rotary_args(qkv, positions, n_head, n_kv_head, sections, theta, q_norm, k_norm, eps, interleaved)
     out = torch.empty_like(qkv) if out is None else _device_rows(out, "out", torch.bfloat16, qkv, qkv.shape)
-    with torch.cuda.device(qkv.device):
-        _check(lib().qwen3_rotary_forward(ctypes.byref(r), qkv.data_ptr(), positions.data_ptr(), _ptr(q_norm),
-                                          _ptr(k_norm), out.data_ptr(), torch.cuda.current_stream().cuda_stream))
+    _check(on_stream(qkv.device, lib().qwen3_rotary_forward, r, qkv.data_ptr(), positions.data_ptr(), _ptr(q_norm),
+                     _ptr(k_norm), out.data_ptr()))
     return out
 
 
@@ -255,10 +262,8 @@ def rotary_backward(dout, qkv, positions, *, n_head, n_kv_head, sections, theta=
     r = _rotary_args(qkv, positions, n_head, n_kv_head, sections, theta, q_norm, k_norm, eps, interleaved)
     _device_rows(dout, "dout", torch.bfloat16, qkv, qkv.shape)
     out = torch.empty_like(qkv) if out is None else _device_rows(out, "out", torch.bfloat16, qkv, qkv.shape)
-    with torch.cuda.device(qkv.device):
-        _check(lib().qwen3_rotary_backward(ctypes.byref(r), dout.data_ptr(), qkv.data_ptr(), positions.data_ptr(),
-                                           _ptr(q_norm), _ptr(k_norm), out.data_ptr(),
-                                           torch.cuda.current_stream().cuda_stream))
+    _check(on_stream(qkv.device, lib().qwen3_rotary_backward, r, dout.data_ptr(), qkv.data_ptr(),
+                     positions.data_ptr(), _ptr(q_norm), _ptr(k_norm), out.data_ptr()))
     return out
 
 
@@ -281,8 +286,9 @@ class SharedPrefix:
         self.n_head, self.width, self.out_width = n_head, (n_head + 2 * n_kv_head) * head_dim, n_head * head_dim
         self.plan = torch.empty(n.value, dtype=torch.uint8, device=device)
         with torch.cuda.device(self.plan.device):
-            _check(lib().qwen3_prefix_create(ctypes.byref(cfg), c_lens, self.plan.data_ptr(), n.value,
-                                             torch.cuda.current_stream().cuda_stream, ctypes.byref(self.h)))
+            stream = torch.cuda.current_stream().cuda_stream
+            _check(lib().qwen3_prefix_create(ctypes.byref(cfg), c_lens, self.plan.data_ptr(), n.value, stream,
+                                             ctypes.byref(self.h)))
 
     def close(self):
         if self.h:
@@ -308,9 +314,8 @@ class SharedPrefix:
         out = qkv.new_empty(shapes[0]) if out is None else self._rows(out, "out", shapes[0])
         lse = (qkv.new_empty(shapes[1], dtype=torch.float32) if lse is None
                else self._rows(lse, "lse", shapes[1], torch.float32))
-        with torch.cuda.device(qkv.device):
-            _check(lib().qwen3_prefix_forward(self.h, qkv.data_ptr(), out.data_ptr(), lse.data_ptr(),
-                                              torch.cuda.current_stream().cuda_stream))
+        _check(on_stream(qkv.device, lib().qwen3_prefix_forward, self.h, qkv.data_ptr(), out.data_ptr(),
+                         lse.data_ptr()))
         return out, lse
 
     def backward(self, dout, qkv, out, lse, dqkv=None):
@@ -322,10 +327,8 @@ class SharedPrefix:
         self._rows(out, "out", (self.rows, self.out_width))
         self._rows(lse, "lse", (self.n_head, self.rows), torch.float32)
         dqkv = torch.empty_like(qkv) if dqkv is None else self._rows(dqkv, "dqkv", (self.tokens, self.width))
-        with torch.cuda.device(qkv.device):
-            _check(lib().qwen3_prefix_backward(self.h, qkv.data_ptr(), out.data_ptr(), lse.data_ptr(),
-                                               dout.data_ptr(), dqkv.data_ptr(),
-                                               torch.cuda.current_stream().cuda_stream))
+        _check(on_stream(qkv.device, lib().qwen3_prefix_backward, self.h, qkv.data_ptr(), out.data_ptr(),
+                         lse.data_ptr(), dout.data_ptr(), dqkv.data_ptr()))
         return dqkv
 
 
