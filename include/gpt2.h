@@ -195,7 +195,10 @@ gpt2_status gpt2_adamw_step_noalloc(gpt2_model* m, int64_t step, float* lr_out,
  * 256-byte aligned, scratch of this call until its kernels have run, so that
  * calls (or captured graphs) that may run at the same time need one each. A
  * matrix that holds a NaN or an infinity comes out as NaN. Any rows, cols and
- * count from 1, below 2^31 elements a matrix. */
+ * count from 1, with sides padded to multiples of 64 below 2^31 elements a
+ * matrix and 2^36 in all, count below 2^18. Enqueues on hip_stream, of the
+ * current device, without synchronising; INVALID_ARG, with nothing launched,
+ * for what is not as said here. */
 gpt2_status gpt2_orthogonalise_size(int32_t rows, int32_t cols,
                                     int32_t count, size_t* bytes_out);
 gpt2_status gpt2_orthogonalise(const float* d_x, float* d_y, int32_t rows,

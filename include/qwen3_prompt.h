@@ -32,7 +32,7 @@ typedef struct qwen3_rotary {
   float theta, rms_eps;
 } qwen3_rotary;
 
-/* d_qkv, d_out: bf16 rows of n_tokens tokens, q [n_head * head_dim] | k
+/* d_qkv, d_out: bf16 rows of n_tokens tokens (2^25 at most), q [n_head * head_dim] | k
  * [n_kv_head * head_dim] | v likewise, 16-byte aligned. d_positions: int32
  * [n_axes, n_tokens], any values. d_q_norm, d_k_norm: bf16 [head_dim] gains of
  * the RMSNorm of every query and key head before the turn, 16-byte aligned, or

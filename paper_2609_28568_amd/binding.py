@@ -312,6 +312,7 @@ class GPT2:
             n = ctypes.c_size_t()
             _check(self.L.gpt2_muon_size(ctypes.byref(self.cfg), ctypes.byref(n)))
             self.muon_workspace = self.torch.empty(n.value, dtype=self.torch.uint8, device=self.device)
+            self.muon_workspace.record_stream(self.stream)
         lr = ctypes.c_float()
         how = Muon(float(momentum), int(bool(nesterov)), int(iterations), float(scale))
         _check(self.L.gpt2_muon_step(self.handle, int(step), ctypes.byref(how), self.muon_workspace.data_ptr(),

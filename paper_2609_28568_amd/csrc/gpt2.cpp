@@ -1348,7 +1348,7 @@ gpt2_status gpt2_orthogonalise_size(int32_t rows, int32_t cols, int32_t count, s
   const size_t bytes = ortho_layout(&g, 1);
   if (!bytes || !bytes_out) {
     g_last_error = bytes ? "bytes_out is NULL"
-                         : "rows, cols and count must be positive, a matrix (padded to multiples of 64) below 2^31 elements";
+                         : "rows, cols and count must be positive, a matrix below 2^31 elements and all below 2^36 (padded to multiples of 64), count below 2^18";
     return GPT2_ERR_INVALID_ARG;
   }
   *bytes_out = bytes;

@@ -858,8 +858,7 @@ hipError_t product(const Params& p, hipStream_t s) {
     }
     return t;
   };
-  const long t64 = tiles(64), t128 = tiles(128), t192 = tiles(192);
-  if (t64 > 0x7fffffffL) return hipErrorInvalidValue;
+  const long t128 = tiles(128), t192 = tiles(192);
   int steps = 0;   // the longest contraction
   for (int k = 0; k < p.ngroups; ++k) steps = std::max(steps, PH == GRAM ? p.g[k].np : p.g[k].mp);
 #define L(T, NS) hipLaunchKernelGGL((ortho_product_kernel<T, NS, PH>), dim3((unsigned)tiles(T)), dim3(256), 0, s, p)
@@ -891,20 +890,21 @@ long align128(long n) { return (n + 127) / 128 * 128; }
 // Offsets of every group's planes (fp16 elements), after the partial sums;
 // returns the bytes in all, or 0 when a shape is out of range.
 size_t ortho_layout(OrthoGroup* g, int ngroups) {
-  long mats = 0;
+  long mats = 0, tiles = 0;
   for (int k = 0; k < ngroups; ++k) {
     OrthoGroup& q = g[k];
     if (q.rows < 1 || q.cols < 1 || q.count < 1) return 0;
     q.tall = q.rows > q.cols;
     const long m = q.tall ? q.cols : q.rows, n = q.tall ? q.rows : q.cols;
     const long mp = (m + PAD - 1) / PAD * PAD, np = (n + PAD - 1) / PAD * PAD;
-    // 32-bit byte offsets within a plane, 32-bit tile and part counts
-    if (np > (1L << 30) || mp * np >= (1L << 31) || mp * np / (PAD * PAD) * q.count >= (1L << 31)) return 0;
+    if (np > (1L << 30) || mp * np >= (1L << 31)) return 0;   // 32-bit byte offsets within a plane
     q.mp = (int)mp;
     q.np = (int)np;
     mats += q.count;
+    tiles += mp * np / (PAD * PAD) * q.count;
+    // launches of less than 2^32 threads
+    if (mats * ORTHO_PARTS * 256 >= (1L << 32) || tiles * 256 >= (1L << 32)) return 0;
   }
-  if (mats * ORTHO_PARTS >= (1L << 31)) return 0;
   long o = align128(mats * ORTHO_PARTS * (long)(sizeof(double) / 2));
   for (int k = 0; k < ngroups; ++k) {
     OrthoGroup& q = g[k];

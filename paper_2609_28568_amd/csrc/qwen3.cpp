@@ -641,7 +641,7 @@ const char* rotary_axes(RotaryArgs* a, int hd, int n_axes, const int32_t* sectio
 const char* rotary_args(const qwen3_rotary* r, const void* in, const void* raw, const int32_t* pos, const void* qn,
                         const void* kn, const void* out, RotaryArgs* a) {
   if (!r) return "null rotary description";
-  if (r->n_tokens < 0 || r->n_tokens > (1 << 30) || r->n_head < 1 || r->n_kv_head < 1 || r->n_head > (1 << 20) || r->n_kv_head > (1 << 20))
+  if (r->n_tokens < 0 || r->n_tokens > (1 << 25) || r->n_head < 1 || r->n_kv_head < 1 || r->n_head > (1 << 20) || r->n_kv_head > (1 << 20))
     return "n_tokens, n_head or n_kv_head out of range";
   if (const char* why = rotary_axes(a, r->head_dim, r->n_axes, r->sections, r->interleaved, r->theta)) return why;
   if (!(r->rms_eps >= 0.0f)) return "rms_eps must not be negative";

@@ -286,8 +286,8 @@ class SharedPrefix:
         self.n_head, self.width, self.out_width = n_head, (n_head + 2 * n_kv_head) * head_dim, n_head * head_dim
         self.plan = torch.empty(n.value, dtype=torch.uint8, device=device)
         with torch.cuda.device(self.plan.device):
-            stream = torch.cuda.current_stream().cuda_stream
-            _check(lib().qwen3_prefix_create(ctypes.byref(cfg), c_lens, self.plan.data_ptr(), n.value, stream,
+            self.stream = torch.cuda.current_stream().cuda_stream
+            _check(lib().qwen3_prefix_create(ctypes.byref(cfg), c_lens, self.plan.data_ptr(), n.value, self.stream,
                                              ctypes.byref(self.h)))
 
     def close(self):
@@ -300,6 +300,13 @@ class SharedPrefix:
             self.close()
         except Exception:
             pass
+
+    def _run(self, fn, *args):
+        def call(*args):
+            if args[-1] != self.stream:   # the buffer is another stream's: it stays until this one is done with it
+                self.plan.record_stream(self.torch.cuda.current_stream(self.plan.device))
+            return fn(self.h, *args)
+        _check(on_stream(self.plan.device, call, *args))
 
     def _rows(self, t, name, shape, dtype=None):
         return _device_rows(t, name, dtype or self.torch.bfloat16, self.plan, shape)
@@ -314,8 +321,7 @@ class SharedPrefix:
         out = qkv.new_empty(shapes[0]) if out is None else self._rows(out, "out", shapes[0])
         lse = (qkv.new_empty(shapes[1], dtype=torch.float32) if lse is None
                else self._rows(lse, "lse", shapes[1], torch.float32))
-        _check(on_stream(qkv.device, lib().qwen3_prefix_forward, self.h, qkv.data_ptr(), out.data_ptr(),
-                         lse.data_ptr()))
+        self._run(lib().qwen3_prefix_forward, qkv.data_ptr(), out.data_ptr(), lse.data_ptr())
         return out, lse
 
     def backward(self, dout, qkv, out, lse, dqkv=None):
@@ -327,8 +333,8 @@ class SharedPrefix:
         self._rows(out, "out", (self.rows, self.out_width))
         self._rows(lse, "lse", (self.n_head, self.rows), torch.float32)
         dqkv = torch.empty_like(qkv) if dqkv is None else self._rows(dqkv, "dqkv", (self.tokens, self.width))
-        _check(on_stream(qkv.device, lib().qwen3_prefix_backward, self.h, qkv.data_ptr(), out.data_ptr(),
-                         lse.data_ptr(), dout.data_ptr(), dqkv.data_ptr()))
+        self._run(lib().qwen3_prefix_backward, qkv.data_ptr(), out.data_ptr(), lse.data_ptr(), dout.data_ptr(),
+                  dqkv.data_ptr())
         return dqkv
 
 
@@ -431,6 +437,8 @@ class Qwen3:
                          (len(sections), self.cfg.B * self.cfg.T))
         sec = (ctypes.c_int32 * len(sections))(*sections)
         _check(lib().qwen3_set_positions(self.h, _ptr(positions), len(sections), sec, int(bool(interleaved))), self.h)
+        if positions is not None:
+            positions.record_stream(self.stream)   # read there, whichever stream it was made on
         self._positions = positions
 
     def set_layout(self, prefix_len=0, seq_lens=None):
@@ -446,6 +454,7 @@ class Qwen3:
         _check(lib().qwen3_layout_size(self.h, prefix_len, len(lens), c_lens, ctypes.byref(n)), self.h)
         plan = self.torch.empty(n.value, dtype=self.torch.uint8, device=self.bufs["workspace"].device)
         _check(lib().qwen3_set_layout(self.h, prefix_len, len(lens), c_lens, plan.data_ptr(), n.value), self.h)
+        plan.record_stream(self.stream)
         self._plan = plan
 
     def muon_step(self, norm_out=None, momentum=0.95, nesterov=True, iterations=5, scale=0.2):
@@ -457,6 +466,7 @@ class Qwen3:
             _check(lib().qwen3_muon_size(ctypes.byref(self.cfg), ctypes.byref(n)))
             self.muon_workspace = self.torch.empty(n.value, dtype=self.torch.uint8,
                                                    device=self.bufs["workspace"].device)
+            self.muon_workspace.record_stream(self.stream)
         how = Muon(float(momentum), int(bool(nesterov)), int(iterations), float(scale))
         _check(lib().qwen3_muon_step(self.h, ctypes.byref(how), self.muon_workspace.data_ptr(),
                                      self.muon_workspace.numel(),

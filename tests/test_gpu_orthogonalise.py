@@ -40,7 +40,11 @@ def batch(count, rows, cols, seed, scale=1e-3):
 
 
 SHAPES = [(1, 1, 1), (2, 1, 77), (1, 300, 1), (3, 5, 7), (2, 64, 64), (1, 65, 63), (2, 63, 129), (2, 129, 130),
-          (1, 200, 1000), (1, 1001, 190), (40, 16, 256), (5, 128, 384), (3, 384, 320), (9, 700, 513)]
+          (1, 200, 1000), (1, 1001, 190), (40, 16, 256), (5, 128, 384), (3, 384, 320), (9, 700, 513),
+          # whole in LDS: one to four blocks of 32 rows, sides that do and do not fill them
+          (2, 31, 992), (2, 1184, 32), (3, 64, 480), (2, 450, 50), (2, 96, 288), (2, 70, 301), (1, 128, 128), (2, 141, 97),
+          # larger tiles of the products, odd sides in the last ones
+          (24, 513, 700), (21, 570, 760), (30, 300, 2050), (26, 2050, 300)]
 
 
 @pytest.mark.parametrize("count,rows,cols", SHAPES)
@@ -65,20 +69,22 @@ def test_other_iteration_counts(iterations):
     assert all(rel_l2(y[i], newton_schulz(x[i], iterations)) < tol for i in range(2))
 
 
+@pytest.mark.parametrize("rows,cols", [(70, 90), (200, 190)])
 @pytest.mark.parametrize("scale", [1e-30, 1e-12, 1e18])
-def test_scale_does_not_matter(scale):
+def test_scale_does_not_matter(scale, rows, cols):
     from paper_2609_28568_amd import binding
-    x = batch(1, 70, 90, 5, scale)
+    x = batch(1, rows, cols, 5, scale)
     y = binding.orthogonalise(torch.from_numpy(x).cuda()).cpu().numpy()
     assert rel_l2(y[0], newton_schulz(x[0])) < TOL
 
 
-def test_zeros_and_invalid_numbers_stay_in_their_matrix():
+@pytest.mark.parametrize("rows,cols", [(40, 66), (140, 270)])
+def test_zeros_and_invalid_numbers_stay_in_their_matrix(rows, cols):
     from paper_2609_28568_amd import binding
-    x = batch(5, 40, 66, 6)
+    x = batch(5, rows, cols, 6)
     x[1] = 0
     x[2, 3, 4] = np.nan
-    x[3, 39, 65] = np.inf
+    x[3, rows - 1, cols - 1] = np.inf
     x[4, 7] = 0
     y = binding.orthogonalise(torch.from_numpy(x).cuda()).cpu().numpy()
     assert np.all(y[1] == 0)
@@ -87,13 +93,14 @@ def test_zeros_and_invalid_numbers_stay_in_their_matrix():
     assert all(rel_l2(y[i], newton_schulz(x[i])) < TOL for i in (0, 4))
 
 
-def test_in_place_unaligned_and_an_own_workspace():
+@pytest.mark.parametrize("rows,cols", [(33, 52), (260, 132)])
+def test_in_place_unaligned_and_an_own_workspace(rows, cols):
     from paper_2609_28568_amd import binding
-    x = batch(2, 33, 52, 7)
+    x = batch(2, rows, cols, 7)
     flat = torch.zeros(x.size + 1, device="cuda")
-    d = flat[1:].view(2, 33, 52)   # 4-byte alignment only
+    d = flat[1:].view(2, rows, cols)   # 4-byte alignment only
     d.copy_(torch.from_numpy(x))
-    ws = torch.empty(binding.orthogonalise_size(33, 52, 2), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(binding.orthogonalise_size(rows, cols, 2), dtype=torch.uint8, device="cuda")
     whole = binding.orthogonalise(d.clone())
     assert binding.orthogonalise(d, out=d, workspace=ws) is d
     assert torch.equal(d, whole) and float(flat[0]) == 0.0
@@ -128,11 +135,12 @@ def muon(p, g, mom, coef, lr, wd, momentum, nesterov, scale, iterations=5):
     return p - lr * (wd * p + scale * np.sqrt(max(p.shape)) * newton_schulz(u, iterations)), m
 
 
-@pytest.mark.parametrize("nesterov", [True, False])
-def test_gpt2_muon_step(nesterov):
+@pytest.mark.parametrize("nesterov,wide", [(True, False), (False, False), (True, True)])
+def test_gpt2_muon_step(nesterov, wide):
+    """wide: matrices that go through the products, tall, wide and square; otherwise they stay in LDS."""
     from paper_2609_28568_amd import binding
     # one warmup step, so that the rate is the peak and the update is well above fp32's rounding of the weights
-    w = workload("tiny")
+    w = workload("tiny", **(dict(d_model=256, d_ff=1024) if wide else {}))
     opt = dict(synth.OPTIM, lr_max=0.05, warmup_steps=1, grad_clip=0.5)
     m = binding.GPT2(binding.make_config(w, opt))
     other = binding.GPT2(binding.make_config(w, opt))

@@ -84,6 +84,11 @@ CASES = {
     "long_walks": (1, 1, 128, 2500, [30, 50], False),
     "long_walks_hd64": (2, 1, 64, 2100, [300, 11, 200], True),
     "prefix_of_one_tile": (2, 2, 128, 128, [128, 64], True),
+    # more workgroups than CUs: one group of waves each, walks whole and shared
+    "many_items": (16, 16, 64, 700, [250, 333], True),
+    "many_items_wide": (12, 12, 128, 500, [700, 61], True),
+    "few_rows_shared_widely": (2, 1, 128, 6000, [1, 2], False),
+    "few_rows_shared_widely_hd64": (8, 2, 64, 5000, [3] * 7, False),
 }
 
 
@@ -177,6 +182,25 @@ def test_a_sequence_does_not_read_the_others():
     z, _ = plan("answers").forward(dev(other))
     keep = np.r_[0:P + 40, P + 57:qkv.shape[0]]
     assert torch.equal(y[keep], z[keep])
+
+
+def test_on_a_stream_of_its_own():
+    """A layout made on one stream and used on another, and freed right after."""
+    qkv, dout, how = inputs("long_walks")
+    x, g = dev(qkv), dev(dout)
+    y, l = plan("long_walks").forward(x)
+    d = plan("long_walks").backward(g, x, y, l)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    p = plan("long_walks")
+    size = p.plan.numel()
+    with torch.cuda.stream(side):
+        got = p.forward(x)
+        grad = p.backward(g, x, *got)
+    del p
+    torch.empty(size, dtype=torch.uint8, device="cuda").fill_(255)   # may not take the layout's place yet
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], y) and torch.equal(got[1], l) and torch.equal(grad, d)
 
 
 def test_a_captured_pass_replays():

@@ -27,7 +27,7 @@ def test_library_exports_the_prompt_header():
 # ---- orthogonalised updates
 
 @pytest.mark.parametrize("shape", [(0, 4, 1), (4, 0, 1), (4, 4, 0), (-1, 4, 1), (1 << 16, 1 << 16, 1),
-                                   (64, 64, 1 << 30)])
+                                   (64, 64, 1 << 30), (8, 8, 1 << 18), (1 << 14, 1 << 14, 1 << 9)])
 def test_orthogonalise_refuses_shapes(shape):
     with pytest.raises(binding.LibError) as e:
         binding.orthogonalise_size(*shape)
@@ -86,7 +86,7 @@ def rotary_desc(**over):
 
 
 @pytest.mark.parametrize("over,why", [
-    (dict(n_tokens=-1), "n_tokens"), (dict(n_head=0), "n_head"), (dict(n_kv_head=0), "n_kv_head"),
+    (dict(n_tokens=-1), "n_tokens"), (dict(n_tokens=(1 << 25) + 1), "n_tokens"), (dict(n_head=0), "n_head"), (dict(n_kv_head=0), "n_kv_head"),
     (dict(head_dim=96), "head_dim"), (dict(n_axes=0), "n_axes"), (dict(n_axes=5), "n_axes"),
     (dict(sections=(16, 24, 25)), "sum"), (dict(sections=(16, 24, 23)), "sum"), (dict(sections=(-1, 41, 24)), "range"),
     (dict(sections=(0, 40, 24), interleaved=1), "fit"), (dict(theta=0.0), "theta"), (dict(theta=float("inf")), "theta"),
