@@ -575,16 +575,16 @@ gpt2_status clip_norm(qwen3_model* m, float* d_grad_norm_out) {
   return GPT2_OK;
 }
 
-// The adapters' matrices for the orthogonalised update: of every projection
-// its A, the r real rows of its block, and its B, whole (RP columns: the
-// padding is zero, and a zero column stays one through every product). m null:
-// shapes only.
+// The adapters' matrices for the orthogonalised update: the r real rows of
+// every projection's A and the r real columns of its B; the padding is left as
+// it is, zero. m null: shapes only.
 void muon_groups(const Dims& d, OrthoArgs* a, qwen3_model* m, const gpt2_muon* how) {
   size_t off = 0;
-  auto add = [&](size_t at, long stride, int rows, int cols, int count) {
+  auto add = [&](size_t at, long stride, int rows, int cols, int ld, int count) {
     OrthoGroup& g = a->g[a->ngroups++];
     g.rows = rows;
-    g.cols = g.ld = cols;
+    g.cols = cols;
+    g.ld = ld;
     g.count = count;
     g.stride = stride;
     if (!m) return;
@@ -592,15 +592,15 @@ void muon_groups(const Dims& d, OrthoArgs* a, qwen3_model* m, const gpt2_muon* h
     g.y = static_cast<float*>(m->buf.lora_f32) + at;
     g.mom = static_cast<float*>(m->buf.adam_m) + at;
     g.p_bf16 = static_cast<bf16_t*>(m->buf.lora_bf16) + at;
-    g.scale = how->scale * std::sqrt((float)std::max(rows, cols == RP ? d.r : cols));
+    g.scale = how->scale * std::sqrt((float)std::max(rows, cols));
   };
   for (int g = 0; g < G_N; ++g) {
     if (!(d.groups & (1 << g))) continue;
     const GroupGeom gg = group_geom(d, g);
-    add(off, (long)RP * gg.in, d.r, gg.in, d.L * gg.n);
+    add(off, (long)RP * gg.in, d.r, gg.in, gg.in, d.L * gg.n);
     off += (size_t)d.L * gg.n * RP * gg.in;
     for (int j = 0, row = 0; j < gg.n; row += gg.out[j], ++j)
-      add(off + (size_t)row * RP, (long)gg.out_total * RP, gg.out[j], RP, d.L);
+      add(off + (size_t)row * RP, (long)gg.out_total * RP, gg.out[j], d.r, RP, d.L);
     off += (size_t)d.L * gg.out_total * RP;
   }
 }

@@ -203,13 +203,15 @@ def unpack_lora(packed: dict, targets, r: int, out_widths: dict) -> dict:
 
 def _device_rows(t, name, dtype, like=None, shape=None):
     """A contiguous device tensor of the dtype, on like's device, or ValueError."""
-    import torch
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()
-            and (like is None or t.device == like.device) and (shape is None or t.shape == shape)):
-        raise ValueError(f"{name} must be a contiguous {dtype} device tensor"
-                         + (f" of shape {tuple(shape)}" if shape is not None else "")
-                         + (" on the other tensors' device" if like is not None else ""))
-    return t
+    try:
+        if (t.dtype is dtype and (t.device == like.device if like is not None else t.is_cuda)
+                and (shape is None or t.shape == shape) and t.is_contiguous()):
+            return t
+    except AttributeError:   # not a tensor
+        pass
+    raise ValueError(f"{name} must be a contiguous {dtype} device tensor"
+                     + (f" of shape {tuple(shape)}" if shape is not None else "")
+                     + (" on the other tensors' device" if like is not None else ""))
 
 
 @functools.lru_cache(maxsize=256)

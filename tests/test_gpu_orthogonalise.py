@@ -192,9 +192,11 @@ def test_gpt2_muon_step(nesterov, wide):
     other.close()
 
 
-def test_qwen3_muon_step():
+@pytest.mark.parametrize("rank", [16, 1, 21, 32])
+def test_qwen3_muon_step(rank):
     from paper_2609_28568_amd import qwen3_binding as qb
-    w = dict(synth.QWEN3_WORKLOADS["qwen3_tiny"])
+    # 1280 rows of gate and up: with the higher ranks more than a CU's LDS holds
+    w = dict(synth.QWEN3_WORKLOADS["qwen3_tiny"], lora_rank=rank, d_ff=1280)
     opt = dict(synth.QWEN3_OPTIM, lr=0.05, grad_clip=0.1)
     m = qb.Qwen3(qb.make_config(w, opt))
     base, lora = synth.init_qwen3(w, b_std=0.02)
