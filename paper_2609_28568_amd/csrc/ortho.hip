@@ -496,7 +496,9 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
 // apart, hi plane then lo. 8 waves: the tiles of A and P are dealt to them, with
 // few tiles A's contraction too (partial sums through LDS); of X each wave
 // takes blocks of 32 columns, which only depend on themselves, so they are
-// updated in place.
+// updated in place. 112 matrices of 16 x 1024: 42 us, two of 64 x 256: 35, where
+// 17 launches of the products took 193 and 78; an iteration is 5 us (A 1.5, P
+// 1.3, X 2), the loads and the end 10.
 struct SmallShape {
   int mp, np, xs, as, split;   // padded sides; row strides; waves that share a tile of A
   int a_at, red_at, bytes;     // LDS offsets of A and of the partial sums
