@@ -388,6 +388,7 @@ struct PrefixItem {
   int32_t row, f0, f1, slot;
   int32_t npre, own;   // forward, dQ
   int32_t t0, t1;      // dK/dV
+  int32_t tiles;       // of the whole walk
 };
 // Partial results slot..slot+parts-1 of rows (or keys) row..row+127 make one.
 struct PrefixJoin {

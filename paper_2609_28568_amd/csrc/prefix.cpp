@@ -39,6 +39,7 @@ void deal(const std::vector<PrefixItem>& walks, int per, std::vector<PrefixItem>
       it.f0 = (int)((long)nt * i / parts);
       it.f1 = (int)((long)nt * (i + 1) / parts);
       it.slot = parts > 1 ? slots++ : -1;
+      it.tiles = nt;
       items.push_back(it);
     }
   }

@@ -404,6 +404,70 @@ __global__ __launch_bounds__(256) void prefix_dsum_kernel(PrefixArgs a) {
   if (c == 0) a.dsum[(size_t)h * a.nq + t - a.q0] = s;
 }
 
+// D from the bf16 O is off by a rounding of O, which all keys of the row share.
+// Beside the roundings of dS, which average, that counts the more the fewer keys
+// hold the row's weight, so rows of few keys take a first walk that sums D =
+// sum_j P_j dP_j in fp32 and leave it for dK/dV. Longer walks would pay two
+// products more of five for a difference of a few per cent.
+constexpr int EXACT_TILES = 8;
+
+// That sum over the whole walk of the item's rows, tiles dealt out among the
+// groups as below; the walk's first tiles are under way in the first stages.
+template <int HD, int GR>
+DEV float walk_d(const PrefixArgs& a, const KeyWalk<HD>& keys, const Row& r, int tiles, const bf16x8 (&qf)[HD / 16],
+                 const bf16x8 (&df)[HD / 16], float sc, float lse2, lds_char_t* all_groups, int wave, int group,
+                 int lane) {
+  using S = Shape<HD>;
+  constexpr int GROUP = 2 * 2 * S::TBA;
+  lds_char_t* smem = all_groups + group * GROUP;
+  const int lq = lane & 31, g = lane >> 5;
+  float sum = 0.0f;
+  for (int f0 = 0; f0 < tiles; f0 += GR) {
+    const int f = f0 + group;
+    lds_char_t* Ks = smem + f0 / GR % 2 * 2 * S::TBA;
+    wait_vmcnt<0>();
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // this wave's reads of the stage that the next loads overwrite are done
+    block_barrier();
+    if (f + GR < tiles) keys.issue(f + GR, smem + (f0 / GR + 1) % 2 * 2 * S::TBA, wave, lane);
+    if (f >= tiles) continue;
+    const int kv0 = keys.key0(f);
+    const bool own = keys.is_own(f);
+    if (sight(a, r, kv0, own) == NONE) continue;
+    int lo, hi;
+    seen(a, r, own, lo, hi);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      floatx16 p, dp;
+      zero(p);
+      zero(dp);
+#pragma unroll
+      for (int k = 0; k < S::KS; ++k) {
+        p = mfma32(read_row<HD>(Ks, 32 * t + lq, 2 * k + g), qf[k], p);
+        dp = mfma32(read_row<HD>(Ks + S::TBA, 32 * t + lq, 2 * k + g), df[k], dp);
+      }
+      const int k0 = kv0 + 32 * t + 4 * g;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float x = fast_exp2(p[e] * sc - lse2) * dp[e];
+        sum += k0 + acc_row(e, 0) >= lo && k0 + acc_row(e, 0) <= hi ? x : 0.0f;
+      }
+    }
+  }
+  sum = sum32(sum);
+  // the groups' sums, in order; the stages are free for the walk that follows
+  __syncthreads();
+  if constexpr (GR > 1) {
+    LDS_AS float* part = (LDS_AS float*)all_groups;
+    if (lane < 32) part[(group * 4 + wave) * 32 + lq] = sum;
+    __syncthreads();
+    sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < GR; ++k) sum += part[(k * 4 + wave) * 32 + lq];
+    __syncthreads();
+  }
+  return sum;
+}
+
 // dQ of 128 rows, walking the forward's tiles: dS = P (dO V^T - D), dQ = dS K.
 template <int HD, int GR>
 __global__ __launch_bounds__(256 * GR, GR == 1 ? 2 : 1) void prefix_dq_kernel(PrefixArgs a) {
@@ -420,7 +484,9 @@ __global__ __launch_bounds__(256 * GR, GR == 1 ? 2 : 1) void prefix_dq_kernel(Pr
   keys.init(a, w);
   auto stage = [&](int f) { return smem + (f - w.it.f0) / GR % 2 * 2 * S::TBA; };
   // under way while the rows are read
-  if (w.it.f0 + group < w.it.f1) keys.issue(w.it.f0 + group, stage(w.it.f0 + group), wave, lane);
+  const bool exact = w.it.tiles <= EXACT_TILES;
+  const int from = exact ? 0 : w.it.f0, to = exact ? w.it.tiles : w.it.f1;
+  if (from + group < to) keys.issue(from + group, smem, wave, lane);
   const Row r = row_of(a, w.it.row + 32 * wave, w.j, lane);
 
   bf16x8 qf[S::KS], df[S::KS];
@@ -431,12 +497,21 @@ __global__ __launch_bounds__(256 * GR, GR == 1 ? 2 : 1) void prefix_dq_kernel(Pr
     qf[s] = as_bf16x8(*reinterpret_cast<const uint4*>(q + 16 * s + 8 * g));
     df[s] = as_bf16x8(*reinterpret_cast<const uint4*>(dout + 16 * s + 8 * g));
   }
-  const float lse2 = a.lse[(size_t)r.h * a.nq + r.rq] * LOG2E, dsum = a.dsum[(size_t)r.h * a.nq + r.rq];
+  const size_t d_at = (size_t)r.h * a.nq + r.rq;
+  const float lse2 = a.lse[d_at] * LOG2E;
+  const float scale = 1.0f / sqrtf((float)HD);
+  const float sc = scale * LOG2E;
+  float dsum;
+  if (exact) {
+    dsum = walk_d<HD, GR>(a, keys, r, w.it.tiles, qf, df, sc, lse2, (lds_char_t*)smem_raw, wave, group, lane);
+    if (w.it.f0 + group < w.it.f1) keys.issue(w.it.f0 + group, smem, wave, lane);
+    if (w.it.f0 == 0 && group == 0 && r.on && g == 0) a.dsum[d_at] = dsum;
+  } else {
+    dsum = a.dsum[d_at];
+  }
   floatx16 dq[S::DT];
 #pragma unroll
   for (int d = 0; d < S::DT; ++d) zero(dq[d]);
-  const float scale = 1.0f / sqrtf((float)HD);
-  const float sc = scale * LOG2E;
 
   for (int f0 = w.it.f0; f0 < w.it.f1; f0 += GR) {
     const int f = f0 + group;

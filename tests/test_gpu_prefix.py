@@ -138,6 +138,26 @@ def test_against_the_definition(name):
     p.close()
 
 
+@pytest.mark.parametrize("name", ["answers_hd64", "nothing_but_a_token", "groups_of_eight", "packed_without_prefix", "many_short"])
+def test_rows_of_one_key_have_no_score_gradient(name):
+    """Such a row's probability is 1 and dP - D = 0. P comes from scores and a
+    log-sum-exp below 32 in fp32, about eight roundings of them: |1 - P| <=
+    2^-24 * 8 * 32 = 2^-16, so dS is at most 2^-16 |dP|, and its two roundings
+    to bf16 do not double that. D from the bf16 output would leave 2^-9 |dP|."""
+    qkv, dout, (H, Hkv, hd, P, lens, q0) = inputs(name)
+    p = plan(name)
+    x, g = torch.tensor(qkv).cuda().bfloat16(), torch.tensor(dout).cuda().bfloat16()
+    out, lse = p.forward(x)
+    dqkv = p.backward(g, x, out, lse).float().cpu().numpy().astype(np.float64).reshape(qkv.shape[0], -1, hd)
+    xs, gs = np.abs(qkv.astype(np.float64)).reshape(-1, H + 2 * Hkv, hd), np.abs(dout.astype(np.float64)).reshape(-1, H, hd)
+    rows = np.flatnonzero(sees(P, lens, q0).sum(1) == 1)
+    assert len(rows) > 0
+    for r in rows:
+        for h in range(H):
+            k, v = xs[q0 + r, H + h // (H // Hkv)], xs[q0 + r, H + Hkv + h // (H // Hkv)]
+            assert (np.abs(dqkv[q0 + r, h]) <= 2.0 ** -15 * (gs[r, h] @ v) * k / np.sqrt(hd)).all(), (r, h)
+
+
 def test_gradient_against_differences():
     name = "answers_hd64"
     qkv, dout, how = inputs(name)
