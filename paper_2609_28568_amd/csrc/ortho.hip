@@ -12,15 +12,16 @@
 // errors with them, so bf16 products would leave a per cent. Every operand is
 // held as two fp16 numbers instead, hi = fp16(v s) and lo = fp16(v s - hi)
 // with s = 2^13 (|v| < 3, so v s < 65504; the rest of an fp32 significand down
-// to 2^-37 absolute), and a product is three MFMAs into one fp32 accumulator:
+// to 2^-37 absolute), and a product is three MFMAs into fp32 accumulators:
 // hi hi + hi lo + lo hi. The dropped lo lo is 2^-22 of the product at most.
 // That is a third of the fp16 rate, which is five times the card's fp32 one.
 //
 // Matrices that fit the LDS of a CU go through all iterations in one workgroup
-// (ortho_small_kernel). For the others, one product kernel for the three products; A and A^2 are symmetric, so only
-// the tiles on and below the diagonal are computed, and written twice. All
-// matrices of all shapes of one call go through each product in one launch:
-// workgroup b finds its group, matrix and tile.
+// (ortho_small_kernel). For the others, one product kernel for the three
+// products; A and A^2 are symmetric, so only the tiles on and below the diagonal
+// are computed, and written twice. All matrices of all shapes of one call go
+// through each product in one launch: workgroup b finds its group, matrix and
+// tile.
 //
 // What bounds it: 48 matrices of 768 x 768 take 1.6 ms, their products
 // 795 (A), 750 (P) and 840 (X) TFLOP/s of MFMA work, at the MFMA unit's power
@@ -305,13 +306,22 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
     if (part == 1) issue_panel<T>(rl[1], g.mp, m0, kt, st + PLANE, wave, lane);
     if (part == 2) right(1);
   };
-  floatx16 acc[TT][TT];
+  // The cross terms in sums of their own where the registers hold them (192
+  // would take 288 for the sums alone), so that the large sums are rounded a
+  // third as often. Against 64 bits, one sum and two: 28 x 2032 2.2e-6 and
+  // 1.2e-6, 682 x 489 2.3e-6 and 1.4e-6, 1024 x 1024 3.0e-6 and 1.8e-6 (fp32
+  // library products 1.1e-6, 2.1e-6, 2.5e-6), for at most a hundredth of the time.
+  constexpr bool APART = T <= 128;
+  floatx16 acc[TT][TT], low[APART ? TT : 1][APART ? TT : 1];
 #pragma unroll
   for (int i = 0; i < TT; ++i)
 #pragma unroll
     for (int j = 0; j < TT; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+      for (int r = 0; r < 16; ++r) {
+        acc[i][j][r] = 0.0f;
+        if constexpr (APART) low[i][j][r] = 0.0f;
+      }
   half8 fl[2][2][TT], fr[2][2][TT];   // [buffer][hi, lo]
   constexpr int FRAGS = 4 * TT;
   // a k-step's fragments, in three parts, the hi ones first
@@ -329,9 +339,10 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
 #pragma unroll
     for (int i = 0; i < TT; ++i)
 #pragma unroll
-      for (int j = 0; j < TT; ++j)
-        acc[i][j] =
-            __builtin_amdgcn_mfma_f32_32x32x16_f16(fr[b][part == 1][j], fl[b][part == 2][i], acc[i][j], 0, 0, 0);
+      for (int j = 0; j < TT; ++j) {
+        floatx16& sum = APART && part > 0 ? low[APART ? i : 0][APART ? j : 0] : acc[i][j];
+        sum = __builtin_amdgcn_mfma_f32_32x32x16_f16(fr[b][part == 1][j], fl[b][part == 2][i], sum, 0, 0, 0);
+      }
   };
   // One k-step's MFMAs on fragment buffer b, with the reads of the next step's
   // fragments and the loads of a later stage dealt out between them: issued in
@@ -376,6 +387,14 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
 #pragma unroll
   for (int s = 0; s + 1 < KSTEPS; ++s) step(s & 1, true, nk - 1, s + 1, false, 0);
   step(1, false, 0, 0, false, 0);
+  if constexpr (APART) {
+#pragma unroll
+    for (int i = 0; i < TT; ++i)
+#pragma unroll
+      for (int j = 0; j < TT; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] += low[i][j][r];
+  }
 
   // Blocks of 32 x 32 go through LDS, so that every store is one contiguous
   // run: from the accumulators, where lane l holds row l%32 and, in registers
