@@ -20,8 +20,8 @@
 // second launch in a fixed order.
 //
 // Measured: 16 sequences of 256 over a prefix of 2048, 16 + 8 heads of 128:
-// forward 130 us (690 TFLOP/s), dQ 175-194 (700-770), dK/dV 246 + 11 (730);
-// waves wait on their own chain of products, exponentials and products. 64
+// forward 127-130 us (700 TFLOP/s), dQ 170-194 (700-790), dK/dV 230-246 + 11
+// (750); waves wait on their own chain of products, exponentials and products. 64
 // single tokens after 8192: 18 + 5 us, 34 MB of keys and values and 12 MB of
 // partial results.
 //
@@ -407,8 +407,11 @@ __global__ __launch_bounds__(256) void prefix_dsum_kernel(PrefixArgs a) {
 // D from the bf16 O is off by a rounding of O, which all keys of the row share.
 // Beside the roundings of dS, which average, that counts the more the fewer keys
 // hold the row's weight, so rows of few keys take a first walk that sums D =
-// sum_j P_j dP_j in fp32 and leave it for dK/dV. Longer walks would pay two
-// products more of five for a difference of a few per cent.
+// sum_j P_j dP_j in fp32 and leave it for dK/dV: gradients of 9 ragged answers
+// with 64-wide heads are 2.4e-3 off instead of 2.6e-3, of rows of up to 70 keys
+// 2.4e-3 instead of 2.8e-3 (rounding exact ones 1.7e-3); dQ of the former takes
+// 19 us instead of 14. Longer walks would pay two products more of five for a
+// difference of a few per cent.
 constexpr int EXACT_TILES = 8;
 
 // That sum over the whole walk of the item's rows, tiles dealt out among the
@@ -798,11 +801,18 @@ __global__ __launch_bounds__(512, 1) void prefix_dkdv_kernel(PrefixArgs a) {
 template <int HD>
 hipError_t fwd_t(const PrefixArgs& a, hipStream_t s) {
   const unsigned wgs = a.nitems * a.Hkv;
-  constexpr int GR = HD == 64 ? 4 : 2;   // as many as the registers allow
+  // One workgroup a CU: groups of waves share its walk, as many as the registers
+  // allow (one walk of 129 tiles for each of 8 heads of 128: 187 us with one
+  // group, 117 with two). With more workgroups than CUs two of one group share
+  // a CU instead.
+  constexpr int GR = HD == 64 ? 4 : 2;
   if (wgs <= 256) hipLaunchKernelGGL((prefix_fwd_kernel<HD, GR>), dim3(wgs), dim3(256 * GR), 0, s, a);
   else hipLaunchKernelGGL((prefix_fwd_kernel<HD, 1>), dim3(wgs), dim3(256), 0, s, a);
   if (!a.njoins) return hipGetLastError();
   const unsigned joins = a.njoins * a.Hkv;
+  // Many parts: a wave a row (64 tokens after 8,192, 19 parts: 5-7 us, a few
+  // lanes a row 15). Few: a few lanes a row (12 answers after 1,500, walks in a few
+  // parts: 7.5 us, a wave a row 11.4).
   if (a.parts > 8) hipLaunchKernelGGL(prefix_fwd_join_kernel<HD>, dim3(joins, BQ / 4), dim3(256), 0, s, a);
   else hipLaunchKernelGGL(prefix_fwd_join_few_kernel<HD>, dim3(joins, BQ * HD / 2048), dim3(256), 0, s, a);
   return hipGetLastError();
