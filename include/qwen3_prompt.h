@@ -102,7 +102,9 @@ gpt2_status qwen3_prefix_forward(const qwen3_prefix* p, const void* d_qkv,
 /* The gradient of d_qkv to d_dqkv (written whole, not d_qkv itself; zero where
  * a prefix has no queries) from d_dout, that of d_out, and the forward's d_qkv,
  * d_out and d_lse. A key's gradient sums over its group's query heads and, in
- * the prefix, over all sequences, in fp32 and in a fixed order. */
+ * the prefix, over all sequences, in fp32 and in a fixed order.
+ * Both: what a token does not see must be finite all the same; infinite or NaN
+ * rows of one sequence can reach its neighbours' (0 times NaN in a product). */
 gpt2_status qwen3_prefix_backward(const qwen3_prefix* p, const void* d_qkv,
                                   const void* d_out, const float* d_lse,
                                   const void* d_dout, void* d_dqkv,
