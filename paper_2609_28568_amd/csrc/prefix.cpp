@@ -210,10 +210,12 @@ std::string prefix_check(const qwen3_prefix_config* c, const int32_t* lens) {
 
 size_t prefix_bytes(const qwen3_prefix_config& c, const int32_t* lens) { return places(c, lay_out(c, lens)).total; }
 
-hipError_t prefix_make(const qwen3_prefix_config& c, const int32_t* lens, void* d_plan, hipStream_t s,
-                       qwen3_prefix* out) {
+hipError_t prefix_make(const qwen3_prefix_config& c, const int32_t* lens, void* d_plan, size_t plan_bytes,
+                       hipStream_t s, qwen3_prefix* out, bool* fits) {
   const Tables t = lay_out(c, lens);
   const Places p = places(c, t);
+  *fits = plan_bytes >= p.total;
+  if (!*fits) return hipErrorInvalidValue;
   char* d = static_cast<char*>(d_plan);
   std::vector<char> host(p.dsum);
   auto put = [&](size_t at, const void* from, size_t bytes) {
@@ -273,10 +275,11 @@ gpt2_status qwen3_prefix_create(const qwen3_prefix_config* cfg, const int32_t* s
     if (!why.empty()) return fail(GPT2_ERR_INVALID_ARG, why.c_str());
     if (!d_plan || !out || reinterpret_cast<uintptr_t>(d_plan) % 256)
       return fail(GPT2_ERR_INVALID_ARG, "d_plan is NULL or not 256-byte aligned, or out is NULL");
-    if (plan_bytes < prefix_bytes(*cfg, seq_lens))
-      return fail(GPT2_ERR_INVALID_ARG, "d_plan is smaller than qwen3_prefix_size says");
     std::unique_ptr<qwen3_prefix> p(new qwen3_prefix());
-    const hipError_t e = prefix_make(*cfg, seq_lens, d_plan, static_cast<hipStream_t>(hip_stream), p.get());
+    bool fits = false;
+    const hipError_t e = prefix_make(*cfg, seq_lens, d_plan, plan_bytes, static_cast<hipStream_t>(hip_stream), p.get(),
+                                     &fits);
+    if (!fits) return fail(GPT2_ERR_INVALID_ARG, "d_plan is smaller than qwen3_prefix_size says");
     if (e != hipSuccess) return fail(GPT2_ERR_DEVICE, hipGetErrorString(e));
     *out = p.release();
     return GPT2_OK;

@@ -382,35 +382,22 @@ __global__ __launch_bounds__(256) void prefix_fwd_join_few_kernel(PrefixArgs a) 
   if (c == 0) a.lse[(size_t)h * a.nq + rq] = (m + log2f(l)) * LN2;
 }
 
-// D = rowsum(dO * O) of every row with a query, HD/8 lanes each; a prefix
-// without queries takes a zero gradient there.
+// The zero gradient of queries that a prefix does not have.
 template <int HD>
-__global__ __launch_bounds__(256) void prefix_dsum_kernel(PrefixArgs a) {
-  constexpr int LANES = HD / 8;
-  const long i = ((long)blockIdx.x * 256 + threadIdx.x) / LANES;
-  const int c = threadIdx.x % LANES * 8, ld = (a.H + 2 * a.Hkv) * HD;
-  if (i >= (long)a.N * a.H) return;
-  const int t = (int)(i / a.H), h = (int)(i % a.H);
-  if (t < a.q0) {
-    *reinterpret_cast<uint4*>(a.dqkv + (size_t)t * ld + h * HD + c) = make_uint4(0, 0, 0, 0);
-    return;
-  }
-  const size_t at = ((size_t)(t - a.q0) * a.H + h) * HD + c;
-  const uint4 d = *reinterpret_cast<const uint4*>(a.dout + at), o = *reinterpret_cast<const uint4*>(a.out + at);
-  float s = lo_f(d.x) * lo_f(o.x) + hi_f(d.x) * hi_f(o.x) + lo_f(d.y) * lo_f(o.y) + hi_f(d.y) * hi_f(o.y);
-  s += lo_f(d.z) * lo_f(o.z) + hi_f(d.z) * hi_f(o.z) + lo_f(d.w) * lo_f(o.w) + hi_f(d.w) * hi_f(o.w);
-#pragma unroll
-  for (int m = LANES / 2; m; m >>= 1) s += __shfl_xor(s, m);
-  if (c == 0) a.dsum[(size_t)h * a.nq + t - a.q0] = s;
+__global__ __launch_bounds__(256) void prefix_zero_kernel(PrefixArgs a) {
+  const int lanes = a.H * (HD / 8);
+  const long i = (long)blockIdx.x * 256 + threadIdx.x;
+  const int t = (int)(i / lanes), c = (int)(i - (long)t * lanes) * 8;
+  if (t < a.q0) *reinterpret_cast<uint4*>(a.dqkv + (size_t)t * (a.H + 2 * a.Hkv) * HD + c) = make_uint4(0, 0, 0, 0);
 }
 
-// D from the bf16 O is off by a rounding of O, which all keys of the row share.
-// Beside the roundings of dS, which average, that counts the more the fewer keys
-// hold the row's weight, so rows of few keys take a first walk that sums D =
-// sum_j P_j dP_j in fp32 and leave it for dK/dV: gradients of 9 ragged answers
-// with 64-wide heads are 2.4e-3 off instead of 2.6e-3, of rows of up to 70 keys
-// 2.4e-3 instead of 2.8e-3 (rounding exact ones 1.7e-3); dQ of the former takes
-// 19 us instead of 14. Longer walks would pay two products more of five for a
+// D = rowsum(dO * O) from the bf16 O is off by a rounding that all keys of the
+// row share. Beside the roundings of dS, which average, that counts the more the
+// fewer keys hold the row's weight, so rows of few keys take a first walk that
+// sums D = sum_j P_j dP_j in fp32: gradients of 9 ragged answers with 64-wide
+// heads are 2.4e-3 off instead of 2.6e-3, of rows of up to 70 keys 2.4e-3
+// instead of 2.8e-3 (rounding exact ones 1.7e-3); dQ of the former takes 18 us
+// instead of 14. Longer walks would pay two products more of five for a
 // difference of a few per cent.
 constexpr int EXACT_TILES = 8;
 
@@ -508,10 +495,18 @@ __global__ __launch_bounds__(256 * GR, GR == 1 ? 2 : 1) void prefix_dq_kernel(Pr
   if (exact) {
     dsum = walk_d<HD, GR>(a, keys, r, w.it.tiles, qf, df, sc, lse2, (lds_char_t*)smem_raw, wave, group, lane);
     if (w.it.f0 + group < w.it.f1) keys.issue(w.it.f0 + group, smem, wave, lane);
-    if (w.it.f0 == 0 && group == 0 && r.on && g == 0) a.dsum[d_at] = dsum;
   } else {
-    dsum = a.dsum[d_at];
+    const bf16_t* out = a.out + ((size_t)r.rq * a.H + r.h) * HD;
+    dsum = 0.0f;
+#pragma unroll
+    for (int s = 0; s < S::KS; ++s) {
+      const uint4 o = *reinterpret_cast<const uint4*>(out + 16 * s + 8 * g), d = __builtin_bit_cast(uint4, df[s]);
+      dsum += lo_f(d.x) * lo_f(o.x) + hi_f(d.x) * hi_f(o.x) + lo_f(d.y) * lo_f(o.y) + hi_f(d.y) * hi_f(o.y);
+      dsum += lo_f(d.z) * lo_f(o.z) + hi_f(d.z) * hi_f(o.z) + lo_f(d.w) * lo_f(o.w) + hi_f(d.w) * hi_f(o.w);
+    }
+    dsum = sum32(dsum);
   }
+  if (w.it.f0 == 0 && group == 0 && r.on && g == 0) a.dsum[d_at] = dsum;   // for dK/dV
   floatx16 dq[S::DT];
 #pragma unroll
   for (int d = 0; d < S::DT; ++d) zero(dq[d]);
@@ -820,8 +815,8 @@ hipError_t fwd_t(const PrefixArgs& a, hipStream_t s) {
 
 template <int HD>
 hipError_t bwd_t(const PrefixArgs& a, hipStream_t s) {
-  const long lanes = (long)a.N * a.H * (HD / 8);
-  hipLaunchKernelGGL(prefix_dsum_kernel<HD>, dim3((unsigned)((lanes + 255) / 256)), dim3(256), 0, s, a);
+  const long zeros = (long)a.q0 * a.H * (HD / 8);
+  if (zeros) hipLaunchKernelGGL(prefix_zero_kernel<HD>, dim3((unsigned)((zeros + 255) / 256)), dim3(256), 0, s, a);
   const unsigned wgs = a.nitems * a.Hkv;
   if (wgs <= 256) hipLaunchKernelGGL((prefix_dq_kernel<HD, 2>), dim3(wgs), dim3(512), 0, s, a);
   else hipLaunchKernelGGL((prefix_dq_kernel<HD, 1>), dim3(wgs), dim3(256), 0, s, a);
