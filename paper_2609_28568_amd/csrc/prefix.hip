@@ -22,7 +22,7 @@
 // Measured: 16 sequences of 256 over a prefix of 2048, 16 + 8 heads of 128:
 // forward 127-130 us (700 TFLOP/s), dQ 170-194 (700-790), dK/dV 230-246 + 11
 // (750); waves wait on their own chain of products, exponentials and products. 64
-// single tokens after 8192: 18 + 5 us, 34 MB of keys and values and 12 MB of
+// single tokens after 8192: 18 + 5 us, 34 MB of keys and values and 10 MB of
 // partial results.
 //
 // The tile arithmetic is attention.hip's: S^T = K Q^T with one row per lane,
