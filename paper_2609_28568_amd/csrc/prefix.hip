@@ -545,9 +545,10 @@ __global__ __launch_bounds__(256 * GR, GR == 1 ? 2 : 1) void prefix_dq_kernel(Pr
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          float pv = fast_exp2(p[e] * sc - lse2);
-          if constexpr (decltype(masked)::value) pv = acc_row(e, 0) >= lo && acc_row(e, 0) <= hi ? pv : 0.0f;
-          ds[t][e] = pv * (ds[t][e] - dsum);
+          float x = fast_exp2(p[e] * sc - lse2) * (ds[t][e] - dsum);
+          // the product goes, not a factor: dO V of a key that is not seen may be infinite
+          if constexpr (decltype(masked)::value) x = acc_row(e, 0) >= lo && acc_row(e, 0) <= hi ? x : 0.0f;
+          ds[t][e] = x;
         }
       };
       if (see == SOME) probs(std::true_type{});

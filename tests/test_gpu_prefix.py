@@ -350,3 +350,30 @@ def test_refusals_of_the_step():
     with pytest.raises(binding.LibError, match="B = 1"):
         two.set_layout(96, [96])
     two.close()
+
+
+@pytest.mark.parametrize("name,seq", [("answers", 1), ("answers_hd64", 0), ("long_walks_hd64", 1), ("known_prefix", 1),
+                                      ("many_items_wide", 0)])
+def test_gradients_of_a_sequence_do_not_read_the_others(name, seq):
+    """As above for the backward: values whose products with a gradient of
+    order 1 leave fp32's range reach no other sequence's gradients. The prefix'
+    keys see every sequence, so theirs do depend on it."""
+    qkv, dout, (H, Hkv, hd, P, lens, q0) = inputs(name)
+    dout = synth.round_to_bf16(dout * np.float32(100))
+    lo = P + sum(lens[:seq])
+    hi = lo + lens[seq]
+    other = qkv.copy()
+    other[lo:hi] = 3e38
+    p, g = plan(name), dev(dout)
+    got = []
+    for x in (dev(qkv), dev(other)):
+        y, l = p.forward(x)
+        got.append((y, l, p.backward(g, x, y, l)))
+    (y, l, d), (y2, l2, d2) = got
+    rows = np.r_[0:lo, hi:P + sum(lens)]
+    seen = rows[rows >= q0] - q0
+    assert torch.equal(y[seen], y2[seen]) and torch.equal(l[:, seen], l2[:, seen])
+    own = rows[rows >= P]
+    assert torch.isfinite(d2[own]).all() and torch.equal(d[own], d2[own])
+    dq = slice(0, H * hd)
+    assert torch.isfinite(d2[rows][:, dq]).all() and torch.equal(d[rows][:, dq], d2[rows][:, dq])
