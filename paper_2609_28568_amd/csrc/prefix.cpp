@@ -201,6 +201,8 @@ std::string prefix_check(const qwen3_prefix_config* c, const int32_t* lens) {
   for (int i = 0; i < c->n_seq; ++i) {
     if (lens[i] < 0) return "a sequence's length is negative";
     n += lens[i];
+    // far more than the 32-bit offsets reach, and the sum and the bytes below stay within 64 bits
+    if (n >= (1l << 32)) return "the rows of q|k|v exceed 32-bit offsets";
   }
   if (n - (c->prefix_queries ? 0 : c->prefix_len) < 1) return "no token has a query";
   if ((n + 2 * ROWS) * (c->n_head + 2 * c->n_kv_head) * c->head_dim * 2 >= (1l << 32))

@@ -168,3 +168,10 @@ def test_prefix_refuses_arguments():
     n = ctypes.c_size_t()
     assert L.qwen3_layout_size(None, 1, 1, lens, ctypes.byref(n)) == INVALID
     assert L.qwen3_set_layout(None, 1, 1, lens, None, 0) == INVALID
+
+
+@pytest.mark.parametrize("n_seq", [1500, 3000, 5000, 600000])
+def test_prefix_refuses_lengths_whose_bytes_pass_64_bits(n_seq):
+    """Sums of lengths whose bytes wrap around 64 bits, to either sign."""
+    st, _ = prefix_size([2 ** 31 - 1] * n_seq, n_head=4096, n_kv_head=4096, prefix_len=0)
+    assert st == INVALID and "32-bit" in qb.lib().qwen3_last_error(None).decode()
