@@ -183,6 +183,14 @@ def on_stream(device, fn, *args):
         return fn(*args, stream)
 
 
+def stream_buffer(nbytes, device, stream):
+    """A uint8 tensor that work on `stream` may write at once: memory of its
+    pool, which no other stream's pending work still holds."""
+    import torch
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
 def orthogonalise(x, iterations=5, out=None, workspace=None):
     """Newton-Schulz orthogonalisation of one fp32 matrix [rows, cols] or a
     batch [count, rows, cols] (gpt2_orthogonalise) on the current stream of
@@ -313,8 +321,7 @@ class GPT2:
         if getattr(self, "muon_workspace", None) is None:
             n = ctypes.c_size_t()
             _check(self.L.gpt2_muon_size(ctypes.byref(self.cfg), ctypes.byref(n)))
-            self.muon_workspace = self.torch.empty(n.value, dtype=self.torch.uint8, device=self.device)
-            self.muon_workspace.record_stream(self.stream)
+            self.muon_workspace = stream_buffer(n.value, self.device, self.stream)
         lr = ctypes.c_float()
         how = Muon(float(momentum), int(bool(nesterov)), int(iterations), float(scale))
         _check(self.L.gpt2_muon_step(self.handle, int(step), ctypes.byref(how), self.muon_workspace.data_ptr(),

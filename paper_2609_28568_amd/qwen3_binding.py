@@ -13,7 +13,7 @@ import functools
 
 import numpy as np
 
-from .binding import LibError, Muon, lib as _lib_gpt2, on_stream
+from .binding import LibError, Muon, lib as _lib_gpt2, on_stream, stream_buffer
 
 RP = 64   # padded adapter rank of the library
 # kernel classes of the timing probes (QWEN3_K_* in include/qwen3.h)
@@ -433,14 +433,19 @@ class Qwen3:
 
     def set_positions(self, positions=None, sections=(64,), interleaved=False):
         """Positions int32 [axes, B*T] of the tokens from the next forward on,
-        with the pairs per axis (qwen3_set_positions); None: the default."""
+        with the pairs per axis (qwen3_set_positions); None: the default. What
+        the current stream has enqueued is done before the model reads them."""
         if positions is not None:
             _device_rows(positions, "positions", self.torch.int32, self.bufs["workspace"],
                          (len(sections), self.cfg.B * self.cfg.T))
         sec = (ctypes.c_int32 * len(sections))(*sections)
         _check(lib().qwen3_set_positions(self.h, _ptr(positions), len(sections), sec, int(bool(interleaved))), self.h)
         if positions is not None:
-            positions.record_stream(self.stream)   # read there, whichever stream it was made on
+            # the model's stream reads them: after what the current one has to do with them, and before they are freed
+            now = self.torch.cuda.current_stream(positions.device)
+            if now != self.stream:
+                self.stream.wait_stream(now)
+            positions.record_stream(self.stream)
         self._positions = positions
 
     def set_layout(self, prefix_len=0, seq_lens=None):
@@ -454,9 +459,8 @@ class Qwen3:
         c_lens = (ctypes.c_int32 * len(lens))(*lens)
         n = ctypes.c_size_t()
         _check(lib().qwen3_layout_size(self.h, prefix_len, len(lens), c_lens, ctypes.byref(n)), self.h)
-        plan = self.torch.empty(n.value, dtype=self.torch.uint8, device=self.bufs["workspace"].device)
+        plan = stream_buffer(n.value, self.bufs["workspace"].device, self.stream)
         _check(lib().qwen3_set_layout(self.h, prefix_len, len(lens), c_lens, plan.data_ptr(), n.value), self.h)
-        plan.record_stream(self.stream)
         self._plan = plan
 
     def muon_step(self, norm_out=None, momentum=0.95, nesterov=True, iterations=5, scale=0.2):
@@ -466,9 +470,7 @@ class Qwen3:
         if getattr(self, "muon_workspace", None) is None:
             n = ctypes.c_size_t()
             _check(lib().qwen3_muon_size(ctypes.byref(self.cfg), ctypes.byref(n)))
-            self.muon_workspace = self.torch.empty(n.value, dtype=self.torch.uint8,
-                                                   device=self.bufs["workspace"].device)
-            self.muon_workspace.record_stream(self.stream)
+            self.muon_workspace = stream_buffer(n.value, self.bufs["workspace"].device, self.stream)
         how = Muon(float(momentum), int(bool(nesterov)), int(iterations), float(scale))
         _check(lib().qwen3_muon_step(self.h, ctypes.byref(how), self.muon_workspace.data_ptr(),
                                      self.muon_workspace.numel(),

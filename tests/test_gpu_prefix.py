@@ -377,3 +377,42 @@ def test_gradients_of_a_sequence_do_not_read_the_others(name, seq):
     assert torch.isfinite(d2[own]).all() and torch.equal(d[own], d2[own])
     dq = slice(0, H * hd)
     assert torch.isfinite(d2[rows][:, dq]).all() and torch.equal(d[rows][:, dq], d2[rows][:, dq])
+
+
+def test_step_set_up_with_another_stream_current():
+    """Layout, positions and the update's workspace asked for while another
+    stream is current and busy: the memory that stream's pool has free is still
+    being written there, and the positions are not made yet."""
+    from paper_2609_28568_amd import qwen3_binding as qb
+    P, lens = 60, [50, 31, 51]
+    w = dict(synth.QWEN3_WORKLOADS["qwen3_tiny"], B=1, T=192, max_seq_len=192)
+    base, lora = synth.init_qwen3(w, seed=51, b_std=0.02)
+    ids, tgt = (torch.from_numpy(a) for a in synth.token_batch(w, seed=52))
+    axes = torch.randint(0, 300, (2, 192), dtype=torch.int32, device="cuda")
+    side, got = torch.cuda.Stream(), []
+    for busy in (False, True):
+        m = qb.Qwen3(qb.make_config(w, synth.QWEN3_OPTIM))
+        m.set_base(base)
+        m.set_lora(lora)
+        m.forward(ids, tgt)
+        m.backward()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side if busy else torch.cuda.current_stream()):
+            if busy:
+                sizes = (got[0][3], got[0][4])
+                blocks = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes]
+                torch.cuda._sleep(10 ** 7)
+                for b in blocks:
+                    b.fill_(255)
+                del blocks, b
+            pos = axes.clone()
+            m.set_layout(P, lens)
+            m.set_positions(pos, (30, 34))
+            m.muon_step()
+        m.forward(ids, tgt)
+        m.backward()
+        got.append((m.loss(), m.adapters("lora_grads"), m.adapters(), m._plan.numel(), m.muon_workspace.numel()))
+        m.close()
+    assert got[0][0] == got[1][0]
+    for k in got[0][1]:
+        assert np.array_equal(got[0][1][k], got[1][1][k]) and np.array_equal(got[0][2][k], got[1][2][k]), k

@@ -175,3 +175,72 @@ def test_prefix_refuses_lengths_whose_bytes_pass_64_bits(n_seq):
     """Sums of lengths whose bytes wrap around 64 bits, to either sign."""
     st, _ = prefix_size([2 ** 31 - 1] * n_seq, n_head=4096, n_kv_head=4096, prefix_len=0)
     assert st == INVALID and "32-bit" in qb.lib().qwen3_last_error(None).decode()
+
+
+# ---- buffers of a model used with another stream current
+
+class _Library:
+    """Accepts every call."""
+    def __getattr__(self, name):
+        return lambda *args: 0
+
+
+class _Stream:
+    def __init__(self, name):
+        self.name, self.waited = name, []
+
+    def wait_stream(self, other):
+        self.waited.append(other.name)
+
+
+@pytest.fixture
+def streams(monkeypatch):
+    """(torch, model's stream, list of (stream current at the allocation)): a side stream is current."""
+    import contextlib
+    torch = pytest.importorskip("torch")
+    current, made = [_Stream("side")], []
+
+    @contextlib.contextmanager
+    def on(s):
+        current.append(s)
+        yield
+        current.pop()
+
+    empty = torch.empty
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: current[-1])
+    monkeypatch.setattr(torch, "empty", lambda *a, **kw: made.append(current[-1].name) or empty(*a, **kw))
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda self, s: None)
+    monkeypatch.setattr(qb, "lib", _Library)
+    return torch, _Stream("model"), made
+
+
+def _bare_qwen3(torch, stream):
+    m = qb.Qwen3.__new__(qb.Qwen3)
+    m.torch, m.stream, m.h, m.bufs = torch, stream, None, {"workspace": torch.zeros(1, dtype=torch.uint8)}
+    m.cfg = qb.make_config(synth.QWEN3_WORKLOADS["qwen3_tiny"], synth.QWEN3_OPTIM)
+    m._positions = m._plan = m._in_use = None
+    return m
+
+
+def test_buffers_of_a_step_come_from_the_models_stream(streams):
+    """The library writes them there at once: memory of another stream's pool
+    may still be in that stream's use."""
+    torch, stream, made = streams
+    m = _bare_qwen3(torch, stream)
+    m.set_layout(5, [3, 4])
+    m.muon_step()
+    g = binding.GPT2.__new__(binding.GPT2)
+    g.torch, g.stream, g.handle, g.L, g.device = torch, stream, None, _Library(), torch.device("cpu")
+    g.cfg = binding.make_config(workload("tiny"), synth.OPTIM)
+    g.muon_step(0)
+    assert made == ["model"] * 3
+
+
+def test_positions_are_read_after_the_stream_that_made_them(streams):
+    torch, stream, _ = streams
+    m = _bare_qwen3(torch, stream)
+    m.set_positions(torch.zeros(1, m.cfg.B * m.cfg.T, dtype=torch.int32))
+    assert stream.waited == ["side"]
+    m.set_positions(None)
+    assert stream.waited == ["side"]
