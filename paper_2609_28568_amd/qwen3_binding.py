@@ -13,7 +13,7 @@ import functools
 
 import numpy as np
 
-from .binding import LibError, Muon, lib as _lib_gpt2, on_stream, stream_buffer
+from .binding import GPT2_ERR_INVALID_ARG, LibError, Muon, lib as _lib_gpt2, on_stream, stream_buffer
 
 RP = 64   # padded adapter rank of the library
 # kernel classes of the timing probes (QWEN3_K_* in include/qwen3.h)
@@ -417,12 +417,15 @@ class Qwen3:
 
     def forward(self, ids, targets=None):
         torch = self.torch
-        # a backward takes its forward's positions and layout, whatever is set in between
-        self._in_use = (self._positions, self._plan)
         self._ids = ids.to(torch.int32).cuda().contiguous()
         self._tgt = None if targets is None else targets.to(torch.int32).cuda().contiguous()
-        _check(lib().qwen3_forward(self.h, ctypes.c_void_p(self._ids.data_ptr()),
-                                   ctypes.c_void_p(self._tgt.data_ptr() if self._tgt is not None else 0)), self.h)
+        status = lib().qwen3_forward(self.h, ctypes.c_void_p(self._ids.data_ptr()),
+                                     ctypes.c_void_p(self._tgt.data_ptr() if self._tgt is not None else 0))
+        if status != GPT2_ERR_INVALID_ARG:
+            # a backward takes its forward's positions and layout, whatever is set in between; those
+            # of the forward before stay where this one is refused
+            self._in_use = (self._positions, self._plan)
+        _check(status, self.h)
 
     def backward(self):
         _check(lib().qwen3_backward(self.h), self.h)

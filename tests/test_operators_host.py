@@ -244,3 +244,29 @@ def test_positions_are_read_after_the_stream_that_made_them(streams):
     assert stream.waited == ["side"]
     m.set_positions(None)
     assert stream.waited == ["side"]
+
+
+def test_a_forward_that_is_refused_keeps_the_last_ones_layout(streams, monkeypatch):
+    """A backward may still follow the forward before it, and reads that one's
+    positions and layout: they stay allocated."""
+    torch, stream, _ = streams
+    monkeypatch.setattr(torch.Tensor, "cuda", lambda self: self)
+    m = _bare_qwen3(torch, stream)
+    ids = torch.zeros(1, 192, dtype=torch.int64)
+    m.set_layout(100, [92])
+    first = m._plan
+    m.forward(ids, ids)
+    m.set_layout(90, [102])
+    with pytest.raises(AttributeError):
+        m.forward("not a tensor")
+    assert m._in_use[1] is first
+    refuse = _Library()
+    refuse.qwen3_forward = lambda *args: INVALID
+    refuse.qwen3_last_error = lambda h: b"refused"
+    monkeypatch.setattr(qb, "lib", lambda: refuse)
+    with pytest.raises(binding.LibError):
+        m.forward(ids, ids)
+    assert m._in_use[1] is first
+    monkeypatch.setattr(qb, "lib", _Library)
+    m.forward(ids, ids)
+    assert m._in_use[1] is m._plan is not first
