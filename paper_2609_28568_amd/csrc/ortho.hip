@@ -909,9 +909,11 @@ long align128(long n) { return (n + 127) / 128 * 128; }
 }  // namespace
 
 // Offsets of every group's planes (fp16 elements), after the partial sums;
-// returns the bytes in all, or 0 when a shape is out of range.
+// returns the bytes in all, or 0 when a shape is out of range. Matrices that
+// stay in LDS use neither; a nominal 256 bytes for each tile of one of them keep
+// a size telling their shapes apart.
 size_t ortho_layout(OrthoGroup* g, int ngroups) {
-  long mats = 0, tiles = 0;
+  long mats = 0, tiles = 0, large = 0, nominal = 0;
   for (int k = 0; k < ngroups; ++k) {
     OrthoGroup& q = g[k];
     if (q.rows < 1 || q.cols < 1 || q.count < 1) return 0;
@@ -925,10 +927,13 @@ size_t ortho_layout(OrthoGroup* g, int ngroups) {
     tiles += mp * np / (PAD * PAD) * q.count;
     // launches of less than 2^32 threads
     if (mats * ORTHO_PARTS * 256 >= (1L << 32) || tiles * 256 >= (1L << 32)) return 0;
+    if (is_small(q)) nominal += mp * np / (PAD * PAD) * 128;
+    else large += q.count;
   }
-  long o = align128(mats * ORTHO_PARTS * (long)(sizeof(double) / 2));
+  long o = align128(large * ORTHO_PARTS * (long)(sizeof(double) / 2)) + nominal;
   for (int k = 0; k < ngroups; ++k) {
     OrthoGroup& q = g[k];
+    if (is_small(q)) continue;
     const long xn = align128((long)q.count * 2 * q.mp * q.np), an = align128((long)q.count * 2 * q.mp * q.mp);
     q.x_off[0] = o; o += xn;
     q.x_off[1] = o; o += xn;

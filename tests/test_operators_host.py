@@ -270,3 +270,28 @@ def test_a_forward_that_is_refused_keeps_the_last_ones_layout(streams, monkeypat
     monkeypatch.setattr(qb, "lib", _Library)
     m.forward(ids, ids)
     assert m._in_use[1] is m._plan is not first
+
+
+# ---- workspace of matrices that a workgroup holds in LDS
+
+@pytest.mark.parametrize("rows,cols", [(16, 16), (16, 1024), (128, 128), (64, 256), (1024, 32)])
+def test_matrices_that_stay_in_lds_take_no_planes(rows, cols):
+    """The size does not grow with their number, and is small against one of them."""
+    one = binding.orthogonalise_size(rows, cols, 1)
+    assert 0 < one == binding.orthogonalise_size(rows, cols, 100000) <= max(256, rows * cols)
+
+
+def test_muon_size_leaves_out_the_small_adapters():
+    """Ranks and widths of the small test model: everything stays in LDS but
+    what its width forbids, whose planes are counted."""
+    n = ctypes.c_size_t()
+    w = dict(synth.QWEN3_WORKLOADS["qwen3_tiny"], lora_rank=8)
+    q = qb.make_config(w, synth.QWEN3_OPTIM)
+    assert qb.lib().qwen3_muon_size(ctypes.byref(q), ctypes.byref(n)) == 0
+    assert n.value < 64 << 10
+    # rank 32 and 1,280 rows of gate and up: past what LDS holds
+    q = qb.make_config(dict(w, lora_rank=32, d_ff=1280), synth.QWEN3_OPTIM)
+    assert qb.lib().qwen3_muon_size(ctypes.byref(q), ctypes.byref(n)) == 0
+    L = w["n_layer"]
+    # two matrices a layer of gate and up's B and one of down's A: four planes of X and of the Gram size, 64 rows padded
+    assert 3 * L * 8 * 64 * (1280 + 64) <= n.value < 3 * L * 8 * 64 * (1280 + 64) + (64 << 10)
