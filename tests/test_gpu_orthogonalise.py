@@ -231,3 +231,59 @@ def test_qwen3_muon_step(rank):
         assert all(np.all(a.reshape(a.shape[0], -1, qb.RP, a.shape[2])[:, :, r:] == 0)
                    for n, a in packed.items() if n.endswith("_A"))
     m.close()
+
+
+# 192-wide tiles for A and P (odd sides in the last ones), and for X of tall
+# matrices; long contractions of few tiles for X, and for A and P
+@pytest.mark.parametrize("count,rows,cols", [(12, 1100, 1100), (12, 1152, 1090), (21, 760, 570), (4, 1500, 1500),
+                                             (1, 2030, 2040), (1, 2200, 2100)])
+def test_large_tiles_against_the_definition(count, rows, cols):
+    from paper_2609_28568_amd import binding
+    print(f"orthogonalise {count} x {rows} x {cols}", flush=True)
+    x = batch(count, rows, cols, 11)
+    y = binding.orthogonalise(torch.from_numpy(x).cuda()).cpu().numpy()
+    for i in {0, count - 1}:
+        assert rel_l2(y[i], newton_schulz(x[i])) < TOL, i
+
+
+@pytest.mark.parametrize("shape", [dict(n_layer=12, d_model=768, n_head=12, d_ff=3072),
+                                   dict(n_layer=2, d_model=640, n_head=10, d_ff=2560)])
+def test_gpt2_muon_step_of_real_widths(shape):
+    """Square, tall and wide matrices together on the update's 192- and 128-wide
+    tiles, one step from a momentum that is not zero; a few matrices against 64
+    bits, every weight's bf16 copy, and the momenta."""
+    from paper_2609_28568_amd import binding
+    w = workload("tiny", **shape)
+    opt = dict(synth.OPTIM, lr_max=0.05, warmup_steps=1, grad_clip=0.5)
+    m = binding.GPT2(binding.make_config(w, opt), seed=3)
+    m.forward(*(torch.from_numpy(a) for a in synth.token_batch(w)))
+    m.backward()
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    m.flat("grads").copy_(torch.randn(m.n_params, generator=gen, device="cuda") * 1e-3)
+    m.flat("m").copy_(torch.randn(m.n_params, generator=gen, device="cuda") * 1e-3)
+    before, grads, mom = m.to_dict(), m.to_dict("grads"), m.to_dict("m")
+    lr = m.muon_step(0, momentum=0.9)
+    torch.cuda.synchronize()
+    after, mom2 = m.to_dict(), m.to_dict("m")
+    total = np.sqrt(sum((g.astype(np.float64) ** 2).sum() for g in grads.values()))
+    coef = min(1.0, 0.5 / total)
+    bf = m.flat_bf16().float().cpu().numpy()
+    last = shape["n_layer"] - 1
+    for kind, parts, which in (("qkvw", 3, [(0, 1), (last, 2)]), ("attprojw", 1, [(last, 0)]),
+                               ("fcw", 1, [(0, 0), (last, 0)]), ("fcprojw", 1, [(0, 0), (last, 0)])):
+        rows = before[kind].shape[1] // parts
+        for l, j in which:
+            at = (l, slice(j * rows, (j + 1) * rows))
+            ref, new = muon(before[kind][at].astype(np.float64), grads[kind][at], mom[kind][at].astype(np.float64),
+                            coef, lr, 0.1, 0.9, True, 0.2)
+            step = ref - before[kind][at]
+            err = np.linalg.norm(after[kind][at] - before[kind][at] - step)
+            assert err < 2 * TOL * np.linalg.norm(step) + 2.0 ** -24 * np.linalg.norm(ref), (kind, l, j)
+        # two fp32 roundings of terms no larger than the sum of their sizes, and the clip coefficient's own
+        size = 0.9 * np.abs(mom[kind]) + coef * np.abs(grads[kind])
+        new = 0.9 * mom[kind].astype(np.float64) + coef * grads[kind].astype(np.float64)
+        assert np.all(np.abs(mom2[kind] - new) <= 2.0 ** -20 * size), kind
+        off, _ = m.kinds[kind]
+        n = after[kind].size
+        assert np.array_equal(bf[off:off + n], synth.round_to_bf16(after[kind]).ravel()), kind
+    m.close()
