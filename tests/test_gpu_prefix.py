@@ -416,3 +416,19 @@ def test_step_set_up_with_another_stream_current():
     assert got[0][0] == got[1][0]
     for k in got[0][1]:
         assert np.array_equal(got[0][1][k], got[1][1][k]) and np.array_equal(got[0][2][k], got[1][2][k]), k
+
+
+CASES.update({
+    # short walks on more workgroups than CUs
+    "many_short_walks": (16, 16, 64, 0, [64, 63, 1, 70] * 14, True),
+    "many_short_walks_wide": (16, 16, 128, 3, [64, 63, 1, 70] * 14, True),
+    # groups of heads that leave a block of rows inside a token, or make up two
+    "groups_of_48": (48, 1, 128, 33, [2, 0, 1, 7], False),
+    "groups_of_256": (256, 1, 64, 70, [5, 3], True),
+    "groups_of_three_wide": (6, 2, 128, 129, [1, 64, 66], True),
+})
+
+
+@pytest.mark.parametrize("name", list(CASES)[-5:])
+def test_short_walks_and_large_groups(name):
+    test_against_the_definition(name)
