@@ -896,9 +896,11 @@ hipError_t product(const Params& p, hipStream_t s) {
   // computes less: with tiles of 128 two workgroups share one.
   const long cost128 = ((t128 + 511) / 512 * 2 - (t128 % 512 > 0 && t128 % 512 <= 256)) * 128 * 128;
   const long cost192 = (t192 + 255) / 256 * 192 * 192;
+  const bool few_long = t128 <= 256 && steps >= 2048;
   if (t128 < 144) L(64, 4);
-  else if (t128 <= 256 && steps >= 2048) L(128, 3);
   else if (t128 > 256 && cost192 < cost128) L(192, 2);
+  else if constexpr (PH == LAST_UPDATE) L(128, 2);   // the steps' blocks of width 2048 have 1,024 tiles and more
+  else if (few_long) L(128, 3);
   else L(128, 2);
 #undef L
   return hipGetLastError();
