@@ -432,3 +432,50 @@ CASES.update({
 @pytest.mark.parametrize("name", list(CASES)[-5:])
 def test_short_walks_and_large_groups(name):
     test_against_the_definition(name)
+
+
+def test_millions_of_single_tokens():
+    """More rows than the division of walks is estimated for; the prefix' keys
+    sum their gradients over all of them. Tolerances as above, and fp32 sums of
+    up to 700 partial sums (540 products of 16 a workgroup, 130 workgroups):
+    2^-24 700 < 2^-14 of the sum of absolute values."""
+    from paper_2609_28568_amd import qwen3_binding as qb
+    P, n, hd = 100, 2200000, 64
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(P + n, 3 * hd, generator=gen, device="cuda")
+    x[:, :2 * hd] *= 1.4
+    x, g = x.bfloat16(), (torch.randn(n, hd, generator=gen, device="cuda") * 1e-2).bfloat16()
+    p = qb.SharedPrefix(1, 1, hd, P, [1] * n, prefix_queries=False)
+    y, lse = p.forward(x)
+    dx = p.backward(g, x, y, lse).double()
+    del p
+    q, do = x[P:, :hd].double(), g.double()
+    kp, vp = x[:P, hd:2 * hd].double(), x[:P, 2 * hd:].double()
+    k, v = x[P:, hd:2 * hd].double(), x[P:, 2 * hd:].double()
+    s = torch.cat([q @ kp.T.contiguous(), (q * k).sum(1, keepdim=True)], 1) / hd ** 0.5
+    ref = torch.logsumexp(s, 1)
+    pr = torch.exp(s - ref[:, None])
+    del s
+    assert (lse[0].double() - ref).abs().max() <= 2.0 ** -18 * (1 + ref.abs().max())
+    pp, ps = pr[:, :P].contiguous(), pr[:, P:]
+    out, mass = pp @ vp + ps * v, pp @ vp.abs() + ps * v.abs()
+    e_out = R * (out.abs() + mass) + 2.0 ** -15 * mass
+    assert ((y.double() - out).abs() <= e_out).all()
+    del mass
+    noise = (do.abs() * e_out).sum(1, keepdim=True)
+    D = (do * out).sum(1, keepdim=True)
+    del out, e_out
+    rest = R + 2.0 ** -14
+    dv, e_dv = pp.T @ do, rest * (pp.T @ do.abs())
+    assert ((dx[:P, 2 * hd:] - dv).abs() <= e_dv + R * dv.abs()).all()
+    assert ((dx[P:, 2 * hd:] - ps * do).abs() <= 2 * R * (ps * do).abs() + 2.0 ** -15 * do.abs()).all()
+    ds = pp * (do @ vp.T.contiguous() - D)
+    e_ds = rest * ds.abs() + pp * (noise + 2.0 ** -15 * (do.abs() @ vp.abs().T.contiguous()))
+    dk, e_dk = ds.T @ q / hd ** 0.5, e_ds.T @ q.abs() / hd ** 0.5
+    assert ((dx[:P, hd:2 * hd] - dk).abs() <= e_dk + R * dk.abs()).all()
+    dss = ps * ((do * v).sum(1, keepdim=True) - D)
+    e_dss = rest * dss.abs() + ps * (noise + 2.0 ** -15 * (do.abs() * v.abs()).sum(1, keepdim=True))
+    dq = (ds @ kp + dss * k) / hd ** 0.5
+    e_dq = (e_ds @ kp.abs() + e_dss * k.abs()) / hd ** 0.5
+    assert ((dx[P:, :hd] - dq).abs() <= e_dq + R * dq.abs()).all()
+    assert (dx[:P, :hd] == 0).all()

@@ -295,3 +295,12 @@ def test_muon_size_leaves_out_the_small_adapters():
     L = w["n_layer"]
     # two matrices a layer of gate and up's B and one of down's A: four planes of X and of the Gram size, 64 rows padded
     assert 3 * L * 8 * 64 * (1280 + 64) <= n.value < 3 * L * 8 * 64 * (1280 + 64) + (64 << 10)
+
+
+def test_a_long_walk_is_shared_out_among_many_short_ones():
+    """2.2 million sequences of one token: the walk of the prefix' keys over all
+    of them is 34,375 tiles beside 17,188 walks of two or three."""
+    n = 2200000
+    st, size = prefix_size([1] * n, n_head=1, n_kv_head=1, head_dim=64, prefix_queries=0)
+    # tables and the backward's D, 16 bytes a token, and the partial results of 64 workgroups or more
+    assert st == 0 and size >= 16 * n + 64 * 2 * 128 * 64 * 4
