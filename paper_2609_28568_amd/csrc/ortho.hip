@@ -92,8 +92,9 @@ DEV int first_matrix(const Params& p, const OrthoGroup& g) {
 
 DEV float update_of(float g, float m_new, float mu, int nesterov) { return nesterov ? fmaf(mu, m_new, g) : m_new; }
 
-// Multiplication by s / sqrt(sum), whatever the range of the sum: a factor in
-// [0.5, 1) in fp32 and a power of two. 0 for no sum (a matrix of zeros).
+// Multiplication by s / sqrt(sum), whatever the range of the sum: a power of
+// two, which brings subnormal numbers up whole, and a factor in [0.5, 1) in
+// fp32. 0 for no sum (a matrix of zeros).
 struct Scale {
   float f;
   int e;
@@ -102,7 +103,7 @@ struct Scale {
     f = (float)__builtin_amdgcn_frexp_mant(inv);
     e = __builtin_amdgcn_frexp_exp(inv);
   }
-  DEV float operator()(float v) const { return __builtin_amdgcn_ldexpf(v * f, e); }
+  DEV float operator()(float v) const { return __builtin_amdgcn_ldexpf(v, e) * f; }
 };
 
 // Sum of squares of each matrix in fp64, ORTHO_PARTS partial sums. With

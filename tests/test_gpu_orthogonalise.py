@@ -287,3 +287,14 @@ def test_gpt2_muon_step_of_real_widths(shape):
         n = after[kind].size
         assert np.array_equal(bf[off:off + n], synth.round_to_bf16(after[kind]).ravel()), kind
     m.close()
+
+
+@pytest.mark.parametrize("rows,cols", [(40, 66), (140, 270)])
+@pytest.mark.parametrize("scale", [1e-42, 3e-40])
+def test_subnormal_matrices(scale, rows, cols):
+    """Whatever bits such numbers have are kept: the input is exact as it is."""
+    from paper_2609_28568_amd import binding
+    x = batch(1, rows, cols, 12, scale)
+    assert np.count_nonzero(x) > 0.9 * x.size and np.abs(x).max() < 2.0 ** -126
+    y = binding.orthogonalise(torch.from_numpy(x).cuda()).cpu().numpy()
+    assert rel_l2(y[0], newton_schulz(x[0])) < TOL
