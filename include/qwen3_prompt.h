@@ -36,11 +36,11 @@ typedef struct qwen3_rotary {
  * [n_kv_head * head_dim] | v likewise, 16-byte aligned. d_positions: int32
  * [n_axes, n_tokens], any values. d_q_norm, d_k_norm: bf16 [head_dim] gains of
  * the RMSNorm of every query and key head before the turn, 16-byte aligned, or
- * both NULL for none. Values pass through; d_out may be d_qkv. Angles are in
- * fp64, all else in fp32, the result rounded once.
+ * both NULL for none. Values pass through; d_out may be d_qkv, and overlaps it
+ * in no other way. Angles are in fp64, all else in fp32, the result rounded once.
  * qwen3_rotary_backward: from d_dout (the gradient of d_out) and the same
  * d_qkv, positions and gains, the gradient of d_qkv to d_dqkv, which may be
- * d_dout. The gains are frozen; without them d_qkv is not read and may be
+ * d_dout or d_qkv and overlaps them in no other way. The gains are frozen; without them d_qkv is not read and may be
  * NULL. INVALID_ARG for what is not as said here; nothing is launched then,
  * nor for n_tokens 0. */
 gpt2_status qwen3_rotary_forward(const qwen3_rotary* r, const void* d_qkv,
@@ -96,11 +96,12 @@ gpt2_status qwen3_prefix_create(const qwen3_prefix_config* cfg,
                                 qwen3_prefix** out);
 /* d_qkv bf16 [tokens, (n_head + 2 n_kv_head) * head_dim]; d_out bf16 [rows,
  * n_head * head_dim], rows the tokens with queries; d_lse fp32 [n_head, rows],
- * the log-sum-exp of the scaled scores; d_qkv, d_out 16-byte aligned. */
+ * the log-sum-exp of the scaled scores; d_qkv, d_out 16-byte aligned. The three
+ * do not overlap. */
 gpt2_status qwen3_prefix_forward(const qwen3_prefix* p, const void* d_qkv,
                                  void* d_out, float* d_lse, void* hip_stream);
-/* The gradient of d_qkv to d_dqkv (written whole, not d_qkv itself; zero where
- * a prefix has no queries) from d_dout, that of d_out, and the forward's d_qkv,
+/* The gradient of d_qkv to d_dqkv (written whole, over none of the inputs; zero
+ * where a prefix has no queries) from d_dout, that of d_out, and the forward's d_qkv,
  * d_out and d_lse. A key's gradient sums over its group's query heads and, in
  * the prefix, over all sequences, in fp32 and in a fixed order.
  * Both: what a token does not see must be finite all the same; infinite or NaN

@@ -1365,6 +1365,8 @@ gpt2_status gpt2_orthogonalise(const float* d_x, float* d_y, int32_t rows, int32
   else if (reinterpret_cast<uintptr_t>(d_workspace) % 256) why = "the workspace is not 256-byte aligned";
   else if (workspace_bytes < need) why = "the workspace is smaller than gpt2_orthogonalise_size says";
   else if (iterations < 1 || iterations > 32) why = "iterations must be in 1..32";
+  const size_t bytes = (size_t)rows * cols * count * sizeof(float);
+  if (!why && overlap(d_y, bytes, d_x, bytes, true)) why = "y overlaps x without being it";
   if (why) {
     g_last_error = why;
     return GPT2_ERR_INVALID_ARG;

@@ -7,6 +7,12 @@
 
 typedef uint16_t bf16_t;
 
+// Whether two buffers share bytes (host); with `same` one at the same address does not count.
+inline bool overlap(const void* a, size_t an, const void* b, size_t bn, bool same = false) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return (x != y || !same) && x < y + bn && y < x + an;
+}
+
 // ---------------------------------------------------------------- GEMM
 enum GemmEpilogue {
   EPI_BF16 = 0,      // C = bf16(acc + bias? + residual?)

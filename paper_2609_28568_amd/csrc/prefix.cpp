@@ -189,6 +189,15 @@ gpt2_status fail(gpt2_status st, const char* why) {
   return st;
 }
 
+// Bytes of q|k|v, of the rows of out and dout, and of lse.
+struct Bytes {
+  size_t qkv, rows, lse;
+  explicit Bytes(const PrefixArgs& a)
+      : qkv((size_t)a.N * (a.H + 2 * a.Hkv) * a.hd * sizeof(bf16_t)),
+        rows((size_t)a.nq * a.H * a.hd * sizeof(bf16_t)),
+        lse((size_t)a.nq * a.H * sizeof(float)) {}
+};
+
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 }  // namespace
@@ -297,6 +306,10 @@ gpt2_status qwen3_prefix_forward(const qwen3_prefix* p, const void* d_qkv, void*
   if (!p || !d_qkv || !d_out || !d_lse) return fail(GPT2_ERR_INVALID_ARG, "null argument");
   if (!aligned16(d_qkv) || !aligned16(d_out) || reinterpret_cast<uintptr_t>(d_lse) % 4)
     return fail(GPT2_ERR_INVALID_ARG, "a pointer is not aligned");
+  const Bytes n(p->args);
+  if (overlap(d_out, n.rows, d_qkv, n.qkv) || overlap(d_lse, n.lse, d_qkv, n.qkv) ||
+      overlap(d_lse, n.lse, d_out, n.rows))
+    return fail(GPT2_ERR_INVALID_ARG, "out or lse overlaps another buffer");
   PrefixArgs a = p->args;
   a.qkv = static_cast<const bf16_t*>(d_qkv);
   a.out = static_cast<bf16_t*>(d_out);
@@ -311,7 +324,10 @@ gpt2_status qwen3_prefix_backward(const qwen3_prefix* p, const void* d_qkv, cons
   if (!aligned16(d_qkv) || !aligned16(d_out) || !aligned16(d_dout) || !aligned16(d_dqkv) ||
       reinterpret_cast<uintptr_t>(d_lse) % 4)
     return fail(GPT2_ERR_INVALID_ARG, "a pointer is not aligned");
-  if (d_dqkv == d_qkv) return fail(GPT2_ERR_INVALID_ARG, "dqkv may not be qkv");
+  const Bytes n(p->args);
+  if (overlap(d_dqkv, n.qkv, d_qkv, n.qkv) || overlap(d_dqkv, n.qkv, d_out, n.rows) ||
+      overlap(d_dqkv, n.qkv, d_dout, n.rows) || overlap(d_dqkv, n.qkv, d_lse, n.lse))
+    return fail(GPT2_ERR_INVALID_ARG, "dqkv overlaps another buffer");
   PrefixArgs a = p->args;
   a.qkv = static_cast<const bf16_t*>(d_qkv);
   a.out = static_cast<bf16_t*>(const_cast<void*>(d_out));

@@ -652,6 +652,9 @@ const char* rotary_args(const qwen3_rotary* r, const void* in, const void* raw, 
                         reinterpret_cast<uintptr_t>(qn) | reinterpret_cast<uintptr_t>(kn) |
                         (qn ? reinterpret_cast<uintptr_t>(raw) : 0);
   if (all % 16 || reinterpret_cast<uintptr_t>(pos) % 4) return "a pointer is not aligned";
+  const size_t bytes = (size_t)r->n_tokens * (r->n_head + 2 * r->n_kv_head) * r->head_dim * sizeof(bf16_t);
+  if (overlap(out, bytes, in, bytes, true) || (qn && overlap(out, bytes, raw, bytes, true)))
+    return "the result overlaps an input without being it";
   a->tokens = r->n_tokens;
   a->H = r->n_head;
   a->Hkv = r->n_kv_head;

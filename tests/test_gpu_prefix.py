@@ -479,3 +479,25 @@ def test_millions_of_single_tokens():
     e_dq = (e_ds @ kp.abs() + e_dss * k.abs()) / hd ** 0.5
     assert ((dx[P:, :hd] - dq).abs() <= e_dq + R * dq.abs()).all()
     assert (dx[:P, :hd] == 0).all()
+
+
+def test_results_over_what_is_read_are_refused():
+    from paper_2609_28568_amd import binding
+    qkv, dout, (H, Hkv, hd, P, lens, q0) = inputs("groups_of_three")
+    p = plan("groups_of_three")
+    n, width = qkv.shape
+    rows = n - q0
+    x, g = dev(qkv), dev(dout)
+    y, l = p.forward(x)
+    with pytest.raises(binding.LibError, match="overlap"):
+        p.forward(x, out=x.view(-1)[:rows * H * hd].view(rows, -1))
+    with pytest.raises(binding.LibError, match="overlap"):
+        p.forward(x, out=y, lse=y.view(torch.float32).view(-1)[:H * rows].view(H, rows))
+    place = torch.empty(2 * n * width, dtype=torch.bfloat16, device="cuda")
+    dx = place[64:64 + n * width].view(n, width)
+    over = place[:rows * H * hd].view(rows, -1)
+    lse = place.view(torch.float32)[40:40 + H * rows].view(H, rows)
+    for a in ((over, x, y, l), (g, x, over, l), (g, x, y, lse), (g, place[:n * width].view(n, width), y, l)):
+        with pytest.raises(binding.LibError, match="overlap"):
+            p.backward(*a, dqkv=dx)
+    p.close()

@@ -206,3 +206,11 @@ def test_step_with_the_default_positions_spelled_out():
     assert m.loss() == loss
     assert all(np.array_equal(v, grads[k]) for k, v in m.adapters("lora_grads").items())
     m.close()
+
+
+@pytest.mark.parametrize("name", ["three_axes", "hd256", "no_norm"])
+def test_gradient_in_place_of_the_rows(name):
+    from paper_2609_28568_amd import qwen3_binding as qb
+    x, d, (dx, dd), pos, how, ref = setup(name)
+    g = qb.rotary_backward(dd, dx, pos, **how)
+    assert torch.equal(qb.rotary_backward(dd, dx, pos, out=dx, **how), g) and dx.data_ptr() != g.data_ptr()

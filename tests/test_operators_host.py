@@ -304,3 +304,24 @@ def test_a_long_walk_is_shared_out_among_many_short_ones():
     st, size = prefix_size([1] * n, n_head=1, n_kv_head=1, head_dim=64, prefix_queries=0)
     # tables and the backward's D, 16 bytes a token, and the partial results of 64 workgroups or more
     assert st == 0 and size >= 16 * n + 64 * 2 * 128 * 64 * 4
+
+
+# ---- results that lie over what is still read
+
+@pytest.mark.parametrize("x,y", [(4096, 4100), (4100, 4096), (4096, 4096 + 8 * 8 * 3 * 4 - 4)])
+def test_orthogonalise_refuses_partial_overlap(x, y):
+    L = binding.lib()
+    assert L.gpt2_orthogonalise(x, y, 8, 8, 3, 5, 1 << 20, 1 << 30, None) == INVALID
+    assert "overlap" in L.gpt2_last_error(None).decode()
+
+
+@pytest.mark.parametrize("out", [(1 << 20) + 16, (1 << 20) - 16])
+def test_rotary_refuses_partial_overlap(out):
+    L, d = qb.lib(), rotary_desc()
+    base, far, pos, gain = 1 << 20, 1 << 22, 4096, 8192
+    calls = (lambda: L.qwen3_rotary_forward(ctypes.byref(d), base, pos, gain, gain, out, None),
+             lambda: L.qwen3_rotary_backward(ctypes.byref(d), base, far, pos, gain, gain, out, None),
+             lambda: L.qwen3_rotary_backward(ctypes.byref(d), far, base, pos, gain, gain, out, None))
+    for call in calls:
+        assert call() == INVALID
+        assert "overlap" in L.qwen3_last_error(None).decode()
