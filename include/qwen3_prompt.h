@@ -85,9 +85,10 @@ typedef struct qwen3_prefix qwen3_prefix;   /* opaque host-side handle */
  * aligned, the caller's, holding the layout's tables and the calls' scratch.
  * Laid out once per set of lengths and used by any number of calls, one at a
  * time: calls (or captured graphs) that may run at the same time take a layout
- * each. create writes the tables through hip_stream and synchronises it; it
- * cannot be captured. INVALID_ARG for lengths or sizes out of range (no
- * query at all; rows beyond 4 GiB), a NULL or unaligned buffer. */
+ * each. create writes the tables through hip_stream and synchronises it;
+ * ERR_STATE, and the capture goes on, while that stream is captured.
+ * INVALID_ARG for lengths or sizes out of range (no query at all; rows beyond
+ * 4 GiB), a NULL or unaligned buffer. */
 gpt2_status qwen3_prefix_size(const qwen3_prefix_config* cfg,
                               const int32_t* seq_lens, size_t* bytes_out);
 gpt2_status qwen3_prefix_create(const qwen3_prefix_config* cfg,
@@ -120,7 +121,8 @@ void qwen3_prefix_destroy(qwen3_prefix* p);
  * token and loss_from begin behind the prefix, and each answer's first token
  * is predicted within its own sequence. d_plan: qwen3_layout_size bytes,
  * 256-byte aligned, the caller's to keep while the layout is in use (by the
- * next forwards, and a backward that follows one). Synchronises the stream.
+ * next forwards, a backward that follows one, and graphs that either is captured
+ * into). Synchronises the stream, and is refused in a capture, as above.
  * d_plan NULL goes back to B sequences of T tokens. */
 gpt2_status qwen3_layout_size(const qwen3_model* m, int32_t prefix_len,
                               int32_t n_seq, const int32_t* seq_lens,

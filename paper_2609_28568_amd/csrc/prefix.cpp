@@ -229,6 +229,10 @@ hipError_t prefix_make(const qwen3_prefix_config& c, const int32_t* lens, void* 
   const Places p = places(c, t);
   *fits = plan_bytes >= p.total;
   if (!*fits) return hipErrorInvalidValue;
+  // the copy and the wait below would end a capture
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  if (hipError_t e = hipStreamIsCapturing(s, &capture)) return e;
+  if (capture != hipStreamCaptureStatusNone) return hipErrorStreamCaptureUnsupported;
   char* d = static_cast<char*>(d_plan);
   std::vector<char> host(p.dsum);
   auto put = [&](size_t at, const void* from, size_t bytes) {
@@ -293,6 +297,8 @@ gpt2_status qwen3_prefix_create(const qwen3_prefix_config* cfg, const int32_t* s
     const hipError_t e = prefix_make(*cfg, seq_lens, d_plan, plan_bytes, static_cast<hipStream_t>(hip_stream), p.get(),
                                      &fits);
     if (!fits) return fail(GPT2_ERR_INVALID_ARG, "d_plan is smaller than qwen3_prefix_size says");
+    if (e == hipErrorStreamCaptureUnsupported)
+      return fail(GPT2_ERR_STATE, "a layout is not made while its stream is captured");
     if (e != hipSuccess) return fail(GPT2_ERR_DEVICE, hipGetErrorString(e));
     *out = p.release();
     return GPT2_OK;

@@ -18,7 +18,8 @@ std::string prefix_check(const qwen3_prefix_config* c, const int32_t* seq_lens);
 // Bytes of the device buffer of a layout that prefix_check accepts. Throws std::bad_alloc.
 size_t prefix_bytes(const qwen3_prefix_config& c, const int32_t* seq_lens);
 // Its tables written to d_plan (synchronises the stream), unless plan_bytes is
-// too few for it. Throws std::bad_alloc.
+// too few for it; hipErrorStreamCaptureUnsupported, with nothing enqueued, in a
+// capture. Throws std::bad_alloc.
 hipError_t prefix_make(const qwen3_prefix_config& c, const int32_t* seq_lens, void* d_plan, size_t plan_bytes,
                        hipStream_t s, qwen3_prefix* out, bool* fits);
 

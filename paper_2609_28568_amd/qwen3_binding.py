@@ -453,7 +453,9 @@ class Qwen3:
 
     def set_layout(self, prefix_len=0, seq_lens=None):
         """The tokens as a prefix and sequences over it (qwen3_set_layout),
-        from the next forward on; without seq_lens: B sequences of T tokens."""
+        from the next forward on; without seq_lens: B sequences of T tokens.
+        Not in a capture, and a graph captured with a layout (or positions) is
+        replayed only until others are set, when these are let go."""
         if seq_lens is None:
             _check(lib().qwen3_set_layout(self.h, 0, 0, None, None, 0), self.h)
             self._plan = None

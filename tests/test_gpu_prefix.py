@@ -501,3 +501,31 @@ def test_results_over_what_is_read_are_refused():
         with pytest.raises(binding.LibError, match="overlap"):
             p.backward(*a, dqkv=dx)
     p.close()
+
+
+def test_a_layout_asked_for_in_a_capture_is_refused_and_the_capture_goes_on():
+    from paper_2609_28568_amd import binding, qwen3_binding as qb
+    qkv, dout, (H, Hkv, hd, P, lens, q0) = inputs("answers")
+    p = plan("answers")
+    x, g = dev(qkv), dev(dout)
+    y, l = p.forward(x)
+    w = dict(synth.QWEN3_WORKLOADS["qwen3_tiny"], B=1, T=192, max_seq_len=192)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    out, lse = torch.zeros_like(y), torch.zeros_like(l)
+    with torch.cuda.stream(side):
+        m = qb.Qwen3(qb.make_config(w, synth.QWEN3_OPTIM))
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        for make in (lambda: plan("answers"), lambda: m.set_layout(100, [92])):
+            with pytest.raises(binding.LibError, match="captured") as e:
+                make()
+            assert e.value.status == binding.GPT2_ERR_STATE
+        p.forward(x, out=out, lse=lse)
+    for _ in range(3):
+        out.zero_()
+        lse.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, y) and torch.equal(lse, l)
+    m.set_layout(100, [92])
+    m.close()
