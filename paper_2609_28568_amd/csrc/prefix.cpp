@@ -184,6 +184,7 @@ Places places(const qwen3_prefix_config& c, const Tables& t) {
   return p;
 }
 
+// (a reason of up to 15 letters needs no memory)
 gpt2_status fail(gpt2_status st, const char* why) {
   set_qwen3_error(why);
   return st;
@@ -281,7 +282,7 @@ gpt2_status qwen3_prefix_size(const qwen3_prefix_config* cfg, const int32_t* seq
     *bytes_out = prefix_bytes(*cfg, seq_lens);
     return GPT2_OK;
   } catch (const std::bad_alloc&) {
-    return fail(GPT2_ERR_DEVICE, "out of host memory");
+    return fail(GPT2_ERR_DEVICE, "out of memory");
   }
 }
 
@@ -303,7 +304,7 @@ gpt2_status qwen3_prefix_create(const qwen3_prefix_config* cfg, const int32_t* s
     *out = p.release();
     return GPT2_OK;
   } catch (const std::bad_alloc&) {
-    return fail(GPT2_ERR_DEVICE, "out of host memory");
+    return fail(GPT2_ERR_DEVICE, "out of memory");
   }
 }
 

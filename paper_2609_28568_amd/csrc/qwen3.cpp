@@ -556,6 +556,12 @@ gpt2_status fail(qwen3_model* m, gpt2_status st, const std::string& why) {
   return st;
 }
 
+// std::bad_alloc at an entry point; a reason this short needs no memory
+gpt2_status no_memory(qwen3_model* m) {
+  m->err = g_err = "out of memory";
+  return GPT2_ERR_DEVICE;
+}
+
 // Norm of the adapter gradients and the clip coefficient, into normcoef; the
 // norm also to d_grad_norm_out if given.
 gpt2_status clip_norm(qwen3_model* m, float* d_grad_norm_out) {
@@ -1051,11 +1057,15 @@ gpt2_status qwen3_layout_size(const qwen3_model* m, int32_t prefix_len, int32_t 
   if (!m) return fail(nullptr, GPT2_ERR_INVALID_ARG, "null model");
   const qwen3_prefix_config c{m->d.H, m->d.Hkv, m->d.hd, prefix_len, n_seq, 1};
   const gpt2_status st = qwen3_prefix_size(&c, seq_lens, bytes_out);
-  return st == GPT2_OK ? st : fail(const_cast<qwen3_model*>(m), st, std::string(g_err));
+  try {
+    return st == GPT2_OK ? st : fail(const_cast<qwen3_model*>(m), st, std::string(g_err));
+  } catch (const std::bad_alloc&) {
+    return no_memory(const_cast<qwen3_model*>(m));
+  }
 }
 
 gpt2_status qwen3_set_layout(qwen3_model* m, int32_t prefix_len, int32_t n_seq, const int32_t* seq_lens, void* d_plan,
-                             size_t plan_bytes) {
+                             size_t plan_bytes) try {
   if (!m) return fail(nullptr, GPT2_ERR_INVALID_ARG, "null model");
   if (!d_plan) {
     m->layout.reset();
@@ -1073,6 +1083,8 @@ gpt2_status qwen3_set_layout(qwen3_model* m, int32_t prefix_len, int32_t n_seq, 
     return fail(m, st, std::string(g_err));
   m->layout.reset(p);
   return GPT2_OK;
+} catch (const std::bad_alloc&) {
+  return no_memory(m);
 }
 
 gpt2_status qwen3_muon_size(const qwen3_config* cfg, size_t* bytes_out) {
