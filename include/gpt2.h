@@ -187,7 +187,8 @@ gpt2_status gpt2_adamw_step_noalloc(gpt2_model* m, int64_t step, float* lr_out,
  *   A = X X^T,  X <- 3.4445 X + (-4.7750 A + 2.0315 A^2) X
  * (the shorter side's Gram matrix: a G taller than wide goes as its
  * transpose). Five of them bring every singular value that is not small
- * against the norm near 1. Operands are kept to 22 bits or more, sums in fp32.
+ * against the norm near 1. Operands are kept to 22 bits, or to 2^-37 of the
+ * matrix's norm where that is more, sums in fp32.
  *
  * gpt2_orthogonalise: d_x, d_y fp32 [count, rows, cols], the matrices one
  * after another, each its own problem; d_y may be d_x, and overlaps it in no

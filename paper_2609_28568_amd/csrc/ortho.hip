@@ -5,16 +5,18 @@
 //   A = X X^T,  P = a I + b A + c A^2,  X <- P X     (each iteration)
 //
 // with a, b, c = 3.4445, -4.7750, 2.0315: a quintic on the singular values
-// that keeps [0, 1.2023] in itself and multiplies small ones by a, so all the
-// values the iteration stores stay within a factor of 3 of 1 or below.
+// that keeps [0, 1.2023] in itself and multiplies small ones by a, so X and A
+// stay below 1.5 and P, with its a on the diagonal, below 3.5.
 //
 // Precision: small singular values are multiplied by a^5 = 485, and rounding
 // errors with them, so bf16 products would leave a per cent. Every operand is
 // held as two fp16 numbers instead, hi = fp16(v s) and lo = fp16(v s - hi)
-// with s = 2^13 (|v| < 3, so v s < 65504; the rest of an fp32 significand down
-// to 2^-37 absolute), and a product is three MFMAs into fp32 accumulators:
-// hi hi + hi lo + lo hi. The dropped lo lo is 2^-22 of the product at most.
-// That is a third of the fp16 rate, which is five times the card's fp32 one.
+// with s = 2^13 (|v| < 3.5, so v s < 28673 of fp16's 65504): 22 bits of v from
+// about 2^-15 up, and below that what reaches down to 2^-37, fp16's smallest
+// number over s, where 1 is the norm of the matrix. A product is three MFMAs into
+// fp32 accumulators: hi hi + hi lo + lo hi. The dropped lo lo is 2^-22 of the
+// product at most. That is a third of the fp16 rate, which is five times the
+// card's fp32 one.
 //
 // Matrices that fit the LDS of a CU go through all iterations in one workgroup
 // (ortho_small_kernel). For the others, one product kernel for the three
@@ -23,10 +25,11 @@
 // through each product in one launch: workgroup b finds its group, matrix and
 // tile.
 //
-// What bounds it: 48 matrices of 768 x 768 take 1.6 ms, their products
-// 795 (A), 750 (P) and 840 (X) TFLOP/s of MFMA work, at the MFMA unit's power
-// limit for numbers of this kind (the library's batched fp16 products of the same
-// sizes: 815 and 706), plus 28 and 50 us for the norms and the halves.
+// What bounds it: 48 matrices of 768 x 768 take 1.60-1.68 ms on different
+// cards, their products 800 (A), 745 (P), 780 (X) and, with the fp32 result
+// stored, 700 TFLOP/s of MFMA work, at the MFMA unit's power limit for numbers of
+// this kind (the library's batched fp16 products of the same sizes: 815 and 706),
+// plus 28 and 50 us for the norms and the halves.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>

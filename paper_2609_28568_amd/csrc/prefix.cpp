@@ -53,7 +53,15 @@ void deal(const std::vector<PrefixItem>& walks, int per, std::vector<PrefixItem>
 // joined by a launch that reads them all. Measured (forward, head size 128, one
 // walk of 129 tiles for each of 8 heads, per 5, 6, 8, 12, 16, 24, 40, 129: 21.9,
 // 21.3, 21.6, 23.3, 25.7, 30.9, 38.8, 117; this gives 21.3, 21.1, 21.5, 23.4,
-// 25.4, 30.7, 39.8, 118).
+// 25.4, 30.7, 39.8, 118; with head size 64 measured 13.2, 13.2, 13.3, 15.0, 16.5,
+// 19.7, 24.9, 68.2, chosen 12.8). One sequence of 8,256 tokens, 2 heads, walks of
+// 2 to 129 tiles, whole backward for dK/dV's lengths, per 8, 12, 16, 24, 40, 64, 129:
+//   head size 128   244, 213, 218, 202, 220, 269, 321; chosen 198
+//   head size 64    138, 124, 128, 121, 136, 171, 206; chosen 117
+// and its forward, whose choice is off there:
+//   head size 128   69, 62, 62, 61, 81, 90, 112; chosen 78
+//   head size 64    42, 38, 41, 44, 63, 58, 69; chosen 50
+// dQ walks the forward's items: its best lengths were the forward's, within 2 %.
 constexpr int CUS = 256;
 struct Costs {
   int slots;            // workgroups that run at a time

@@ -20,9 +20,9 @@
 // second launch in a fixed order.
 //
 // Measured: 16 sequences of 256 over a prefix of 2048, 16 + 8 heads of 128:
-// forward 127-130 us (700 TFLOP/s), dQ 170-194 (700-790), dK/dV 230-246 + 11
+// forward 115-130 us (700-790 TFLOP/s), dQ 170-194 (700-790), dK/dV 230-248 + 11
 // (750); waves wait on their own chain of products, exponentials and products. 64
-// single tokens after 8192: 18 + 5 us, 34 MB of keys and values and 10 MB of
+// single tokens after 8192: 17 + 5 us, 34 MB of keys and values and 10 MB of
 // partial results.
 //
 // The tile arithmetic is attention.hip's: S^T = K Q^T with one row per lane,
@@ -808,7 +808,11 @@ hipError_t fwd_t(const PrefixArgs& a, hipStream_t s) {
   const unsigned joins = a.njoins * a.Hkv;
   // Many parts: a wave a row (64 tokens after 8,192, 19 parts: 5-7 us, a few
   // lanes a row 15). Few: a few lanes a row (12 answers after 1,500, walks in a few
-  // parts: 7.5 us, a wave a row 11.4).
+  // parts: 7.5 us, a wave a row 11.4). Where both counts are high the two are
+  // close or a few lanes ahead: 12 of 75 tokens after 1,500 in items of three
+  // tiles, nine parts, forward and join 64.6 and 66.0 us at head size 128, 30.7
+  // and 35.5 at 64; in single tokens' items of 7 to 26 tiles (19 to 5 parts) 23.0
+  // and 20.7 (7), 23.8 and 21.8 (9), 22.8 and 22.7 (11), 33.3 and 33.8 (26).
   if (a.parts > 8) hipLaunchKernelGGL(prefix_fwd_join_kernel<HD>, dim3(joins, BQ / 4), dim3(256), 0, s, a);
   else hipLaunchKernelGGL(prefix_fwd_join_few_kernel<HD>, dim3(joins, BQ * HD / 2048), dim3(256), 0, s, a);
   return hipGetLastError();
