@@ -183,6 +183,18 @@ def on_stream(device, fn, *args):
         return fn(*args, stream)
 
 
+def i32(n) -> int:
+    """n as an int of the C interface, which ctypes would cut off silently."""
+    n = int(n)
+    if not -2 ** 31 <= n < 2 ** 31:
+        raise ValueError(f"{n} does not fit 32 bits")
+    return n
+
+
+def muon_settings(momentum, nesterov, iterations, scale) -> Muon:
+    return Muon(float(momentum), int(bool(nesterov)), i32(iterations), float(scale))
+
+
 def stream_buffer(nbytes, device, stream):
     """A uint8 tensor that work on `stream` may write at once: memory of its
     pool, which no other stream's pending work still holds."""
@@ -210,14 +222,14 @@ def orthogonalise(x, iterations=5, out=None, workspace=None):
     elif workspace.dtype != torch.uint8 or workspace.device != x.device or not workspace.is_contiguous():
         raise ValueError("the workspace must be a contiguous uint8 tensor on x's device")
     _check(on_stream(x.device, lib().gpt2_orthogonalise, x.data_ptr(), out.data_ptr(), rows, cols, count,
-                     int(iterations), workspace.data_ptr(), workspace.numel()))
+                     i32(iterations), workspace.data_ptr(), workspace.numel()))
     return out
 
 
 def orthogonalise_size(rows, cols, count=1) -> int:
     """Workspace bytes of orthogonalise."""
     n = ctypes.c_size_t()
-    _check(lib().gpt2_orthogonalise_size(rows, cols, count, ctypes.byref(n)))
+    _check(lib().gpt2_orthogonalise_size(i32(rows), i32(cols), i32(count), ctypes.byref(n)))
     return n.value
 
 
@@ -323,7 +335,7 @@ class GPT2:
             _check(self.L.gpt2_muon_size(ctypes.byref(self.cfg), ctypes.byref(n)))
             self.muon_workspace = stream_buffer(n.value, self.device, self.stream)
         lr = ctypes.c_float()
-        how = Muon(float(momentum), int(bool(nesterov)), int(iterations), float(scale))
+        how = muon_settings(momentum, nesterov, iterations, scale)
         _check(self.L.gpt2_muon_step(self.handle, int(step), ctypes.byref(how), self.muon_workspace.data_ptr(),
                                      self.muon_workspace.numel(), ctypes.byref(lr),
                                      norm_out.data_ptr() if norm_out is not None else None), self.handle)

@@ -13,7 +13,8 @@ import functools
 
 import numpy as np
 
-from .binding import GPT2_ERR_INVALID_ARG, LibError, Muon, lib as _lib_gpt2, on_stream, stream_buffer
+from .binding import (GPT2_ERR_INVALID_ARG, LibError, Muon, i32, lib as _lib_gpt2, muon_settings, on_stream,
+                      stream_buffer)
 
 RP = 64   # padded adapter rank of the library
 # kernel classes of the timing probes (QWEN3_K_* in include/qwen3.h)
@@ -220,7 +221,8 @@ def _rotary_desc(n, n_head, n_kv_head, width, sections, interleaved, theta, eps)
     if n_head < 1 or n_kv_head < 1 or width % (n_head + 2 * n_kv_head) or not 1 <= len(sections) <= 4:
         raise ValueError("rows of q | k | v are (n_head + 2 n_kv_head) head_dim wide, with 1 to 4 sections")
     hd = width // (n_head + 2 * n_kv_head)
-    return ctypes.byref(Rotary(n, n_head, n_kv_head, hd, len(sections), (ctypes.c_int32 * 4)(*sections),
+    return ctypes.byref(Rotary(i32(n), i32(n_head), i32(n_kv_head), i32(hd), len(sections),
+                               (ctypes.c_int32 * 4)(*map(i32, sections)),
                                int(bool(interleaved)), theta, eps)), hd
 
 
@@ -278,7 +280,8 @@ class SharedPrefix:
         import torch
         self.torch = torch
         self.h = ctypes.c_void_p()
-        lens = [int(n) for n in seq_lens]
+        lens = [i32(n) for n in seq_lens]
+        n_head, n_kv_head, head_dim, prefix_len = map(i32, (n_head, n_kv_head, head_dim, prefix_len))
         cfg = PrefixConfig(n_head, n_kv_head, head_dim, prefix_len, len(lens), int(bool(prefix_queries)))
         c_lens = (ctypes.c_int32 * len(lens))(*lens)
         n = ctypes.c_size_t()
@@ -441,7 +444,7 @@ class Qwen3:
         if positions is not None:
             _device_rows(positions, "positions", self.torch.int32, self.bufs["workspace"],
                          (len(sections), self.cfg.B * self.cfg.T))
-        sec = (ctypes.c_int32 * len(sections))(*sections)
+        sec = (ctypes.c_int32 * len(sections))(*map(i32, sections))
         _check(lib().qwen3_set_positions(self.h, _ptr(positions), len(sections), sec, int(bool(interleaved))), self.h)
         if positions is not None:
             # the model's stream reads them: after what the current one has to do with them, and before they are freed
@@ -460,7 +463,7 @@ class Qwen3:
             _check(lib().qwen3_set_layout(self.h, 0, 0, None, None, 0), self.h)
             self._plan = None
             return
-        lens = [int(n) for n in seq_lens]
+        lens, prefix_len = [i32(n) for n in seq_lens], i32(prefix_len)
         c_lens = (ctypes.c_int32 * len(lens))(*lens)
         n = ctypes.c_size_t()
         _check(lib().qwen3_layout_size(self.h, prefix_len, len(lens), c_lens, ctypes.byref(n)), self.h)
@@ -476,7 +479,7 @@ class Qwen3:
             n = ctypes.c_size_t()
             _check(lib().qwen3_muon_size(ctypes.byref(self.cfg), ctypes.byref(n)))
             self.muon_workspace = stream_buffer(n.value, self.bufs["workspace"].device, self.stream)
-        how = Muon(float(momentum), int(bool(nesterov)), int(iterations), float(scale))
+        how = muon_settings(momentum, nesterov, iterations, scale)
         _check(lib().qwen3_muon_step(self.h, ctypes.byref(how), self.muon_workspace.data_ptr(),
                                      self.muon_workspace.numel(),
                                      norm_out.data_ptr() if norm_out is not None else None), self.h)

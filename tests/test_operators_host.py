@@ -325,3 +325,18 @@ def test_rotary_refuses_partial_overlap(out):
     for call in calls:
         assert call() == INVALID
         assert "overlap" in L.qwen3_last_error(None).decode()
+
+
+# ---- numbers as the bindings take them
+
+@pytest.mark.parametrize("call", [
+    lambda: binding.orthogonalise_size(2 ** 32 + 8, 8),
+    lambda: binding.orthogonalise_size(8, 8, 2 ** 32 + 1),
+    lambda: qb.SharedPrefix(4, 2, 128, 2 ** 32 + 100, [5]),
+    lambda: qb.SharedPrefix(4, 2, 128, 100, [2 ** 32 + 5]),
+    lambda: qb.SharedPrefix(2 ** 32 + 4, 2, 128, 100, [5]),
+    lambda: qb._rotary_desc(8, 4, 2, 1024, (2 ** 32 + 64,), False, 1e6, 1e-6),
+    lambda: binding.muon_settings(0.9, True, 2 ** 32 + 5, 0.2)])
+def test_integers_past_32_bits_are_not_cut_off(call):
+    with pytest.raises(ValueError, match="32 bits"):
+        call()
