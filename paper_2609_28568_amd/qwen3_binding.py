@@ -232,7 +232,9 @@ def _rotary_args(qkv, positions, n_head, n_kv_head, sections, theta, q_norm, k_n
     if qkv.dim() != 2:
         raise ValueError("rows of q | k | v [tokens, (n_head + 2 n_kv_head) head_dim]")
     n, width = qkv.shape
-    r, hd = _rotary_desc(n, n_head, n_kv_head, width, tuple(sections), interleaved, theta, eps)
+    # plain numbers: descriptions are kept by value, and a tensor's would be its identity
+    sections = tuple(map(int, sections))
+    r, hd = _rotary_desc(n, int(n_head), int(n_kv_head), width, sections, bool(interleaved), float(theta), float(eps))
     _device_rows(positions, "positions", torch.int32, qkv, (len(sections), n))
     for name, g in (("q_norm", q_norm), ("k_norm", k_norm)):
         if g is not None:

@@ -340,3 +340,19 @@ def test_rotary_refuses_partial_overlap(out):
 def test_integers_past_32_bits_are_not_cut_off(call):
     with pytest.raises(ValueError, match="32 bits"):
         call()
+
+
+def test_a_rotary_description_is_made_of_the_numbers_it_was_given(monkeypatch):
+    """Descriptions are kept by their values: one of a tensor that has changed is another."""
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(qb, "_device_rows", lambda *a, **kw: a[0])
+    x, pos = torch.zeros(4, 8 * 128, dtype=torch.bfloat16), torch.zeros(1, 4, dtype=torch.int32)
+    theta, eps, section = torch.tensor(1e4), torch.tensor(1e-6), torch.tensor(64)
+    made = []
+    for _ in range(2):
+        r = qb._rotary_args(x, pos, 4, 2, (section, 0), theta, None, None, eps, False)._obj
+        made.append((r.theta, r.rms_eps, r.sections[0]))
+        theta.mul_(4)
+        eps.mul_(4)
+        section.sub_(1)
+    assert made[0] == (1e4, ctypes.c_float(1e-6).value, 64) and made[1] == (4e4, ctypes.c_float(4e-6).value, 63)
