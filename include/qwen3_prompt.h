@@ -40,9 +40,9 @@ typedef struct qwen3_rotary {
  * in no other way. Angles are in fp64, all else in fp32, the result rounded once.
  * qwen3_rotary_backward: from d_dout (the gradient of d_out) and the same
  * d_qkv, positions and gains, the gradient of d_qkv to d_dqkv, which may be
- * d_dout or d_qkv and overlaps them in no other way. The gains are frozen; without them d_qkv is not read and may be
- * NULL. INVALID_ARG for what is not as said here; nothing is launched then,
- * nor for n_tokens 0. */
+ * d_dout or d_qkv and overlaps them in no other way. The gains are frozen;
+ * without them d_qkv is not read and may be NULL. INVALID_ARG for what is not as
+ * said here; nothing is launched then, nor for n_tokens 0. */
 gpt2_status qwen3_rotary_forward(const qwen3_rotary* r, const void* d_qkv,
                                  const int32_t* d_positions,
                                  const void* d_q_norm, const void* d_k_norm,
@@ -102,8 +102,8 @@ gpt2_status qwen3_prefix_create(const qwen3_prefix_config* cfg,
 gpt2_status qwen3_prefix_forward(const qwen3_prefix* p, const void* d_qkv,
                                  void* d_out, float* d_lse, void* hip_stream);
 /* The gradient of d_qkv to d_dqkv (written whole, over none of the inputs; zero
- * where a prefix has no queries) from d_dout, that of d_out, and the forward's d_qkv,
- * d_out and d_lse. A key's gradient sums over its group's query heads and, in
+ * where a prefix has no queries) from d_dout, that of d_out, and the forward's
+ * d_qkv, d_out and d_lse. A key's gradient sums over its group's query heads and, in
  * the prefix, over all sequences, in fp32 and in a fixed order.
  * Both: what a token does not see must be finite all the same; infinite or NaN
  * rows of one sequence can reach its neighbours' (0 times NaN in a product). */

@@ -28,7 +28,7 @@
 // The tile arithmetic is attention.hip's: S^T = K Q^T with one row per lane,
 // probabilities handed to the next MFMA from the accumulator registers, where they
 // and the score gradients are rounded to bf16 (2^-8 of each at most): products of
-// fp32 operands would run at a sixth of the rate or less. Sums, maxima and the
+// fp32 operands would run at an eighth of the rate. Sums, maxima and the
 // log-sum-exp are fp32. Against 64 bits the output is 2.2e-3 and the gradients
 // 2.4e-3 off, where rounding only the results leaves 1.7e-3.
 #include <type_traits>
