@@ -1,0 +1,333 @@
+// The pages of a cache of keys and values: forking, appending, compacting. A
+// page is one piece of memory in each layer, [2: keys, values][Hkv][ps][hd], so
+// that a key/value head's tokens are consecutive rows for the attention and a
+// page moves as one run of bytes.
+//
+// The books (table, lengths, counts of holders) are kept on the device: which
+// pages are taken follows from the counts alone, so results do not depend on
+// which workgroup comes first. Books of a call are one launch of few
+// workgroups, bound by a few dependent memory round trips; the tokens and pages
+// they name are moved by a second one, bound by HBM.
+#include <algorithm>
+
+#include "common.h"
+#include "kernels.h"
+
+namespace {
+
+constexpr int BOOK = 1024;   // threads of the one workgroup that keeps the books
+constexpr int WAVES = BOOK / 64;
+
+// Exclusive prefix sum of v over the workgroup, in thread order; *total: the sum.
+// `parts`: WAVES ints of LDS, free again after a barrier.
+DEV int block_scan(int v, int* parts, int* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 63) parts[wave] = x;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    const int p = parts[w];
+    before += w < wave ? p : 0;
+    all += p;
+  }
+  *total = all;
+  return before + x - v;
+}
+
+DEV int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
+
+// A column of the table (one page of every sequence) follows from that column
+// alone, so a workgroup takes some of them, reads the old ones into LDS and
+// writes the new ones. Lengths go with the first workgroup.
+__global__ __launch_bounds__(256) void fork_kernel(CacheArgs c, const int32_t* src, const int32_t* keep, int cols) {
+  extern __shared__ int32_t old[];
+  const int col0 = blockIdx.x * cols, n = c.n_seq * cols;
+  const int32_t kept_pages = c.max_pages;
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const int col = col0 + i % cols;
+    old[i] = col < kept_pages ? c.table[(size_t)(i / cols) * c.max_pages + col] : -1;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const int s = i / cols, k = i - s * cols, col = col0 + k;
+    if (col >= c.max_pages) continue;
+    const int from = src[s];
+    int page = (unsigned)from < (unsigned)c.n_seq ? old[from * cols + k] : -1;
+    if (keep && (long)col * c.ps >= keep[s]) page = -1;
+    const int was = old[i];
+    if (page == was) continue;
+    c.table[(size_t)s * c.max_pages + col] = page;
+    if ((unsigned)was < (unsigned)c.n_pages) atomicSub(c.refs + was, 1);
+    if ((unsigned)page < (unsigned)c.n_pages) atomicAdd(c.refs + page, 1);
+  }
+  if (blockIdx.x) return;
+  __syncthreads();
+  for (int s = threadIdx.x; s < c.n_seq; s += 256) old[s] = c.lens[s];
+  __syncthreads();
+  for (int s = threadIdx.x; s < c.n_seq; s += 256) {
+    const int from = src[s];
+    int len = (unsigned)from < (unsigned)c.n_seq ? old[from] : 0;
+    if (keep) len = min(len, max(keep[s], 0));
+    c.lens[s] = len;
+  }
+}
+
+// What sequence s appends: tokens, and the place of the first.
+struct Add {
+  int len, n;
+};
+DEV Add adding(const CacheArgs& c, const AppendArgs& a, int s) {
+  Add r;
+  r.len = clampi(c.lens[s], 0, c.max_pages * c.ps);
+  const int b = clampi(a.starts[s], 0, a.n_rows), e = clampi(a.starts[s + 1], b, a.n_rows);
+  r.n = min(e - b, a.max_new);
+  if (a.counts) r.n = clampi(a.counts[s], 0, a.path ? a.max_new : r.n);
+  return r;
+}
+
+// Pages for the new tokens: how many each sequence needs, which are free, and
+// the i-th needed is the i-th free one. Leaves a record (length, tokens, shared
+// page, its copy) for every sequence and the list of those that copy.
+__global__ __launch_bounds__(BOOK) void append_book_kernel(CacheArgs c, AppendArgs a) {
+  __shared__ int32_t end[CACHE_MAX_SEQ], shared_page[CACHE_MAX_SEQ], first_col[CACHE_MAX_SEQ];
+  __shared__ int parts[3][WAVES];
+  __shared__ int copies;
+  int32_t* head = c.scratch;
+  int4* rec = reinterpret_cast<int4*>(c.scratch + CACHE_HEADER);
+  int32_t* copying = c.scratch + CACHE_HEADER + 4 * c.n_seq;   // [n_seq] at most n_pages
+  int32_t* freed = copying + c.n_pages;
+  const int tid = threadIdx.x;
+  if (tid == 0) copies = 0;
+
+  // free pages of this thread's run
+  const int per = (c.n_pages + BOOK - 1) / BOOK, p0 = min(tid * per, c.n_pages), p1 = min(p0 + per, c.n_pages);
+  int nfree = 0;
+#pragma unroll 4
+  for (int p = p0; p < p1; ++p) nfree += c.refs[p] == 0;
+
+  const int each = (c.n_seq + BOOK - 1) / BOOK;
+  int need = 0, over = 0;
+  for (int k = 0; k < each; ++k) {
+    const int s = tid * each + k;
+    if (s >= c.n_seq) break;
+    const Add d = adding(c, a, s);
+    const int at = d.len / c.ps, from = (d.len + c.ps - 1) / c.ps, to = (int)(((long)d.len + d.n + c.ps - 1) / c.ps);
+    int page = -1;
+    if (d.n > 0 && d.len % c.ps) {
+      page = c.table[(size_t)s * c.max_pages + at];
+      if ((unsigned)page >= (unsigned)c.n_pages || c.refs[page] < 2) page = -1;
+    }
+    shared_page[s] = page;
+    first_col[s] = from;
+    need += (page >= 0) + to - from;
+    end[s] = need;   // within the thread's run of sequences
+    over += max(0, to - c.max_pages);
+    rec[s] = make_int4(d.len, d.n, page, -1);
+  }
+  int total, nfrees, overs;
+  const int before = block_scan(need, parts[0], &total);
+  const int rank0 = block_scan(nfree, parts[1], &nfrees);
+  block_scan(over, parts[2], &overs);
+  const int missing = max(0, total - nfrees) + overs;
+  if (tid == 0) {
+    *c.missing = missing;
+    head[0] = missing == 0;
+  }
+  if (missing) return;
+  for (int k = 0; k < each; ++k) {
+    const int s = tid * each + k;
+    if (s >= c.n_seq) break;
+    end[s] += before;
+    const int4 r = rec[s];
+    c.lens[s] = r.x + r.y;
+    if (r.z >= 0) copying[atomicAdd(&copies, 1)] = s;
+  }
+  int rank = rank0;
+  for (int p = p0; p < p1 && rank < total; ++p)
+    if (c.refs[p] == 0) freed[rank++] = p;
+  __syncthreads();
+  if (tid == 0) head[1] = copies;
+  for (int i = tid; i < total; i += BOOK) {
+    int lo = 0, hi = c.n_seq - 1;   // the first sequence whose end lies past i
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (end[mid] > i) hi = mid;
+      else lo = mid + 1;
+    }
+    const int s = lo, k = i - (s ? end[s - 1] : 0), page = freed[i], was = shared_page[s];
+    const int col = first_col[s] + k - (was >= 0);
+    c.table[(size_t)s * c.max_pages + col] = page;
+    c.refs[page] = 1;
+    if (was >= 0 && k == 0) {
+      atomicSub(c.refs + was, 1);
+      reinterpret_cast<int32_t*>(rec + s)[3] = page;
+    }
+  }
+}
+
+DEV size_t page_at(const CacheArgs& c, int layer, int page) {   // in elements
+  return ((size_t)layer * c.n_pages + page) * (2 * (size_t)c.Hkv * c.ps * c.hd);
+}
+
+// Tokens into their places, a wave `tok` tokens of one sequence and layer, and
+// behind those blocks the shared pages' tokens, a wave one head of one page.
+__global__ __launch_bounds__(64) void append_move_kernel(CacheArgs c, AppendArgs a, int tok, int groups, unsigned nt) {
+  const int32_t* head = c.scratch;
+  const int4* rec = reinterpret_cast<const int4*>(c.scratch + CACHE_HEADER);
+  const int lane = threadIdx.x;
+  if (!head[0]) return;
+  const int hu = c.hd / 8, units = 2 * c.Hkv * hu;   // 16-byte units of a head, of a token
+  if (blockIdx.x < nt) {
+    const int layer = blockIdx.y;
+    const int s = blockIdx.x / groups, i0 = (blockIdx.x - s * groups) * tok;
+    const int4 r = rec[s];
+    const int n = min(tok, r.y - i0);
+    if (n <= 0) return;
+    const int b = clampi(a.starts[s], 0, a.n_rows), e = clampi(a.starts[s + 1], b, a.n_rows);
+    const size_t ld = (size_t)(a.H + 2 * c.Hkv) * c.hd;
+    const bf16_t* rows = a.qkv + layer * a.layer_stride + (size_t)a.H * c.hd;
+    constexpr int FLIGHT = 4;
+    const int all = n * units;
+    for (int u0 = lane; u0 < all; u0 += 64 * FLIGHT) {
+      uint4 v[FLIGHT];
+      bf16_t* to[FLIGHT];
+#pragma unroll
+      for (int k = 0; k < FLIGHT; ++k) {
+        const int u = u0 + 64 * k;
+        to[k] = nullptr;
+        v[k] = make_uint4(0, 0, 0, 0);
+        if (u < all) {
+          const int i = u / units, w = u - i * units, h = w / hu;
+          const int row = a.path ? a.path[(size_t)s * a.max_new + i0 + i] : i0 + i;
+          const int pos = r.x + i0 + i, page = c.table[(size_t)s * c.max_pages + pos / c.ps];
+          if ((unsigned)row < (unsigned)(e - b) && (unsigned)page < (unsigned)c.n_pages) {
+            to[k] = c.pages + page_at(c, layer, page) + ((size_t)h * c.ps + pos % c.ps) * c.hd + (w - h * hu) * 8;
+            v[k] = *reinterpret_cast<const uint4*>(rows + (size_t)(b + row) * ld + w * 8);
+          }
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < FLIGHT; ++k)
+        if (to[k]) *reinterpret_cast<uint4*>(to[k]) = v[k];
+    }
+    return;
+  }
+  const int32_t* copying = c.scratch + CACHE_HEADER + 4 * c.n_seq;
+  const int layer = blockIdx.y, n = head[1] * 2 * c.Hkv;
+  for (int i = blockIdx.x - nt; i < n; i += gridDim.x - nt) {
+    const int s = copying[i / (2 * c.Hkv)], h = i % (2 * c.Hkv);
+    const int4 r = rec[s];
+    const uint4* from = reinterpret_cast<const uint4*>(c.pages + page_at(c, layer, r.z) + (size_t)h * c.ps * c.hd);
+    uint4* to = reinterpret_cast<uint4*>(c.pages + page_at(c, layer, r.w) + (size_t)h * c.ps * c.hd);
+    const int m = r.x % c.ps * hu;
+#pragma unroll 4
+    for (int u = lane; u < m; u += 64) to[u] = from[u];
+  }
+}
+
+// Which page moves where: the k-th page in use at or above their number to the
+// k-th free one below.
+__global__ __launch_bounds__(BOOK) void compact_book_kernel(CacheArgs c) {
+  __shared__ int parts[3][WAVES];
+  int32_t* head = c.scratch;
+  int32_t* holes = c.scratch + CACHE_HEADER + 4 * c.n_seq;   // the k-th move's target
+  int32_t* from = holes + c.n_pages;                         // ... and source
+  const int tid = threadIdx.x;
+  const int per = (c.n_pages + BOOK - 1) / BOOK, p0 = min(tid * per, c.n_pages), p1 = min(p0 + per, c.n_pages);
+  int mine = 0, used, moves, nholes;
+#pragma unroll 4
+  for (int p = p0; p < p1; ++p) mine += c.refs[p] != 0;
+  const int before = block_scan(mine, parts[0], &used);   // pages in use below this thread's run
+  // of pages below `used`, those not in use; of pages from there on, those in use
+  const int below = clampi(used - p0, 0, p1 - p0);
+  int low = 0;
+  for (int p = p0; p < p0 + below; ++p) low += c.refs[p] != 0;
+  int hole = block_scan(below - low, parts[1], &nholes);
+  int move = block_scan(mine - low, parts[2], &moves);
+  (void)before;
+  for (int p = p0; p < p1; ++p) {
+    const bool on = c.refs[p] != 0;
+    if (p < used && !on) holes[hole++] = p;
+    if (p >= used && on) from[move++] = p;
+  }
+  if (tid == 0) {
+    head[0] = moves;
+    head[1] = used;
+  }
+  __syncthreads();
+  for (int k = tid; k < moves; k += BOOK) {
+    const int a = from[k], b = holes[k];
+    c.refs[b] = c.refs[a];
+    c.refs[a] = 0;
+  }
+}
+
+// The pages' contents and the table's entries. A move's target is found from its
+// source by a search in the sorted list.
+__global__ __launch_bounds__(256) void compact_move_kernel(CacheArgs c) {
+  const int32_t* head = c.scratch;
+  const int32_t* holes = c.scratch + CACHE_HEADER + 4 * c.n_seq;
+  const int32_t* from = holes + c.n_pages;
+  const int moves = head[0], used = head[1];
+  if (moves == 0) return;
+  const long entries = (long)c.n_seq * c.max_pages, step = (long)gridDim.x * 256;
+  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < entries; i += step) {
+    const int p = c.table[i];
+    if (p < used || p >= c.n_pages) continue;
+    int lo = 0, hi = moves - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (from[mid] >= p) hi = mid;
+      else lo = mid + 1;
+    }
+    if (from[lo] == p) c.table[i] = holes[lo];
+  }
+  const int units = 2 * c.Hkv * c.ps * c.hd / 8;   // of a page, a multiple of 256
+  const int pieces = (units + 1023) / 1024;
+  const long per = (long)c.L * pieces, items = moves * per;
+  for (long i = blockIdx.x; i < items; i += gridDim.x) {
+    const int k = (int)(i / per), layer = (int)((i - k * per) / pieces);
+    const int u0 = (int)(i - k * per - (long)layer * pieces) * 1024;
+    const uint4* src = reinterpret_cast<const uint4*>(c.pages + page_at(c, layer, from[k])) + u0;
+    uint4* dst = reinterpret_cast<uint4*>(c.pages + page_at(c, layer, holes[k])) + u0;
+    const int n = min(4, (units - u0) / 256);
+    uint4 v[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = q < n ? src[q * 256 + threadIdx.x] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (q < n) dst[q * 256 + threadIdx.x] = v[q];
+  }
+}
+
+}  // namespace
+
+hipError_t launch_cache_fork(const CacheArgs& c, const int32_t* src, const int32_t* keep, hipStream_t s) {
+  // columns of a workgroup: 64 KiB of LDS hold them for all sequences, and its lengths fit beside none
+  const int cols = std::min(64, std::max(1, 16384 / c.n_seq));
+  const size_t lds = sizeof(int32_t) * (size_t)c.n_seq * cols;
+  hipLaunchKernelGGL(fork_kernel, dim3((c.max_pages + cols - 1) / cols), dim3(256), lds, s, c, src, keep, cols);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_append(const CacheArgs& c, const AppendArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(append_book_kernel, dim3(1), dim3(BOOK), 0, s, c, a);
+  const int tok = a.max_new >= 64 ? 8 : 1, groups = (a.max_new + tok - 1) / tok;
+  const unsigned nt = (unsigned)c.n_seq * groups;
+  const unsigned nc = (unsigned)std::min((long)c.n_seq * 2 * c.Hkv, std::max(1l, 2048l / c.L));
+  hipLaunchKernelGGL(append_move_kernel, dim3(nt + nc, c.L), dim3(64), 0, s, c, a, tok, groups, nt);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_compact(const CacheArgs& c, hipStream_t s) {
+  hipLaunchKernelGGL(compact_book_kernel, dim3(1), dim3(BOOK), 0, s, c);
+  hipLaunchKernelGGL(compact_move_kernel, dim3(2048), dim3(256), 0, s, c);
+  return hipGetLastError();
+}

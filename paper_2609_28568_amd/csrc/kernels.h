@@ -435,6 +435,45 @@ struct RotaryArgs {
 hipError_t launch_rotary(const RotaryArgs& a, const bf16_t* in, const bf16_t* raw, bf16_t* out, int backward,
                          hipStream_t s);
 
+// ---------------------------------------------------------------- paged cache, attention over it, logits
+// The cache as the kernels take it (qwen3_cache). Scratch: int32 header [16],
+// a record of four a sequence, two lists of n_pages.
+struct CacheArgs {
+  int L, Hkv, hd, ps, n_pages, n_seq, max_pages;
+  bf16_t* pages;     // [L][n_pages][2][Hkv][ps][hd]
+  int32_t *table, *lens, *refs, *missing, *scratch;
+};
+constexpr int CACHE_HEADER = 16, CACHE_MAX_SEQ = 4096;
+inline size_t cache_scratch_ints(int n_seq, int n_pages) { return CACHE_HEADER + 4 * (size_t)n_seq + 2 * (size_t)n_pages; }
+hipError_t launch_cache_fork(const CacheArgs& c, const int32_t* src, const int32_t* keep, hipStream_t s);
+struct AppendArgs {
+  const bf16_t* qkv;      // [L][n_rows][(H + 2 Hkv) hd], layer_stride elements apart
+  int H, n_rows, max_new;
+  size_t layer_stride;
+  const int32_t *starts, *counts, *path;
+};
+hipError_t launch_cache_append(const CacheArgs& c, const AppendArgs& a, hipStream_t s);
+hipError_t launch_cache_compact(const CacheArgs& c, hipStream_t s);
+
+// Attention of new tokens over one layer of the cache (tree.hip).
+struct TreeArgs {
+  int H, Hkv, hd, ps, n_pages, n_seq, max_pages;
+  int n_rows, max_new, mask_words;
+  const bf16_t* pages;    // the layer's
+  const int32_t *table, *lens, *starts, *mask;
+  const bf16_t* qkv;
+  bf16_t* out;
+  float* lse;
+  int32_t* plan;          // workspace: n_seq + 2 int32, then partial results
+  float* part;
+};
+// workspace bytes: the plan, then the partial results, which begin at *part_at; 0: out of range
+size_t tree_workspace(const TreeArgs& a, size_t* part_at);
+hipError_t launch_tree(const TreeArgs& a, hipStream_t s);
+
+struct qwen3_logits;
+hipError_t launch_adjust_logits(const qwen3_logits& l, const void* logits, void* out, hipStream_t s);
+
 // ---------------------------------------------------------------- orthogonalised updates
 constexpr int ORTHO_GROUPS = 12;   // shapes in one call
 constexpr int ORTHO_PARTS = 64;    // partial sums of squares per matrix

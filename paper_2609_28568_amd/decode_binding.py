@@ -1,0 +1,274 @@
+"""ctypes binding of what answers are generated with (include/qwen3_decode.h) in
+libgpt2_mi355x.so: a paged cache of keys and values, attention of new tokens
+over it, and the adjustment of logits before a token is chosen.
+
+Argument marshalling only: torch supplies the device buffers and the stream,
+everything runs in the library's HIP kernels. No call synchronises, so all of
+them can be captured into graphs: lengths, tables and counts are read on the
+device when a graph is replayed.
+"""
+from __future__ import annotations
+
+import ctypes
+
+from .binding import i32, on_stream
+from .qwen3_binding import _check, _device_rows, _ptr, lib as _lib_qwen3
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_layer", "n_kv_head", "head_dim", "page_size", "n_pages", "n_seq",
+                                              "max_pages")] + [
+        (n, ctypes.c_void_p) for n in ("d_pages", "d_table", "d_lens", "d_refs", "d_short", "d_scratch")]
+
+
+class Tree(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_head", "n_rows", "max_new", "layer", "mask_words")]
+
+
+class Logits(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "vocab", "dtype")] + [
+        (n, ctypes.c_int64) for n in ("logits_stride", "out_stride")] + [
+        (n, ctypes.c_int32) for n in ("n_seq", "history_stride", "path_len", "n_bias", "n_masks")] + [
+        (n, ctypes.c_void_p) for n in ("d_history", "d_prompt_lens", "d_lens", "d_row_seq", "d_path", "d_repetition",
+                                       "d_frequency", "d_presence", "d_bias_ids", "d_bias", "d_masks", "d_row_mask")]
+
+
+_lib = None
+
+
+def lib():
+    """The shared library with the prototypes of qwen3_decode.h declared."""
+    global _lib
+    if _lib is not None:
+        return _lib
+    L = _lib_qwen3()
+    P, I32, SIZE = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
+    cache, tree = ctypes.POINTER(Cache), ctypes.POINTER(Tree)
+    protos = {
+        "qwen3_cache_scratch": [cache, ctypes.POINTER(SIZE)],
+        "qwen3_cache_fork": [cache, P, P, P],
+        "qwen3_cache_append": [cache, P, I32, I32, SIZE, P, P, P, I32, P],
+        "qwen3_cache_compact": [cache, P],
+        "qwen3_tree_size": [cache, tree, ctypes.POINTER(SIZE)],
+        "qwen3_tree_attention": [cache, tree, P, P, P, P, P, P, SIZE, P],
+        "qwen3_adjust_logits": [ctypes.POINTER(Logits), P, P, P],
+    }
+    for name, args in protos.items():
+        f = getattr(L, name)
+        f.restype, f.argtypes = I32, args
+    _lib = L
+    return L
+
+
+class PagedCache:
+    """Keys and values of some sequences on pages that they may share
+    (qwen3_cache_*). Its calls run one after another, on the current stream;
+    the tensors are the caller's to read, and to save and restore."""
+
+    def __init__(self, pages, table, lens, refs, short):
+        """Over tensors that hold a cache: pages bf16 [n_layer, n_pages, 2,
+        n_kv_head, page_size, head_dim], table int32 [n_seq, max_pages], lens
+        int32 [n_seq], refs int32 [n_pages], short int32 [1] (qwen3_cache)."""
+        import torch
+        self.torch = torch
+        _device_rows(pages, "pages", torch.bfloat16)
+        if pages.dim() != 6 or pages.shape[2] != 2:
+            raise ValueError("pages are [n_layer, n_pages, 2, n_kv_head, page_size, head_dim]")
+        n_layer, n_pages, _, n_kv_head, page_size, head_dim = map(i32, pages.shape)
+        _device_rows(table, "table", torch.int32, pages)
+        if table.dim() != 2:
+            raise ValueError("the table is [n_seq, max_pages]")
+        n_seq, max_pages = map(i32, table.shape)
+        _device_rows(lens, "lens", torch.int32, pages, (n_seq,))
+        _device_rows(refs, "refs", torch.int32, pages, (n_pages,))
+        _device_rows(short, "short", torch.int32, pages, (1,))
+        self.pages, self.table, self.lens, self.refs, self.short = pages, table, lens, refs, short
+        c = Cache(n_layer, n_kv_head, head_dim, page_size, n_pages, n_seq, max_pages)
+        n = ctypes.c_size_t()
+        _check(lib().qwen3_cache_scratch(ctypes.byref(c), ctypes.byref(n)))
+        self.scratch = torch.empty(n.value, dtype=torch.uint8, device=pages.device)
+        for name in ("pages", "table", "lens", "refs", "short", "scratch"):
+            setattr(c, "d_" + name, getattr(self, name).data_ptr())
+        self._c, self._ref = c, ctypes.byref(c)
+        self._stream = torch.cuda.current_stream(pages.device).cuda_stream
+        self._trees = {}
+
+    @classmethod
+    def empty(cls, n_layer, n_pages, n_kv_head, page_size, head_dim, n_seq, max_pages, device="cuda"):
+        """A cache without tokens."""
+        import torch
+        new = lambda shape, v: torch.full(shape, v, dtype=torch.int32, device=device)   # noqa: E731
+        pages = torch.empty(n_layer, n_pages, 2, n_kv_head, page_size, head_dim, dtype=torch.bfloat16, device=device)
+        return cls(pages, new((n_seq, max_pages), -1), new((n_seq,), 0), new((n_pages,), 0), new((1,), 0))
+
+    def _run(self, fn, *args):
+        def call(*args):
+            if args[-1] != self._stream:   # the scratch is another stream's: it stays until this one is done with it
+                self.scratch.record_stream(self.torch.cuda.current_stream(self.pages.device))
+            return fn(self._ref, *args)
+        _check(on_stream(self.pages.device, call, *args))
+
+    def _ints(self, t, name, shape):
+        return _device_rows(t, name, self.torch.int32, self.pages, shape)
+
+    def fork(self, src, keep=None):
+        """Sequence s becomes the first keep[s] tokens (None: all) of what
+        sequence src[s] was; src[s] -1: it is freed (qwen3_cache_fork)."""
+        n = self._c.n_seq
+        self._ints(src, "src", (n,))
+        if keep is not None:
+            self._ints(keep, "keep", (n,))
+        self._run(lib().qwen3_cache_fork, src.data_ptr(), _ptr(keep))
+
+    def _rows(self, qkv, layers):
+        """(n_head, rows) of q | k | v rows of `layers` layers."""
+        c = self._c
+        _device_rows(qkv, "q | k | v", self.torch.bfloat16, self.pages)
+        if qkv.dim() != (2 if layers is None else 3) or (layers is not None and qkv.shape[0] != layers):
+            raise ValueError("rows of q | k | v are [rows, (n_head + 2 n_kv_head) head_dim], of every layer for append")
+        n_head = qkv.shape[-1] // c.head_dim - 2 * c.n_kv_head
+        if n_head < 1 or qkv.shape[-1] % c.head_dim:
+            raise ValueError("rows of q | k | v are (n_head + 2 n_kv_head) head_dim wide")
+        return i32(n_head), i32(qkv.shape[-2])
+
+    def append(self, qkv, starts, max_new, counts=None, path=None):
+        """Keys and values of new tokens, of all layers (qwen3_cache_append):
+        qkv bf16 [n_layer, rows, (n_head + 2 n_kv_head) head_dim], sequence s's
+        rows starts[s]..starts[s + 1] - 1, of which it takes the first
+        counts[s] (None: all), or those that path int32 [n_seq, max_new] names.
+        `short` then holds the number of pages that were missing; unless it is
+        0 nothing was appended."""
+        c = self._c
+        if qkv.dim() == 2:
+            qkv = qkv[None]
+        n_head, rows = self._rows(qkv, c.n_layer)
+        max_new = i32(max_new)
+        self._ints(starts, "starts", (c.n_seq + 1,))
+        if counts is not None:
+            self._ints(counts, "counts", (c.n_seq,))
+        if path is not None:
+            self._ints(path, "path", (c.n_seq, max_new))
+        self._run(lib().qwen3_cache_append, qkv.data_ptr(), n_head, rows, rows * qkv.shape[2], starts.data_ptr(),
+                  _ptr(counts), _ptr(path), max_new)
+
+    def compact(self):
+        """Moves the pages in use to the lowest numbers (qwen3_cache_compact)."""
+        self._run(lib().qwen3_cache_compact)
+
+    def _tree(self, n_head, rows, max_new, layer, words):
+        """The call's description and workspace bytes, made once per shape."""
+        key = n_head, rows, max_new, layer, words
+        got = self._trees.get(key)
+        if got is None:
+            t, n = Tree(*key), ctypes.c_size_t()
+            _check(lib().qwen3_tree_size(self._ref, ctypes.byref(t), ctypes.byref(n)))
+            if len(self._trees) >= 256:
+                self._trees.clear()
+            got = self._trees[key] = ctypes.byref(t), n.value
+        return got
+
+    def attention(self, qkv, starts, max_new, mask=None, layer=0, out=None, lse=None):
+        """(out [rows, n_head head_dim] bf16, lse [n_head, rows] fp32) of new
+        tokens' rows qkv bf16 [rows, (n_head + 2 n_kv_head) head_dim] over one
+        layer of the cache and among themselves (qwen3_tree_attention): without
+        a mask in order, with mask int32 [rows, words] (tree_mask) as its bits
+        say. Sequence s's rows are starts[s]..starts[s + 1] - 1, max_new at
+        most."""
+        torch, c = self.torch, self._c
+        n_head, rows = self._rows(qkv, None)
+        self._ints(starts, "starts", (c.n_seq + 1,))
+        words = 0
+        if mask is not None:
+            if mask.dim() != 2:
+                raise ValueError("a mask is [rows, words]")
+            words = i32(mask.shape[1])
+            self._ints(mask, "mask", (rows, words))
+        tree, nbytes = self._tree(n_head, rows, i32(max_new), i32(layer), words)
+        shapes = (rows, n_head * c.head_dim), (n_head, rows)
+        out = (qkv.new_empty(shapes[0]) if out is None
+               else _device_rows(out, "out", torch.bfloat16, self.pages, shapes[0]))
+        lse = (qkv.new_empty(shapes[1], dtype=torch.float32) if lse is None
+               else _device_rows(lse, "lse", torch.float32, self.pages, shapes[1]))
+        work = torch.empty(nbytes, dtype=torch.uint8, device=qkv.device)
+        _check(on_stream(self.pages.device, lib().qwen3_tree_attention, self._ref, tree, qkv.data_ptr(),
+                         starts.data_ptr(), _ptr(mask), out.data_ptr(), lse.data_ptr(), work.data_ptr(), nbytes))
+        return out, lse
+
+
+def tree_mask(parents, device="cuda"):
+    """The mask of trees of drafted tokens for PagedCache.attention: parents, a
+    list for each sequence with the place of every token's parent among the
+    sequence's tokens before it, or -1."""
+    import numpy as np
+    import torch
+    words = max([(len(p) + 31) // 32 for p in parents] + [1])
+    out = np.zeros((sum(map(len, parents)), words), np.uint32)
+    at = 0
+    for p in parents:
+        for i, up in enumerate(p):
+            if not -1 <= up < i:
+                raise ValueError(f"the parent of token {i} must be -1 or a token before it")
+            if up >= 0:
+                out[at + i] = out[at + up]
+            out[at + i, i // 32] |= np.uint32(1 << (i % 32))
+        at += len(p)
+    return torch.from_numpy(out.view(np.int32)).to(device)
+
+
+def adjust_logits(logits, history=None, prompt_lens=None, lens=None, repetition=None, frequency=None, presence=None,
+                  *, row_seq=None, path=None, bias_ids=None, bias=None, masks=None, row_mask=None, out=None):
+    """Penalties for repeated tokens, biases and grammar masks on logits bf16 or
+    fp32 [rows, vocab], whose rows may be further apart (qwen3_adjust_logits).
+    history int32 [n_seq, longest], lens and prompt_lens int32 [n_seq] (the
+    tokens that count as repeated begin behind the prompt), row_seq int32 [rows]
+    each row's sequence; path int32 [rows, k] a row's own further tokens, -1
+    where there is none; repetition, frequency and presence fp32 [rows]; bias_ids
+    int32 and bias fp32 [rows, k]; masks int32 [n_masks, ceil(vocab / 32)], a bit
+    for each allowed token, and row_mask int32 [rows], -1 for no mask. On the
+    current stream; out may be logits."""
+    import torch
+    if not (isinstance(logits, torch.Tensor) and logits.is_cuda and logits.dim() == 2
+            and logits.dtype in (torch.bfloat16, torch.float32) and (logits.stride(1) == 1 or logits.shape[1] == 1)
+            and logits.shape[1] > 0):
+        raise ValueError("logits are a bf16 or fp32 device tensor [rows, vocab] whose columns are contiguous")
+    rows, vocab = logits.shape
+    if out is None:
+        out = torch.empty(rows, vocab, dtype=logits.dtype, device=logits.device)
+    elif (out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device
+          or (out.stride(1) != 1 and vocab > 1)):
+        raise ValueError("out must have the logits' shape, type and device, its columns contiguous")
+
+    def given(t, name, dtype, shape):
+        return None if t is None else _device_rows(t, name, dtype, logits, shape).data_ptr()
+
+    I, F = torch.int32, torch.float32
+    n_seq = stride = path_len = n_bias = n_masks = 0
+    if history is not None:
+        _device_rows(history, "history", I, logits)
+        if history.dim() != 2 or lens is None:
+            raise ValueError("a history is [n_seq, longest], with lens")
+        n_seq, stride = history.shape
+    if path is not None:
+        if path.dim() != 2:
+            raise ValueError("a path is [rows, k]")
+        path_len = path.shape[1]
+    if bias is not None or bias_ids is not None:
+        if bias is None or bias_ids is None or bias.dim() != 2:
+            raise ValueError("bias and bias_ids go together, [rows, k]")
+        n_bias = bias.shape[1]
+    if masks is not None:
+        if masks.dim() != 2:
+            raise ValueError("masks are [n_masks, ceil(vocab / 32)]")
+        n_masks = masks.shape[0]
+    step = lambda t: t.stride(0) if rows > 1 else vocab   # noqa: E731
+    desc = Logits(i32(rows), i32(vocab), int(logits.dtype == torch.bfloat16), step(logits), step(out), i32(n_seq),
+                  i32(stride), i32(path_len), i32(n_bias), i32(n_masks),
+                  history.data_ptr() if history is not None and history.numel() else None,
+                  given(prompt_lens, "prompt_lens", I, (n_seq,)), given(lens, "lens", I, (n_seq,)),
+                  given(row_seq, "row_seq", I, (rows,)), given(path, "path", I, (rows, path_len)),
+                  given(repetition, "repetition", F, (rows,)), given(frequency, "frequency", F, (rows,)),
+                  given(presence, "presence", F, (rows,)), given(bias_ids, "bias_ids", I, (rows, n_bias)),
+                  given(bias, "bias", F, (rows, n_bias)), given(masks, "masks", I, (n_masks, (vocab + 31) // 32)),
+                  given(row_mask, "row_mask", I, (rows,)))
+    _check(on_stream(logits.device, lib().qwen3_adjust_logits, ctypes.byref(desc), logits.data_ptr(), out.data_ptr()))
+    return out

@@ -1,0 +1,181 @@
+"""The adjustment of logits on the GPU against its definition in 64 bits, entry
+by entry.
+
+Tolerances. With x the logit and y each step's result: the quotient or product,
+the penalties' product and sum, their difference and the bias are an fp32
+rounding each (2^-24 of its result at most), and the result is rounded once
+(bf16 2^-8, fp32 2^-24):
+  |error| <= round(out) |out| + 2^-24 (|y1| + 3 (|f| count + |p|) + |y2| + |y3|) (1 + 2^-20)
+with the bound of the rounding taken at the exact result plus that error."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+def db():
+    from paper_2609_28568_amd import decode_binding
+    return decode_binding
+
+
+def dev(a):
+    return None if a is None else torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+CASES = {
+    # rows, vocab, stride, dtype, sequences, history, path, biases, masks
+    "one_of_everything": (1, 1, 1, "float32", 1, 1, 1, 1, 1),
+    "one_row": (1, 50257, 50304, "bfloat16", 1, 203, 0, 0, 0),
+    "odd_stride": (5, 4099, 4101, "bfloat16", 5, 70, 0, 9, 2),
+    "odd_stride_fp32": (5, 4099, 4103, "float32", 3, 70, 4, 9, 2),
+    "narrow": (9, 37, 37, "bfloat16", 2, 500, 3, 5, 4),
+    "several_pieces": (7, 20000, 20000, "float32", 7, 3000, 0, 300, 0),
+    "rows_of_drafts": (48, 512, 512, "float32", 4, 1000, 11, 0, 3),
+    "long_history": (3, 50257, 50257, "bfloat16", 3, 30001, 2, 1, 1),
+    "masks_alone": (6, 3001, 3008, "bfloat16", 0, 0, 0, 0, 5),
+    "biases_alone": (6, 3001, 3008, "float32", 0, 0, 0, 1024, 0),
+    "path_alone": (6, 3001, 3008, "float32", 0, 0, 30, 0, 0),
+    "wide_batch": (33, 151936, 151936, "bfloat16", 33, 2500, 0, 64, 5),
+    "nothing": (3, 2048, 2048, "bfloat16", 0, 0, 0, 0, 0),
+}
+
+
+def inputs(name, seed=4):
+    rows, vocab, stride, dtype, n_seq, history, path, n_bias, n_masks = CASES[name]
+    g = np.random.default_rng(seed)
+    x = torch.from_numpy((g.standard_normal((rows, stride)) * 4).astype(np.float32)).to(getattr(torch, dtype))
+    if vocab > 8:
+        x[0, :8] = torch.tensor([0.0, -0.0, float("inf"), -float("inf"), 3e38, -3e38, 1e-40, 0.0])
+    a = dict.fromkeys(("history", "prompt_lens", "lens", "row_seq", "path", "bias_ids", "bias", "masks", "row_mask"))
+    ids = lambda shape: np.where(g.random(shape) < 0.05, g.choice([-1, vocab, 2 ** 31 - 1, -2 ** 31], shape),   # noqa: E731
+                                 np.minimum(vocab ** g.random(shape) - 1, vocab - 1)).astype(np.int32)
+    if n_seq:
+        a["history"] = ids((n_seq, history))
+        a["lens"] = g.integers(0, history + 1, n_seq).astype(np.int32)
+        a["lens"][0] = history
+        a["prompt_lens"] = (a["lens"] * g.random(n_seq)).astype(np.int32)
+        a["row_seq"] = g.integers(-1, n_seq + 1, rows).astype(np.int32)   # some rows without a history
+        a["row_seq"][0] = 0
+    if path:
+        a["path"] = ids((rows, path))
+    if n_bias:
+        a["bias_ids"], a["bias"] = ids((rows, n_bias)), g.standard_normal((rows, n_bias)).astype(np.float32) * 3
+    if n_masks:
+        a["masks"] = g.integers(-2 ** 31, 2 ** 31, (n_masks, (vocab + 31) // 32)).astype(np.int32)
+        a["masks"][0] = 0   # nothing allowed
+        a["row_mask"] = g.integers(-1, n_masks + 1, rows).astype(np.int32)
+        a["row_mask"][-1] = 0
+    for k, lo, hi in (("repetition", 0.7, 1.6), ("frequency", -0.3, 0.8), ("presence", -0.5, 0.9)):
+        a[k] = g.uniform(lo, hi, rows).astype(np.float32)
+    return x, a
+
+
+def reference(x, a, vocab):
+    """(result, bound before the last rounding) in float64."""
+    x = x.double().numpy()[:, :vocab]
+    out, bound = x.copy(), np.zeros_like(x)
+    for r in range(len(x)):
+        seen, count = np.zeros(vocab, bool), np.zeros(vocab)
+        if a["history"] is not None and 0 <= a["row_seq"][r] < len(a["history"]):
+            s = a["row_seq"][r]
+            for i, v in enumerate(a["history"][s, :a["lens"][s]]):
+                if 0 <= v < vocab:
+                    seen[v] = True
+                    count[v] += i >= a["prompt_lens"][s]
+        if a["path"] is not None:
+            for v in a["path"][r]:
+                if 0 <= v < vocab:
+                    seen[v] = True
+                    count[v] += 1
+        one = lambda k, d: float(a[k][r]) if a[k] is not None else d   # noqa: E731
+        rep, f, p = one("repetition", 1.0), one("frequency", 0.0), one("presence", 0.0)
+        y = np.where(seen, np.where(x[r] > 0, x[r] / rep, x[r] * rep), x[r])
+        e = np.where(seen, np.abs(y), 0)
+        y = np.where(count > 0, y - (f * count + p), y)
+        e += np.where(count > 0, 3 * (abs(f) * count + abs(p)) + np.abs(y), 0)
+        if a["bias"] is not None:
+            last = {v: b for v, b in zip(a["bias_ids"][r], a["bias"][r]) if 0 <= v < vocab}
+            at = np.fromiter(last, int, len(last))
+            y[at] += np.fromiter(last.values(), float, len(last))
+            e[at] += np.abs(y[at])
+        if a["masks"] is not None and 0 <= a["row_mask"][r] < len(a["masks"]):
+            m = np.unpackbits(a["masks"][a["row_mask"][r]].view(np.uint8), bitorder="little")[:vocab] > 0
+            y[~m] = -np.inf
+        out[r], bound[r] = y, 2.0 ** -24 * (1 + 2.0 ** -20) * e
+    return out, bound
+
+
+def adjust(x, a, **over):
+    return db().adjust_logits(x, **{k: dev(v) for k, v in a.items()}, **over)
+
+
+def check(y, want, bound, dtype):
+    y, eps = y.double().cpu().numpy(), 2.0 ** -8 if dtype == "bfloat16" else 2.0 ** -24
+    # past the type's range a value may round to infinity, or stay its largest
+    top = 2.0 ** 128 * (1 - (2.0 ** -8 if dtype == "bfloat16" else 2.0 ** -24))
+    with np.errstate(invalid="ignore", over="ignore"):
+        ok = (y == want) | (np.abs(y - want) <= eps * (np.abs(want) + bound) + bound + 2.0 ** -133)
+        ok |= np.isinf(y) & (np.sign(y) == np.sign(want)) & (np.abs(want) >= top * (1 - 2 * eps))
+    assert np.all(ok), np.argwhere(~ok)[:5]
+
+
+@pytest.mark.parametrize("name", list(CASES))
+def test_against_the_definition(name):
+    print(f"{name}: {CASES[name]}", flush=True)
+    rows, vocab, stride, dtype = CASES[name][:4]
+    x, a = inputs(name)
+    want, bound = reference(x, a, vocab)
+    full = x.cuda()
+    y = adjust(full[:, :vocab], a)
+    torch.cuda.synchronize()
+    check(y, want, bound, dtype)
+    assert torch.equal(full.cpu().view(torch.uint8), x.view(torch.uint8))
+    # in place: the same bits, and nothing behind the columns is touched
+    z = adjust(full[:, :vocab], a, out=full[:, :vocab])
+    assert z.data_ptr() == full.data_ptr()
+    raw = torch.int16 if dtype == "bfloat16" else torch.int32
+    assert torch.equal(z.contiguous().view(raw), y.view(raw))
+    assert torch.equal(full.cpu()[:, vocab:], x[:, vocab:])
+
+
+def test_without_penalties_the_bits_stay():
+    x, a = inputs("nothing")
+    for k in ("repetition", "frequency", "presence"):
+        a[k] = None
+    y = adjust(x.cuda(), a)
+    assert torch.equal(y.cpu().view(torch.int16), x.view(torch.int16))
+
+
+def test_a_row_with_nothing_allowed_is_minus_infinity():
+    x, a = inputs("masks_alone")
+    y = adjust(x.cuda()[:, :3001], a)
+    assert bool((y[-1] == -float("inf")).all())
+
+
+def test_the_last_entry_of_a_token_counts():
+    x = torch.zeros(2, 100, device="cuda")
+    ids = dev(np.array([[5, 7, 5, 5], [7, 7, 99, -1]], np.int32))
+    values = dev(np.array([[1, 2, 3, 4], [5, 6, 7, 8]], np.float32))
+    y = db().adjust_logits(x, bias_ids=ids, bias=values)
+    want = torch.zeros(2, 100)
+    want[0, 5], want[0, 7], want[1, 7], want[1, 99] = 4, 2, 6, 7
+    assert torch.equal(y.cpu(), want)
+
+
+def test_no_rows():
+    assert db().adjust_logits(torch.empty(0, 50, device="cuda")).shape == (0, 50)
+
+
+def test_rows_past_4_gib():
+    rows, vocab, stride = 9, 50257, 1 << 28   # 4.5 GiB of bf16 rows
+    x = torch.zeros(rows * stride, dtype=torch.bfloat16, device="cuda").view(rows, stride)[:, :vocab]
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x.copy_(torch.randn(rows, vocab, generator=g, device="cuda"))
+    history = torch.randint(0, vocab, (rows, 300), generator=g, device="cuda").int()
+    how = dict(history=history, lens=torch.full((rows,), 300, dtype=torch.int32, device="cuda"),
+               repetition=torch.full((rows,), 1.3, device="cuda"), presence=torch.full((rows,), 0.5, device="cuda"))
+    y = db().adjust_logits(x, **how)
+    assert torch.equal(db().adjust_logits(x.contiguous(), **how), y)
+    db().adjust_logits(x, **how, out=x)
+    assert torch.equal(x, y)
