@@ -6,20 +6,21 @@
 // through the page table, then the sequence's new ones from the rows themselves,
 // masked by the rows' words or by order. One walk of a block of rows over all its
 // tiles is a segment; segments of all sequences, heads and blocks follow one
-// another in one line of tiles, which is cut into equal shares, one a workgroup,
-// whatever the lengths are. They are on the device, so each workgroup finds its
+// another in one line of tiles, which is cut into equal shares, one a worker,
+// whatever the lengths are. They are on the device, so each worker finds its
 // share from them by itself; with more than 64 sequences a launch before sums
 // them up. A segment that is cut leaves partial results (fp32 O, maximum, sum)
 // that a second launch joins, in order, so runs repeat bit for bit.
 //
-// With 32 rows or fewer a sequence and head a workgroup is one wave, with a ring
-// of its own in LDS and no barriers; five of them share a CU, 80 KiB of loads in
-// flight. More rows take four waves, 128 rows, that share their tiles.
+// A workgroup's four waves are RB blocks of 32 rows times 4/RB groups that walk a
+// share's tiles in turn and merge at a segment's end. With one block of rows and
+// many segments each wave is a worker of its own instead, without barriers.
 //
 // A page's tile rows come through a buffer descriptor that ends with the
 // sequence's last token, so that what a page holds behind it reads as zeros, and
-// with nothing where the table names no page. Values of drafted tokens that are
-// not finite are taken out of the tile and added for the rows that see them only.
+// with nothing where the table names no page. Elements of drafted tokens' values
+// that are not finite are taken out of the product and added for the rows that
+// see them only.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -30,16 +31,19 @@
 
 namespace {
 
-// Workgroups' waves, keys of a tile, and workgroups that run at a time.
-template <int HD, int TEAM>
+// Keys of a tile, and how the line of tiles is shared out.
+template <int HD, int RB>
 struct Walk {
-  static constexpr int KT = TEAM == 1 && HD == 128 ? 32 : 64;
-  static constexpr int ROWS = 32 * TEAM, HEAD = HD;
+  static constexpr int HEAD = HD, ROWS = 32 * RB, GROUPS = 4 / RB;
+  static constexpr int KT = HD == 128 && RB < 4 ? 32 : 64;
   static constexpr int TB = KT * HD * 2;        // bytes of a tile of keys
   static constexpr int STAGES = 2;
-  static constexpr int LDS = STAGES * 2 * TB;
-  static constexpr int SHARES = 256 * (TEAM == 1 ? 5 : 2);
-  static constexpr int LEAST = 4;               // tiles of a share
+  static constexpr int RING = STAGES * 2 * TB;  // of a group
+  static constexpr int KEEP = HD * 32 * 4 + 512;   // a wave's O, maxima and sums
+  static constexpr int LEAST = 4;               // tiles of a share; segments of no more are never cut
+  static constexpr int TEAMS = 256 * (RB == 1 ? 1 : 2);   // workgroups that run at a time
+  static constexpr int MOST = RB == 1 ? 4 * TEAMS : TEAMS;   // shares
+  static_assert((GROUPS - 1) * RB * KEEP <= GROUPS * RING, "the groups' results fit their tiles' space");
 };
 // Rows of a partial result, and its floats: O [rows][hd], maxima, sums.
 __host__ DEV int part_rows(const TreeArgs& a, int rows) {
@@ -55,73 +59,104 @@ struct Seq {
   int len, start, n;
   int tc, t, blocks;   // tiles of cached keys, of a segment; blocks of rows
 };
-template <int KT, int ROWS>
-DEV Seq seq_of(const TreeArgs& a, int s) {
+template <class W>
+DEV Seq seq_from(const TreeArgs& a, int len, int start, int n) {
   Seq q;
-  q.len = clampi(a.lens[s], 0, a.max_pages * a.ps);
-  q.start = clampi(a.starts[s], 0, a.n_rows);
-  q.n = min(clampi(a.starts[s + 1], q.start, a.n_rows) - q.start, a.max_new);
-  q.tc = (q.len + KT - 1) / KT;
-  q.t = q.tc + (q.n + KT - 1) / KT;
-  q.blocks = (q.n * (a.H / a.Hkv) + ROWS - 1) / ROWS;
+  q.len = len;
+  q.start = start;
+  q.n = n;
+  q.tc = (len + W::KT - 1) / W::KT;
+  q.t = q.tc + (n + W::KT - 1) / W::KT;
+  q.blocks = (n * (a.H / a.Hkv) + W::ROWS - 1) / W::ROWS;
   return q;
 }
-
-DEV int wave_scan(int x) {   // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(x, o);
-    if (lane >= o) x += y;
-  }
-  return x;
+template <class W>
+DEV Seq seq_of(const TreeArgs& a, int s) {
+  const int start = clampi(a.starts[s], 0, a.n_rows);
+  return seq_from<W>(a, clampi(a.lens[s], 0, a.max_pages * a.ps), start,
+                     min(clampi(a.starts[s + 1], start, a.n_rows) - start, a.max_new));
 }
 
-// plan[s]: tiles before sequence s, s <= n_seq
-template <int KT, int ROWS>
+// v plus v of the lane that CTRL names, in the rows of ROWS
+template <int CTRL, int ROWS>
+DEV int add_dpp(int v) {
+  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, true);
+}
+// over the lanes up to each: shifts within rows of 16, then rows' last lanes to the rows behind
+DEV int wave_scan(int v) {
+  v = add_dpp<0x111, 0xf>(v);
+  v = add_dpp<0x112, 0xf>(v);
+  v = add_dpp<0x114, 0xf>(v);
+  v = add_dpp<0x118, 0xf>(v);
+  v = add_dpp<0x142, 0xa>(v);
+  return add_dpp<0x143, 0xc>(v);
+}
+
+// plan[s]: tiles before sequence s, s <= n_seq; plan[n_seq + 1]: segments
+template <class W>
 __global__ __launch_bounds__(64) void tree_plan_kernel(TreeArgs a) {
   const int lane = threadIdx.x;
-  int before = 0;
+  int before = 0, segments = 0;
   for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
-    int u = 0;
+    int u = 0, n = 0;
     if (s0 + lane < a.n_seq) {
-      const Seq q = seq_of<KT, ROWS>(a, s0 + lane);
-      u = q.t * q.blocks * a.Hkv;
+      const Seq q = seq_of<W>(a, s0 + lane);
+      n = q.blocks * a.Hkv;
+      u = q.t * n;
     }
     const int x = wave_scan(u);
     if (s0 + lane < a.n_seq) a.plan[s0 + lane] = before + x - u;
     before += __builtin_amdgcn_readlane(x, 63);
+    segments += __builtin_amdgcn_readlane(wave_scan(n), 63);
   }
-  if (lane == 0) a.plan[a.n_seq] = before;
+  if (lane == 0) {
+    a.plan[a.n_seq] = before;
+    a.plan[a.n_seq + 1] = segments;
+  }
 }
 
-// A cut this near a segment's end goes there: segments of up to `least` tiles
-// are never cut, and few tiles are left on one side of a cut.
-DEV int cut_slack(int share, int least) { return share <= 2 * least ? share / 2 : max(least / 2, share / 8); }
+// How the line is cut: whether every wave is a worker, a share's tiles, and how
+// near a segment's end a cut goes there instead (segments of LEAST tiles are
+// never cut, and few tiles are left on one side of a cut).
+struct Cuts {
+  bool solo;
+  int share, slack;
+};
+template <class W>
+DEV Cuts cuts_of(int total, int segments) {
+  Cuts c;
+  c.solo = W::GROUPS == 4 && segments > W::TEAMS && total > 8 * W::TEAMS;
+  const int shares = c.solo ? W::MOST : W::TEAMS;
+  c.share = max(W::LEAST, (total + shares - 1) / shares);
+  c.slack = c.share <= 2 * W::LEAST ? c.share / 2 : max(W::LEAST / 2, c.share / 8);
+  return c;
+}
 
-// The line of tiles. Up to 64 sequences: lane s holds the tiles before sequence
-// s, summed up here. More: they are in plan.
-template <int KT, int ROWS>
+// The line of tiles. Up to 64 sequences: lane s has sequence s and the tiles
+// before it. More: they are in plan.
+template <class W>
 struct Line {
-  int base, total, share, slack;
+  int base, len, start, n, total, segments;
   bool planned;
-  DEV void init(const TreeArgs& a, int shares, int least) {
+  Cuts cuts;
+  DEV void init(const TreeArgs& a) {
     const int lane = threadIdx.x & 63;
     planned = a.n_seq > 64;
     if (planned) {
       total = __builtin_amdgcn_readfirstlane(a.plan[a.n_seq]);
+      segments = __builtin_amdgcn_readfirstlane(a.plan[a.n_seq + 1]);
     } else {
-      int u = 0;
-      if (lane < a.n_seq) {
-        const Seq q = seq_of<KT, ROWS>(a, lane);
-        u = q.t * q.blocks * a.Hkv;
-      }
-      const int x = wave_scan(u);
+      Seq q{};
+      if (lane < a.n_seq) q = seq_of<W>(a, lane);
+      len = q.len;
+      start = q.start;
+      n = q.n;
+      const int u = q.t * q.blocks * a.Hkv, x = wave_scan(u);
       base = x - u;
       total = __builtin_amdgcn_readlane(x, 63);
+      segments = __builtin_amdgcn_readlane(wave_scan(q.blocks * a.Hkv), 63);
     }
-    share = max(least, (total + shares - 1) / shares);
-    slack = cut_slack(share, least);
+    cuts = cuts_of<W>(total, segments);
   }
   // the sequence that has tile p < total, and the tiles before it
   DEV int find(const TreeArgs& a, int p, int* before) const {
@@ -140,25 +175,29 @@ struct Line {
     *before = __builtin_amdgcn_readlane(b, last);
     return k + last;
   }
-  // where the cut at tile p is made, p in the segment [from, from + t)
-  DEV int cut(int p, int from, int t) const {
-    return p - from <= slack ? from : from + t - p <= slack ? from + t : p;
+  DEV Seq seq(const TreeArgs& a, int s) const {
+    if (!planned)
+      return seq_from<W>(a, __builtin_amdgcn_readlane(len, s), __builtin_amdgcn_readlane(start, s),
+                         __builtin_amdgcn_readlane(n, s));
+    const Seq q = seq_of<W>(a, s);
+    return seq_from<W>(a, __builtin_amdgcn_readfirstlane(q.len), __builtin_amdgcn_readfirstlane(q.start),
+                       __builtin_amdgcn_readfirstlane(q.n));
   }
+  // where share w begins
   DEV int bound(const TreeArgs& a, int w) const {
-    const int p = w * share;   // below total + share
+    const int p = w * cuts.share;   // below total + share
     if (p >= total) return total;
     int before;
     const int s = find(a, p, &before);
-    const Seq q = seq_of<KT, ROWS>(a, s);
-    const int from = before + (p - before) / q.t * q.t;
-    return cut(p, from, q.t);
+    const int t = seq(a, s).t, from = before + (p - before) / t * t;
+    return p - from <= cuts.slack ? from : from + t - p <= cuts.slack ? from + t : p;
   }
 };
 
-// Keys and values of one segment, tile by tile into a wave's (or team's) ring.
-template <int HD, int TEAM>
+// Keys and values of one segment, tile by tile into a group's ring.
+template <int HD, int RB>
 struct Keys {
-  using W = Walk<HD, TEAM>;
+  using W = Walk<HD, RB>;
   static constexpr int U = HD / 8, PER = 16 * U / 64;   // 16-byte units of a row; loads of 16 rows
   const TreeArgs* a;
   const int32_t* table;     // the sequence's
@@ -168,10 +207,9 @@ struct Keys {
   size_t head;              // bytes of the heads before this one
   int len, n, tc, lps;
   int win, ids;             // the lane's entry of the table, pages win..win+63
-  uint32_t rel[PER], reld[PER];   // the lane's byte offset in 16 rows of a page, of new tokens
   uint64_t seen;            // of the last tile issued: keys that are there
 
-  DEV void init(const TreeArgs& args, int s, const Seq& q, int j, int lane) {
+  DEV void init(const TreeArgs& args, int s, const Seq& q, int j) {
     a = &args;
     table = args.table + (size_t)s * args.max_pages;
     const int slots = args.H + 2 * args.Hkv;
@@ -185,16 +223,18 @@ struct Keys {
     tc = q.tc;
     lps = 31 - __builtin_clz(args.ps);
     win = -64;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int u = i * 64 + lane, row = u / U, c = unit<HD>(row, u % U) - row * U;   // the XOR is its own inverse
-      rel[i] = (uint32_t)(row * HD + c * 8) * 2u;
-      reld[i] = (uint32_t)row * ld + (uint32_t)c * 16u;
-    }
   }
 
-  DEV void issue(int f, lds_char_t* st, int wave, int lane) {
-    constexpr int GROUPS = W::KT / 16;
+  // the lane's part of load i of 16 rows that are `stride` bytes apart
+  static DEV uint32_t offset(int i, int lane, uint32_t stride) {
+    const int u = i * 64 + lane, row = u / U, c = unit<HD>(row, u % U) - row * U;   // the XOR is its own inverse
+    return (uint32_t)row * stride + (uint32_t)c * 16u;
+  }
+  // by the waves of a group, `wave` of RB
+  DEV void issue(int f, lds_char_t* st, int wave) {
+    constexpr int SIXTEENS = W::KT / 16;
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));   // offsets are made again for each tile: kept, they would leave too few registers
     seen = 0;
     if (f < tc) {
       const int p0 = f * W::KT >> lps, p1 = (f * W::KT + W::KT - 1) >> lps;
@@ -202,90 +242,106 @@ struct Keys {
         win = p0;
         ids = table[min(p0 + lane, a->max_pages - 1)];
       }
+      auto page_of = [&](int key) { return __builtin_amdgcn_readlane(ids, (key >> lps) - win); };
 #pragma unroll
-      for (int q = 0; q < GROUPS; ++q) {
+      for (int q = 0; q < SIXTEENS; ++q) {
         const int key = f * W::KT + 16 * q;
-        const int page = __builtin_amdgcn_readlane(ids, (key >> lps) - win);
-        const int there = (unsigned)page < (unsigned)a->n_pages ? clampi(len - key, 0, 16) : 0;
+        const int there = (unsigned)page_of(key) < (unsigned)a->n_pages ? clampi(len - key, 0, 16) : 0;
         seen |= (uint64_t)((1u << there) - 1u) << (16 * q);
-        if (q % TEAM != wave % GROUPS % TEAM) continue;
-        const char* k = reinterpret_cast<const char*>(a->pages) + (size_t)(there ? page : 0) * page_bytes + head +
+      }
+#pragma unroll 1
+      for (int q = wave; q < SIXTEENS; q += RB) {
+        const int key = f * W::KT + 16 * q, there = __builtin_popcount((uint32_t)(seen >> (16 * q)) & 0xffffu);
+        const char* k = reinterpret_cast<const char*>(a->pages) + (size_t)(there ? page_of(key) : 0) * page_bytes + head +
                         (size_t)(key & (a->ps - 1)) * HD * 2;
         const v4i32 rk = make_rsrc(k, (uint32_t)there * HD * 2), rv = make_rsrc(k + v_bytes, (uint32_t)there * HD * 2);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-          dma16(rk, rel[i], lds_addr(st + (q * PER + i) * 1024));
-          dma16(rv, rel[i], lds_addr(st + W::TB + (q * PER + i) * 1024));
+          dma16(rk, offset(i, lane, HD * 2), lds_addr(st + (q * PER + i) * 1024));
+          dma16(rv, offset(i, lane, HD * 2), lds_addr(st + W::TB + (q * PER + i) * 1024));
         }
       }
     } else {
       const int d0 = (f - tc) * W::KT;
-#pragma unroll
-      for (int q = 0; q < GROUPS; ++q) {
+      seen = n - d0 >= 64 ? ~0ull : (1ull << max(n - d0, 0)) - 1;
+      if constexpr (W::KT < 64) seen &= (1ull << W::KT) - 1;
+#pragma unroll 1
+      for (int q = wave; q < SIXTEENS; q += RB) {
         const int there = clampi(n - d0 - 16 * q, 0, 16);
-        seen |= (uint64_t)((1u << there) - 1u) << (16 * q);
-        if (q % TEAM != wave % GROUPS % TEAM) continue;
         const char* k = reinterpret_cast<const char*>(rows) + (there ? (size_t)(d0 + 16 * q) * ld : 0);
         const uint32_t bytes = there ? (there - 1) * ld + HD * 2 : 0;
         const v4i32 rk = make_rsrc(k, bytes), rv = make_rsrc(k + (size_t)a->Hkv * HD * 2, bytes);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-          dma16(rk, reld[i], lds_addr(st + (q * PER + i) * 1024));
-          dma16(rv, reld[i], lds_addr(st + W::TB + (q * PER + i) * 1024));
+          dma16(rk, offset(i, lane, ld), lds_addr(st + (q * PER + i) * 1024));
+          dma16(rv, offset(i, lane, ld), lds_addr(st + W::TB + (q * PER + i) * 1024));
         }
       }
     }
   }
 };
 
-// Rows of a tile of values with an element that is not finite.
-template <int HD, int KT>
-DEV uint64_t not_finite(const lds_char_t* vs, int lane) {
+DEV bool special(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
+// Of 32 rows of values, those with an element that is not finite.
+template <int HD>
+DEV uint32_t not_finite(const lds_char_t* vs, int lane) {
   constexpr int U = HD / 8;
-  uint64_t bad = 0;
+  uint32_t bad = 0;
 #pragma unroll 4
-  for (int i = 0; i < KT * U / 64; ++i) {
-    const uint4 x = __builtin_bit_cast(uint4, *reinterpret_cast<const lds_v4u32_t*>(vs + (i * 64 + lane) * 16));
-    auto special = [](uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; };
+  for (int i = 0; i < U / 2; ++i) {
+    const v4u32 x = *reinterpret_cast<const lds_v4u32_t*>(vs + (i * 64 + lane) * 16);
     const uint64_t hit = __ballot(special(x.x) || special(x.y) || special(x.z) || special(x.w));
     if (hit) {
 #pragma unroll
       for (int r = 0; r < 64 / U; ++r)
-        if (hit >> (r * U) & ((1ull << U) - 1)) bad |= 1ull << (i * (64 / U) + r);
+        if (hit >> (r * U) & ((1ull << U) - 1)) bad |= 1u << (i * (64 / U) + r);
     }
   }
   return bad;
 }
-
-template <int HD, int TEAM>
-__global__ __launch_bounds__(64 * TEAM, 2) void tree_kernel(TreeArgs a) {
-  using W = Walk<HD, TEAM>;
-  using S = Shape<HD>;
-  constexpr int KT = W::KT, NT = KT / 32;
-  __shared__ __attribute__((aligned(1024))) char smem_raw[W::LDS];
-  lds_char_t* smem = (lds_char_t*)smem_raw;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int lq = lane & 31, g = lane >> 5, me = blockIdx.x, G = a.H / a.Hkv;
-  const float sc = LOG2E / sqrtf((float)HD);
-  Line<KT, W::ROWS> line;
-  line.init(a, W::SHARES, W::LEAST);
-  if (me == 0 && wave == 0 && !line.planned) {   // for the launch that joins
-    if (lane < a.n_seq) a.plan[lane] = line.base;
-    if (lane == 0) a.plan[a.n_seq] = line.total;
+// ... and without them.
+DEV bf16x8 finite(bf16x8 v) {
+  v4u32 x = __builtin_bit_cast(v4u32, v);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if ((x[k] & 0x7f80u) == 0x7f80u) x[k] &= 0xffff0000u;
+    if ((x[k] & 0x7f800000u) == 0x7f800000u) x[k] &= 0xffffu;
   }
-  if ((long)me * line.share >= line.total) return;
+  return __builtin_bit_cast(bf16x8, x);
+}
+
+DEV float inverse(float l) { return l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l; }   // a row that sees nothing: 0
+
+template <int HD, int RB>
+__global__ __launch_bounds__(256, RB == 1 ? 1 : 2) void tree_kernel(TreeArgs a) {
+  using W = Walk<HD, RB>;
+  using S = Shape<HD>;
+  constexpr int KT = W::KT;
+  __shared__ __attribute__((aligned(1024))) char smem_raw[W::GROUPS * W::RING];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lq = lane & 31, g = lane >> 5, G = a.H / a.Hkv;
+  const int rw = wave % RB, group = wave / RB;   // block of 32 rows, group of the workgroup
+  lds_char_t* ring = (lds_char_t*)smem_raw + group * W::RING;
+  const float sc = LOG2E / sqrtf((float)HD);
+  Line<W> line;
+  line.init(a);
+  if (blockIdx.x == 0 && wave == 0 && !line.planned) {   // for the launch that joins
+    if (lane < a.n_seq) a.plan[lane] = line.base;
+    if (lane == 0) {
+      a.plan[a.n_seq] = line.total;
+      a.plan[a.n_seq + 1] = line.segments;
+    }
+  }
+  const bool solo = line.cuts.solo;
+  const int me = solo ? blockIdx.x * 4 + wave : blockIdx.x;
+  const int first = solo ? 0 : group, step = solo ? 1 : W::GROUPS;
+  if ((long)me * line.cuts.share >= line.total) return;
   const int end = line.bound(a, me + 1);
   for (int p = line.bound(a, me); p < end;) {
     int before;
-    const int s = __builtin_amdgcn_readfirstlane(line.find(a, p, &before));
-    before = __builtin_amdgcn_readfirstlane(before);
-    Seq q = seq_of<KT, W::ROWS>(a, s);
-    q.len = __builtin_amdgcn_readfirstlane(q.len);
-    q.start = __builtin_amdgcn_readfirstlane(q.start);
-    q.n = __builtin_amdgcn_readfirstlane(q.n);
-    q.tc = __builtin_amdgcn_readfirstlane(q.tc);
-    q.t = __builtin_amdgcn_readfirstlane(q.t);
-    const int seg = (p - before) / q.t, j = seg % a.Hkv, block = seg / a.Hkv;
+    const int s = line.find(a, p, &before);
+    const Seq q = line.seq(a, s);
+    const int seg = (p - before) / q.t, block = seg / a.Hkv, j = seg - block * a.Hkv;
     const int from = before + seg * q.t;
     const int f0 = p - from, f1 = min(end - from, q.t);
     p = from + f1;
@@ -293,13 +349,13 @@ __global__ __launch_bounds__(64 * TEAM, 2) void tree_kernel(TreeArgs a) {
     const int last = min(((block + 1) * W::ROWS - 1) / G, q.n - 1);
     const int f_end = a.mask ? f1 : min(f1, q.tc + last / KT + 1);
 
-    Keys<HD, TEAM> keys;
-    keys.init(a, s, q, j, lane);
-    auto stage = [&](int f) { return smem + (f - f0) % W::STAGES * 2 * W::TB; };
-    if (f0 < f_end) keys.issue(f0, stage(f0), wave, lane);
+    Keys<HD, RB> keys;
+    keys.init(a, s, q, j);
+    auto stage = [&](int it) { return ring + it % W::STAGES * 2 * W::TB; };
+    if (f0 + first < f_end) keys.issue(f0 + first, stage(0), rw);
     uint64_t next_seen = keys.seen;
 
-    const int row = block * W::ROWS + 32 * wave + lq;
+    const int row = block * W::ROWS + 32 * rw + lq;
     const bool on = row < q.n * G;
     const int r = min(row, q.n * G - 1), i = r / G, h = j * G + r - i * G;
     const size_t token = (size_t)q.start + i;
@@ -312,123 +368,156 @@ __global__ __launch_bounds__(64 * TEAM, 2) void tree_kernel(TreeArgs a) {
     for (int d = 0; d < S::DT; ++d) zero(o[d]);
     float m_run = -INFINITY, l_run = 0.0f;
 
-    for (int f = f0; f < f_end; ++f) {
+    for (int it = 0; f0 + it * step < f_end; ++it) {
+      const int f = f0 + it * step + first;
       wait_vmcnt<0>();
       __builtin_amdgcn_s_waitcnt(0xC07F);   // this wave's reads of the stage that the next loads overwrite are done
-      if constexpr (TEAM > 1) block_barrier();
+      if constexpr (RB > 1) block_barrier();
       const uint64_t there = next_seen;
-      if (f + 1 < f_end) {
-        keys.issue(f + 1, stage(f + 1), wave, lane);
+      if (f + step < f_end) {
+        keys.issue(f + step, stage(it + 1), rw);
         next_seen = keys.seen;
       }
-      const lds_char_t* Ks = stage(f);
-      lds_char_t* Vs = stage(f) + W::TB;
-      // the keys that this lane's row sees
-      constexpr uint64_t ALL = KT == 64 ? ~0ull : (1ull << KT) - 1;
-      uint64_t mine = there, bad = 0;
-      if (f >= q.tc) {
-        const int d0 = (f - q.tc) * KT;
-        if (a.mask) {
-          const int32_t* words = a.mask + token * a.mask_words + d0 / 32;
-          uint64_t w = d0 / 32 < a.mask_words ? (uint32_t)words[0] : 0u;
-          if (KT == 64 && d0 / 32 + 1 < a.mask_words) w |= (uint64_t)(uint32_t)words[1] << 32;
-          mine &= w;
-        } else if (i < d0 + KT - 1) {
-          mine &= i < d0 ? 0ull : (2ull << (i - d0)) - 1;
+      if (f >= f_end) continue;
+      // 32 keys at a time: the scores of 64 at once would leave too few registers
+#pragma unroll 1
+      for (int sub = 0; sub < KT / 32; ++sub) {
+        const lds_char_t* Ks = stage(it) + sub * 64 * HD;
+        const lds_char_t* Vs = Ks + W::TB;
+        // the keys that this lane's row sees
+        uint32_t mine = (uint32_t)(there >> (32 * sub)), bad = 0;
+        const bool drafted = f >= q.tc;
+        if (drafted) {
+          const int d0 = (f - q.tc) * KT + 32 * sub;
+          if (a.mask) mine &= d0 / 32 < a.mask_words ? (uint32_t)a.mask[token * a.mask_words + d0 / 32] : 0u;
+          else if (i < d0 + 31) mine &= i < d0 ? 0u : (2u << (i - d0)) - 1;
         }
-        // (the whole team's rows, so that its waves agree)
-        if (a.mask || block * W::ROWS / G < d0 + KT - 1) {
-          bad = not_finite<HD, KT>(Vs, lane);
-          if (bad) {
-            if constexpr (TEAM > 1) block_barrier();
-            for (int u = threadIdx.x; u < KT * HD / 8; u += 64 * TEAM)
-              if (bad >> (u / (HD / 8)) & 1) *reinterpret_cast<lds_v4u32_t*>(Vs + u * 16) = v4u32{0, 0, 0, 0};
-            __builtin_amdgcn_s_waitcnt(0xC07F);
-            if constexpr (TEAM > 1) block_barrier();
-          }
-        }
-      }
-      if (__ballot(mine != 0) == 0) continue;
+        if (__ballot(mine != 0) == 0) continue;
+        const bool all = __ballot(mine != ~0u) == 0;
+        if (drafted && !all) bad = not_finite<HD>(Vs, lane);
 
-      floatx16 x[NT];
+        floatx16 x;
+        zero(x);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        zero(x[t]);
+        for (int k = 0; k < S::KS; ++k) x = mfma32(read_row<HD>(Ks, lq, 2 * k + g), qf[k], x);
+        float mt = -INFINITY;
+        if (all) {
 #pragma unroll
-        for (int k = 0; k < S::KS; ++k) x[t] = mfma32(read_row<HD>(Ks, 32 * t + lq, 2 * k + g), qf[k], x[t]);
-      }
-      float mt = -INFINITY;
-      if (__ballot(mine != ALL) == 0) {
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) mt = fmaxf(mt, x[t][e]);
-      } else {
-        const uint64_t bits = mine >> (4 * g);
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
+          for (int e = 0; e < 16; ++e) mt = fmaxf(mt, x[e]);
+        } else {
+          const uint32_t bits = mine >> (4 * g);
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            x[t][e] = bits >> (32 * t + acc_row(e, 0)) & 1 ? x[t][e] : -INFINITY;
-            mt = fmaxf(mt, x[t][e]);
+            x[e] = bits >> acc_row(e, 0) & 1 ? x[e] : -INFINITY;
+            mt = fmaxf(mt, x[e]);
           }
-      }
-      mt = max32(mt) * sc;
-      const bool grow = mt > m_run + RESCALE_SLACK;
-      if (__ballot(grow) != 0) {
-        const float alpha = grow ? fast_exp2(m_run - mt) : 1.0f;
-        m_run = grow ? mt : m_run;
-        l_run *= alpha;
+        }
+        mt = max32(mt) * sc;
+        const bool grow = mt > m_run + RESCALE_SLACK;
+        if (__ballot(grow) != 0) {
+          const float alpha = grow ? fast_exp2(m_run - mt) : 1.0f;
+          m_run = grow ? mt : m_run;
+          l_run *= alpha;
 #pragma unroll
-        for (int d = 0; d < S::DT; ++d)
+          for (int d = 0; d < S::DT; ++d)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) o[d][e] *= alpha;
-      }
-      const float shift = m_run == -INFINITY ? 0.0f : m_run;   // nothing seen yet
-      float rsum = 0.0f;
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
+            for (int e = 0; e < 16; ++e) o[d][e] *= alpha;
+        }
+        const float shift = m_run == -INFINITY ? 0.0f : m_run;   // nothing seen yet
+        float rsum = 0.0f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const float w = fast_exp2(fmaf(x[t][e], sc, -shift));
-          x[t][e] = w;
+          const float w = fast_exp2(fmaf(x[e], sc, -shift));
+          x[e] = w;
           rsum += w;
         }
-      l_run += sum32(rsum);
+        l_run += sum32(rsum);
+        auto add_values = [&](auto clean) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+          for (int hh = 0; hh < 2; ++hh) {
+            const bf16x8 pf = acc_slots(x, hh);
 #pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-          const bf16x8 pf = acc_slots(x[t], hh);
-#pragma unroll
-          for (int d = 0; d < S::DT; ++d) o[d] = mfma32(read_tr<HD>(Vs, 32 * d, 32 * t + 16 * hh, lane), pf, o[d]);
-        }
-      // values that are not finite, one token after another
-      while (bad) {
-        const int k = __builtin_ctzll(bad);
-        bad &= bad - 1;
-        float w = 0.0f;
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) w = (k & ~4) == 32 * t + acc_row(e, 0) ? x[t][e] : w;
-        w = __shfl(w, lq + (k >> 2 & 1) * 32);
-        const bf16_t* v = a.qkv + ((size_t)q.start + (f - q.tc) * KT + k) * (a.H + 2 * a.Hkv) * HD +
-                          (size_t)(a.H + a.Hkv + j) * HD;
-        const bool sees = mine >> k & 1;
-#pragma unroll
-        for (int d = 0; d < S::DT; ++d)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float y = o[d][e] + w * bf2f(v[32 * d + acc_row(e, 0) + 4 * g]);
-            o[d][e] = sees ? y : o[d][e];
+            for (int d = 0; d < S::DT; ++d) {
+              bf16x8 v = read_tr<HD>(Vs, 32 * d, 16 * hh, lane);
+              if constexpr (decltype(clean)::value) v = finite(v);
+              o[d] = mfma32(v, pf, o[d]);
+            }
           }
+        };
+        if (bad == 0) {
+          add_values(std::false_type{});
+          continue;
+        }
+        add_values(std::true_type{});
+        // what was left out, one token after another
+        while (bad) {
+          const int k = __builtin_ctz(bad);
+          bad &= bad - 1;
+          float w = 0.0f;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) w = (k & ~4) == acc_row(e, 0) ? x[e] : w;
+          w = __shfl(w, lq + (k >> 2 & 1) * 32);
+          const bool sees = mine >> k & 1;
+#pragma unroll
+          for (int d = 0; d < S::DT; ++d)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              const uint2 v = __builtin_bit_cast(
+                  uint2, *reinterpret_cast<const LDS_AS floatx2*>(Vs + unit<HD>(k, 4 * d + c) * 16 + 8 * g));
+              const float y[4] = {lo_f(v.x), hi_f(v.x), lo_f(v.y), hi_f(v.y)};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[d][4 * c + e] += w * (sees & !isfinite(y[e]) ? y[e] : 0.0f);
+              __builtin_amdgcn_sched_barrier(0);   // one read at a time: this path keeps few registers
+            }
+        }
       }
     }
-    if constexpr (TEAM > 1) __syncthreads();   // the ring is the next segment's
+
+    if constexpr (W::GROUPS > 1) {
+      if (!solo) {
+        // the other groups' results through LDS, joined in order
+        __syncthreads();
+        lds_char_t* keep = (lds_char_t*)smem_raw + ((group - 1) * RB + rw) * W::KEEP + lane * 16;
+        if (group > 0) {
+#pragma unroll
+          for (int d = 0; d < S::DT; ++d)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              *reinterpret_cast<lds_v4f32_t*>(keep + (d * 4 + c) * 1024) =
+                  v4f32{o[d][4 * c], o[d][4 * c + 1], o[d][4 * c + 2], o[d][4 * c + 3]};
+          *reinterpret_cast<LDS_AS floatx2*>(keep + S::DT * 4096 - lane * 8) = floatx2{m_run, l_run};
+        }
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+          for (int k = 1; k < W::GROUPS; ++k) {
+            const lds_char_t* other = keep + k * RB * W::KEEP;
+            const floatx2 ml = *reinterpret_cast<const LDS_AS floatx2*>(other + S::DT * 4096 - lane * 8);
+            const float m = fmaxf(m_run, ml.x);
+            const float w0 = m_run == -INFINITY ? 0.0f : fast_exp2(m_run - m);
+            const float w1 = ml.x == -INFINITY ? 0.0f : fast_exp2(ml.x - m);
+            // (sums of rows that met a NaN have no maximum, but count)
+            l_run = (m_run == -INFINITY ? l_run : l_run * w0) + (ml.x == -INFINITY ? ml.y : ml.y * w1);
+            m_run = m;
+#pragma unroll
+            for (int d = 0; d < S::DT; ++d)
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                const v4f32 y = *reinterpret_cast<const lds_v4f32_t*>(other + (d * 4 + c) * 1024);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[d][4 * c + e] = o[d][4 * c + e] * w0 + y[e] * w1;
+              }
+          }
+        }
+        __syncthreads();   // the rings are the next segment's
+        if (group > 0) continue;
+      }
+    } else {
+      __syncthreads();
+    }
     if (!on) continue;
     if (f0 == 0 && f1 == q.t) {
-      const float inv = l_run > 0.0f ? 1.0f / l_run : l_run == 0.0f ? 0.0f : l_run;
+      const float inv = inverse(l_run);
       bf16_t* out = a.out + (token * a.H + h) * HD;
 #pragma unroll
       for (int d = 0; d < S::DT; ++d)
@@ -441,9 +530,8 @@ __global__ __launch_bounds__(64 * TEAM, 2) void tree_kernel(TreeArgs a) {
       continue;
     }
     // a share has at most two cut segments: one that begins in it, one that does not
-    const int prows = part_rows(a, W::ROWS);
+    const int prows = part_rows(a, W::ROWS), pr = 32 * rw + lq;
     float* part = a.part + (2 * (size_t)me + (f0 == 0)) * part_floats(a, W::ROWS, HD);
-    const int pr = 32 * wave + lq;
 #pragma unroll
     for (int d = 0; d < S::DT; ++d)
 #pragma unroll
@@ -457,13 +545,16 @@ __global__ __launch_bounds__(64 * TEAM, 2) void tree_kernel(TreeArgs a) {
   }
 }
 
-// The parts of a cut segment's row, a wave a row of one query head.
-template <int HD, int TEAM>
-__global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
-  using W = Walk<HD, TEAM>;
+// The parts of a cut segment's row of one query head, WPR waves a row: lane k
+// holds part k's maximum and sum (the maximum's weight afterwards), then HD/8
+// lanes take the row's elements, 8 each, and the groups of them the parts in turn.
+template <int HD, int RB, int WPR>
+__global__ __launch_bounds__(WPR == 1 ? 256 : 64 * WPR) void tree_join_kernel(TreeArgs a) {
+  using W = Walk<HD, RB>;
   constexpr int LANES = HD / 8, GROUPS = 64 / LANES;
-  const int lane = threadIdx.x & 63, G = a.H / a.Hkv;
-  const long at = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  __shared__ float other[WPR][HD + 2];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, G = a.H / a.Hkv;
+  const long at = WPR == 1 ? (long)blockIdx.x * 4 + wave : blockIdx.x;
   const int token = (int)(at / a.H), h = (int)(at - (long)token * a.H);
   if (token >= a.n_rows) return;
   // the sequence that has the row: the last one that begins at or before it
@@ -473,16 +564,15 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
     if (b) s = s0 + 63 - __builtin_clzll(b);
   }
   if (s < 0) return;
-  const Seq q = seq_of<W::KT, W::ROWS>(a, s);
+  const int total = a.plan[a.n_seq], segments = a.plan[a.n_seq + 1], before = a.plan[s];
+  const Seq q = seq_of<W>(a, s);
   const int i = token - q.start;
   if (i < 0 || i >= q.n) return;
-  const int total = a.plan[a.n_seq];
-  const int share = max(W::LEAST, (total + W::SHARES - 1) / W::SHARES);
-  const int slack = cut_slack(share, W::LEAST);
+  const Cuts cuts = cuts_of<W>(total, segments);
   const int j = h / G, r = i * G + h - j * G, block = r / W::ROWS, row = r - block * W::ROWS;
-  const int from = a.plan[s] + (block * a.Hkv + j) * q.t;
+  const int from = before + (block * a.Hkv + j) * q.t;
   // cuts w0..w1 lie inside the segment, so shares w0 - 1..w1 have its parts
-  const int w0 = (from + slack) / share + 1, w1 = (from + q.t - slack - 1) / share;
+  const int w0 = (from + cuts.slack) / cuts.share + 1, w1 = (from + q.t - cuts.slack - 1) / cuts.share;
   if (w1 < w0) return;
   const int parts = w1 - w0 + 2;
   const int prows = part_rows(a, W::ROWS);
@@ -490,21 +580,23 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   const float* part0 = a.part + 2 * (size_t)(w0 - 1) * floats;
   // part k's place: the first begins in its share, the others do not
   auto place = [&](int k) { return part0 + (2 * (size_t)k + (k == 0)) * floats; };
+  // this wave's parts
+  const int k_begin = (int)((long)parts * wave / WPR) * (WPR > 1), k_end = WPR > 1 ? (int)((long)parts * (wave + 1) / WPR) : parts;
   float m = -INFINITY;
-  for (int k = lane; k < parts; k += 64) m = fmaxf(m, place(k)[(size_t)prows * HD + row]);
+  for (int k = k_begin + lane; k < k_end; k += 64) m = fmaxf(m, place(k)[(size_t)prows * HD + row]);
 #pragma unroll
   for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  const float shift = m == -INFINITY ? 0.0f : m;
   const int c = lane % LANES * 8;
   float l = 0.0f, o[8] = {};
-  for (int k0 = 0; k0 < parts; k0 += 64) {
+  for (int k0 = k_begin; k0 < k_end; k0 += 64) {
     float wgt = 0.0f;
-    if (k0 + lane < parts) {
+    if (k0 + lane < k_end) {
       const float* p = place(k0 + lane) + (size_t)prows * HD;
-      wgt = fast_exp2(p[row] - shift);
-      l += wgt * p[prows + row];
+      const float mk = p[row], lk = p[prows + row];
+      wgt = mk == -INFINITY ? 0.0f : fast_exp2(mk - m);
+      l += mk == -INFINITY ? lk : wgt * lk;
     }
-    const int n = min(64, parts - k0);
+    const int n = min(64, k_end - k0);
 #pragma unroll 4
     for (int k = 0; k < n; k += GROUPS) {
       const int w = k + lane / LANES;
@@ -522,29 +614,54 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   for (int e = 0; e < 8; ++e)
 #pragma unroll
     for (int x = LANES; x < 64; x <<= 1) o[e] += __shfl_xor(o[e], x);
+  if constexpr (WPR > 1) {
+    if (lane < LANES) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) other[wave][c + e] = o[e];
+      if (lane == 0) {
+        other[wave][HD] = m;
+        other[wave][HD + 1] = l;
+      }
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < WPR; ++w) top = fmaxf(top, other[w][HD]);
+    l = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WPR; ++w) {
+      const float mw = other[w][HD], lw = other[w][HD + 1], f = mw == -INFINITY ? 0.0f : fast_exp2(mw - top);
+      l += mw == -INFINITY ? lw : f * lw;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] += f * other[w][c + e];
+    }
+    m = top;
+  }
   if (lane >= LANES) return;
-  const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+  const float inv = inverse(l);
   *reinterpret_cast<uint4*>(a.out + ((size_t)token * a.H + h) * HD + c) =
       make_uint4(pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv), pack2(o[4] * inv, o[5] * inv),
                  pack2(o[6] * inv, o[7] * inv));
   if (c == 0 && a.lse) a.lse[(size_t)h * a.n_rows + token] = (m + log2f(l)) * LN2;
 }
 
-int team_of(const TreeArgs& a) { return (long)a.max_new * (a.H / a.Hkv) <= 32 ? 1 : 4; }
+template <int V>
+using Int = std::integral_constant<int, V>;
 
+// f(head size, blocks of rows of a workgroup): as many as a sequence's rows fill
 template <class Fn>
 auto with_walk(const TreeArgs& a, Fn f) {
-  const bool wide = a.hd == 128;
-  if (team_of(a) == 1) return wide ? f(std::integral_constant<int, 128>{}, std::integral_constant<int, 1>{})
-                                   : f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
-  return wide ? f(std::integral_constant<int, 128>{}, std::integral_constant<int, 4>{})
-              : f(std::integral_constant<int, 64>{}, std::integral_constant<int, 4>{});
+  const long rows = (long)a.max_new * (a.H / a.Hkv);
+  if (a.hd == 128) return rows <= 32 ? f(Int<128>{}, Int<1>{}) : rows <= 64 ? f(Int<128>{}, Int<2>{}) : f(Int<128>{}, Int<4>{});
+  return rows <= 32 ? f(Int<64>{}, Int<1>{}) : rows <= 64 ? f(Int<64>{}, Int<2>{}) : f(Int<64>{}, Int<4>{});
 }
 
 // Tiles of all sequences at their longest, and of one of their segments.
-template <int HD, int TEAM>
+template <class W>
 double most_tiles(const TreeArgs& a, double* segment) {
-  using W = Walk<HD, TEAM>;
   *segment = std::ceil((double)a.max_pages * a.ps / W::KT) + std::ceil((double)a.max_new / W::KT);
   return *segment * a.n_seq * a.Hkv * std::ceil((double)a.max_new * (a.H / a.Hkv) / W::ROWS);
 }
@@ -552,31 +669,31 @@ double most_tiles(const TreeArgs& a, double* segment) {
 }  // namespace
 
 size_t tree_workspace(const TreeArgs& a, size_t* part_at) {
-  return with_walk(a, [&](auto hd, auto team) -> size_t {
-    using W = Walk<decltype(hd)::value, decltype(team)::value>;
+  return with_walk(a, [&](auto hd, auto rb) -> size_t {
+    using W = Walk<decltype(hd)::value, decltype(rb)::value>;
     double segment;
-    // tiles are counted in 32 bits
-    if (most_tiles<decltype(hd)::value, decltype(team)::value>(a, &segment) > 2e9) return 0;
-    const size_t plan = ((size_t)a.n_seq + 2) * sizeof(int32_t);
-    *part_at = (plan + 255) / 256 * 256;
-    return *part_at + (segment > W::LEAST ? 2 * (size_t)W::SHARES * part_floats(a, W::ROWS, W::HEAD) * sizeof(float) : 0);
+    if (most_tiles<W>(a, &segment) > 2e9) return 0;   // tiles are counted in 32 bits
+    *part_at = (((size_t)a.n_seq + 2) * sizeof(int32_t) + 255) / 256 * 256;
+    return *part_at + (segment > W::LEAST ? 2 * (size_t)W::MOST * part_floats(a, W::ROWS, W::HEAD) * sizeof(float) : 0);
   });
 }
 
 hipError_t launch_tree(const TreeArgs& a, hipStream_t s) {
   if (a.n_rows < 1) return hipSuccess;
-  return with_walk(a, [&](auto hd, auto team) -> hipError_t {
-    constexpr int HD = decltype(hd)::value, TEAM = decltype(team)::value;
-    using W = Walk<HD, TEAM>;
+  return with_walk(a, [&](auto hd, auto rb) -> hipError_t {
+    constexpr int HD = decltype(hd)::value, RB = decltype(rb)::value;
+    using W = Walk<HD, RB>;
     double segment;
-    const double tiles = most_tiles<HD, TEAM>(a, &segment);
-    if (a.n_seq > 64) hipLaunchKernelGGL((tree_plan_kernel<W::KT, W::ROWS>), dim3(1), dim3(64), 0, s, a);
-    const unsigned shares = (unsigned)std::min((double)W::SHARES, std::ceil(tiles / W::LEAST));
-    hipLaunchKernelGGL((tree_kernel<HD, TEAM>), dim3(shares), dim3(64 * TEAM), 0, s, a);
-    // segments of no more tiles than the smallest share are never cut
-    if (segment > W::LEAST)
-      hipLaunchKernelGGL((tree_join_kernel<HD, TEAM>), dim3((unsigned)(((long)a.n_rows * a.H + 3) / 4)), dim3(256), 0,
-                         s, a);
+    const double tiles = most_tiles<W>(a, &segment);
+    if (a.n_seq > 64) hipLaunchKernelGGL((tree_plan_kernel<W>), dim3(1), dim3(64), 0, s, a);
+    const unsigned teams = (unsigned)std::min((double)W::TEAMS, std::ceil(tiles / W::LEAST));
+    hipLaunchKernelGGL((tree_kernel<HD, RB>), dim3(teams), dim3(256), 0, s, a);
+    if (segment > W::LEAST) {
+      const long rows = (long)a.n_rows * a.H;
+      // a few rows of many parts: 8 waves a row
+      if (rows <= 512) hipLaunchKernelGGL((tree_join_kernel<HD, RB, 8>), dim3((unsigned)rows), dim3(512), 0, s, a);
+      else hipLaunchKernelGGL((tree_join_kernel<HD, RB, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
+    }
     return hipGetLastError();
   });
 }
