@@ -2,58 +2,85 @@
 // biases, grammar masks.
 //
 // A workgroup takes a piece of one row. It counts the row's history within the
-// piece in LDS (whole numbers, so their order does not matter), collects the
-// biases that fall into it, and passes over the logits once, its loads under way
-// while it counts. HBM-bound with many rows; the history is read again by every
-// piece of the row, from L2, so pieces are as long as leaves workgroups for all
-// CUs.
+// piece in LDS (whole numbers, so their order does not matter), then passes over
+// the logits once, whose loads are under way behind the history's. HBM-bound with
+// many rows; every piece of a row reads the history again, from L2, so pieces are
+// long where histories are.
+#include <algorithm>
+
 #include "../../include/qwen3_decode.h"
 #include "common.h"
 #include "kernels.h"
 
 namespace {
 
-constexpr int THREADS = 256, VEC = 8, STEP = THREADS * VEC;
-constexpr uint32_t PROMPT = 1u << 31;   // seen, whatever the count
+constexpr int VEC = 8;
 
-// Rows begin at any element.
-struct __attribute__((packed, aligned(2))) Bf16s { uint32_t w[4]; };
-struct __attribute__((packed, aligned(4))) Floats { float v[4]; };
-
-template <bool BF16>
-DEV void load8(const void* base, size_t at, float* x) {
-  if constexpr (BF16) {
-    const Bf16s u = *reinterpret_cast<const Bf16s*>(static_cast<const bf16_t*>(base) + at);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      x[2 * k] = lo_f(u.w[k]);
-      x[2 * k + 1] = hi_f(u.w[k]);
-    }
-  } else {
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const Floats u = *reinterpret_cast<const Floats*>(static_cast<const float*>(base) + at + 4 * k);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[4 * k + e] = u.v[e];
-    }
+// Counts of a token in 15 bits, two a word, where a history cannot have more of
+// it, otherwise in 31; the bit above says that it was seen in the prompt.
+template <bool SHORT>
+struct Counts {
+  static constexpr int BITS = SHORT ? 16 : 32;
+  static constexpr uint32_t SEEN = 1u << (BITS - 1);
+  static constexpr int words(int piece) { return SHORT ? piece / 2 : piece; }
+  static DEV void add(uint32_t* c, unsigned v, int sign = 1) {
+    if constexpr (SHORT) atomicAdd(c + v / 2, (uint32_t)sign << (16 * (v & 1)));
+    else atomicAdd(c + v, (uint32_t)sign);
   }
+  static DEV void see(uint32_t* c, unsigned v) {
+    if constexpr (SHORT) atomicOr(c + v / 2, SEEN << (16 * (v & 1)));
+    else atomicOr(c + v, SEEN);
+  }
+  static DEV uint32_t get(const uint32_t* c, unsigned v) {
+    if constexpr (SHORT) return c[v / 2] >> (16 * (v & 1)) & 0xffffu;
+    else return c[v];
+  }
+  // a bit for each of tokens v..v+7 that is there
+  static DEV uint32_t eight(const uint32_t* c, unsigned v) {
+    uint32_t some = 0;
+    const uint4 a = reinterpret_cast<const uint4*>(c)[SHORT ? v / 8 : v / 4];
+    if constexpr (SHORT) {
+      const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) some |= (w[k] & 0xffffu ? 1u << (2 * k) : 0u) | (w[k] >> 16 ? 2u << (2 * k) : 0u);
+    } else {
+      const uint4 b = reinterpret_cast<const uint4*>(c)[v / 4 + 1];
+      const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int k = 0; k < 8; ++k) some |= w[k] ? 1u << k : 0u;
+    }
+    return some;
+  }
+};
+
+// Eight logits as they are in memory, where rows begin at any element.
+template <bool BF16>
+struct Raw;
+template <>
+struct __attribute__((packed, aligned(2))) Raw<true> {
+  uint32_t w[4];
+  DEV float get(int e) const { return e & 1 ? hi_f(w[e / 2]) : lo_f(w[e / 2]); }
+  DEV void set(const float* x) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = pack2(x[2 * k], x[2 * k + 1]);
+  }
+};
+template <>
+struct __attribute__((packed, aligned(4))) Raw<false> {
+  float v[8];
+  DEV float get(int e) const { return v[e]; }
+  DEV void set(const float* x) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = x[e];
+  }
+};
+template <bool BF16>
+DEV Raw<BF16> load8(const void* base, size_t at) {
+  return *reinterpret_cast<const Raw<BF16>*>(static_cast<const char*>(base) + at * (BF16 ? 2 : 4));
 }
 template <bool BF16>
-DEV void store8(void* base, size_t at, const float* x) {
-  if constexpr (BF16) {
-    Bf16s u;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) u.w[k] = pack2(x[2 * k], x[2 * k + 1]);
-    *reinterpret_cast<Bf16s*>(static_cast<bf16_t*>(base) + at) = u;
-  } else {
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      Floats u;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) u.v[e] = x[4 * k + e];
-      *reinterpret_cast<Floats*>(static_cast<float*>(base) + at + 4 * k) = u;
-    }
-  }
+DEV void store8(void* base, size_t at, const Raw<BF16>& x) {
+  *reinterpret_cast<Raw<BF16>*>(static_cast<char*>(base) + at * (BF16 ? 2 : 4)) = x;
 }
 template <bool BF16>
 DEV float load1(const void* base, size_t at) {
@@ -66,146 +93,202 @@ DEV void store1(void* base, size_t at, float x) {
   else static_cast<float*>(base)[at] = x;
 }
 
-// The biases of a piece in LDS: which tokens have one, and the entries.
-constexpr int MAX_BIAS = 1024;
-struct Biases {
-  int n;
-  int token[MAX_BIAS], entry[MAX_BIAS];
-  float value[MAX_BIAS];
-};
+struct __attribute__((packed, aligned(4))) Quad { int32_t t[4]; };
 
-template <bool BF16, int STEPS>
-__global__ __launch_bounds__(THREADS) void logits_kernel(qwen3_logits l, const void* in, void* out) {
-  constexpr int PIECE = STEPS * STEP;
+// LDS of a workgroup, in words: counts, a bit for each logit with a bias, the
+// biases of the piece (how many, then token, entry and value of each).
+template <bool SHORT>
+__host__ DEV int lds_words(const qwen3_logits& l, int piece) {
+  return (l.d_history || l.d_path ? Counts<SHORT>::words(piece) : 0) + (l.n_bias > 0 ? piece / 32 + 4 + 3 * l.n_bias : 0);
+}
+
+// (waves a SIMD, by the registers: four workgroups a CU)
+template <bool BF16, bool SHORT, int THREADS, int STEPS>
+__global__ __launch_bounds__(THREADS, 8) void logits_kernel(qwen3_logits l, const void* in,
+                                                                                 void* out) {
+  using C = Counts<SHORT>;
+  constexpr int STEP = THREADS * VEC, PIECE = STEPS * STEP;
+  constexpr int QUADS = 2;   // of history tokens a thread has under way
   extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
   const bool counting = l.d_history || l.d_path, biased = l.n_bias > 0;
   uint32_t* count = lds;
-  uint32_t* has_bias = lds + (counting ? PIECE : 0);
-  Biases* b = reinterpret_cast<Biases*>(has_bias + PIECE / 32);
-  const int tid = threadIdx.x, row = blockIdx.y, v0 = blockIdx.x * PIECE;
+  uint32_t* has_bias = lds + (counting ? C::words(PIECE) : 0);
+  int* n_biases = reinterpret_cast<int*>(has_bias + PIECE / 32);
+  int *bias_token = n_biases + 4, *bias_entry = bias_token + l.n_bias;
+  float* bias_value = reinterpret_cast<float*>(bias_entry + l.n_bias);
+  const int tid = threadIdx.x, row = blockIdx.y, v0 = blockIdx.x * PIECE, n = min(PIECE, l.vocab - v0);
   const size_t at = (size_t)row * l.logits_stride + v0, to = (size_t)row * l.out_stride + v0;
-  const int n = min(PIECE, l.vocab - v0);
 
-  float x[STEPS][VEC];
+  // the history's first tokens, before their number is known
+  int h = l.d_row_seq ? l.d_row_seq[row] : row;
+  if (!l.d_history || (unsigned)h >= (unsigned)l.n_seq) h = -1;
+  const int32_t* tokens = l.d_history + (size_t)max(h, 0) * l.history_stride;
+  auto load = [&](Quad* q, int i0) {   // from token i0 on, the row's last one behind its end
 #pragma unroll
-  for (int k = 0; k < STEPS; ++k) {
-    const int i = k * STEP + tid * VEC;
-    if (i + VEC <= n) {
-      load8<BF16>(in, at + i, x[k]);
-    } else {
+    for (int k = 0; k < QUADS; ++k) {
+      const int i = i0 + 4 * (tid + k * THREADS);
+      if (i + 4 <= l.history_stride) {
+        q[k] = *reinterpret_cast<const Quad*>(tokens + i);
+      } else if (i < l.history_stride) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) x[k][e] = i + e < n ? load1<BF16>(in, at + i + e) : 0.0f;
+        for (int e = 0; e < 4; ++e) q[k].t[e] = tokens[min(i + e, l.history_stride - 1)];
+      }
     }
+  };
+  Quad quads[QUADS];
+  int len = 0, prompt = 0;
+  if (h >= 0) {
+    load(quads, 0);
+    len = min(l.d_lens[h], l.history_stride);
+    prompt = l.d_prompt_lens ? l.d_prompt_lens[h] : 0;
   }
-  const int which = l.d_row_mask ? l.d_row_mask[row] : row;
-  const int32_t* mask = l.n_masks > 0 && (unsigned)which < (unsigned)l.n_masks
-                            ? l.d_masks + (size_t)which * ((l.vocab + 31) / 32) + v0 / 32 : nullptr;
+  int bias_id = -1;
+  float bias = 0.0f;
+  if (tid < l.n_bias) {
+    bias_id = l.d_bias_ids[(size_t)row * l.n_bias + tid];
+    bias = l.d_bias[(size_t)row * l.n_bias + tid];
+  }
   const float rep = l.d_repetition ? l.d_repetition[row] : 1.0f;
   const float freq = l.d_frequency ? l.d_frequency[row] : 0.0f;
   const float pres = l.d_presence ? l.d_presence[row] : 0.0f;
-
-  if (counting || biased) {
-    if (counting)
-      for (int i = tid; i < PIECE / 4; i += THREADS) reinterpret_cast<uint4*>(count)[i] = make_uint4(0, 0, 0, 0);
-    if (biased) {
-      for (int i = tid; i < PIECE / 32; i += THREADS) has_bias[i] = 0;
-      if (tid == 0) b->n = 0;
-    }
-    __syncthreads();
-    const int h = l.d_row_seq ? l.d_row_seq[row] : row;
-    if (l.d_history && (unsigned)h < (unsigned)l.n_seq) {
-      const int32_t* tokens = l.d_history + (size_t)h * l.history_stride;
-      const int len = min(l.d_lens[h], l.history_stride), prompt = l.d_prompt_lens ? l.d_prompt_lens[h] : 0;
-#pragma unroll 8
-      for (int i = tid; i < len; i += THREADS) {
-        const unsigned v = (unsigned)(tokens[i] - v0);
-        if (v < (unsigned)n && tokens[i] >= 0) {
-          if (i < prompt) atomicOr(count + v, PROMPT);
-          else atomicAdd(count + v, 1u);
-        }
-      }
-    }
-    if (l.d_path)
-      for (int i = tid; i < l.path_len; i += THREADS) {
-        const int token = l.d_path[(size_t)row * l.path_len + i];
-        if (token >= v0 && token - v0 < n) atomicAdd(count + (token - v0), 1u);
-      }
-    for (int i = tid; i < l.n_bias; i += THREADS) {
-      const int token = l.d_bias_ids[(size_t)row * l.n_bias + i];
-      if (token >= v0 && token - v0 < n) {
-        atomicOr(has_bias + (token - v0) / 32, 1u << ((token - v0) & 31));
-        const int k = atomicAdd(&b->n, 1);
-        b->token[k] = token - v0;
-        b->entry[k] = i;
-        b->value[k] = l.d_bias[(size_t)row * l.n_bias + i];
-      }
-    }
-    __syncthreads();
-  }
-
+  const int which = l.d_row_mask ? l.d_row_mask[row] : row;
+  const int32_t* mask = l.n_masks > 0 && (unsigned)which < (unsigned)l.n_masks
+                            ? l.d_masks + (size_t)which * ((l.vocab + 31) / 32) + v0 / 32 : nullptr;
+  Raw<BF16> raw[STEPS];
+  uint32_t allowed[STEPS];
 #pragma unroll
   for (int k = 0; k < STEPS; ++k) {
     const int i = k * STEP + tid * VEC;
-    if (i >= n) continue;
+    if (i + VEC <= n) raw[k] = load8<BF16>(in, at + i);
+    allowed[k] = mask && i < n ? (uint32_t)mask[i / 32] >> (i & 31) : ~0u;
+  }
+
+  if (counting || biased) {
     if (counting) {
-      const uint4 c0 = reinterpret_cast<const uint4*>(count)[i / 4], c1 = reinterpret_cast<const uint4*>(count)[i / 4 + 1];
-      const uint32_t c[VEC] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
 #pragma unroll
-      for (int e = 0; e < VEC; ++e)
-        if (c[e]) {
-          float y = x[k][e];
-          y = y > 0.0f ? y / rep : y * rep;
-          if (c[e] & ~PROMPT) y -= freq * (float)(c[e] & ~PROMPT) + pres;
-          x[k][e] = y;
-        }
+      for (int i = tid; i < C::words(PIECE) / 4; i += THREADS) reinterpret_cast<uint4*>(count)[i] = make_uint4(0, 0, 0, 0);
     }
     if (biased) {
-      const uint32_t some = has_bias[i / 32] >> (i & 31) & 0xffu;
-      if (some) {
+      for (int i = tid; i < PIECE / 32; i += THREADS) has_bias[i] = 0;
+      if (tid == 0) *n_biases = 0;
+    }
+    __syncthreads();
+    auto piece_has = [&](int token) { return token >= v0 && token - v0 < n; };
+    for (int i0 = 0; i0 < len; i0 += 4 * QUADS * THREADS) {
+      Quad now[QUADS];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e)
-          if (some >> e & 1) {
-            int best = -1;
-            float value = 0.0f;
-            for (int q = 0; q < b->n; ++q)
-              if (b->token[q] == i + e && b->entry[q] > best) {
-                best = b->entry[q];
-                value = b->value[q];
-              }
-            x[k][e] += value;
+      for (int k = 0; k < QUADS; ++k) now[k] = quads[k];
+      if (i0 + 4 * QUADS * THREADS < len) load(quads, i0 + 4 * QUADS * THREADS);
+#pragma unroll
+      for (int k = 0; k < QUADS; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = i0 + 4 * (tid + k * THREADS) + e, token = now[k].t[e];
+          if (i < len && piece_has(token)) {
+            if (i < prompt) C::see(count, token - v0);
+            else C::add(count, token - v0);
           }
+        }
+    }
+    if (l.d_path) {
+#pragma unroll 1
+      for (int i = tid; i < l.path_len; i += THREADS) {
+        const int token = l.d_path[(size_t)row * l.path_len + i];
+        if (piece_has(token)) C::add(count, token - v0);
       }
     }
-    if (mask) {
-      const uint32_t allowed = (uint32_t)mask[i / 32] >> (i & 31) & 0xffu;
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) x[k][e] = allowed >> e & 1 ? x[k][e] : -INFINITY;
+#pragma unroll 1
+    for (int i = tid; i < l.n_bias; i += THREADS) {
+      if (i >= THREADS) {
+        bias_id = l.d_bias_ids[(size_t)row * l.n_bias + i];
+        bias = l.d_bias[(size_t)row * l.n_bias + i];
+      }
+      if (piece_has(bias_id)) {
+        atomicOr(has_bias + (bias_id - v0) / 32, 1u << ((bias_id - v0) & 31));
+        const int k = atomicAdd(n_biases, 1);
+        bias_token[k] = bias_id - v0;
+        bias_entry[k] = i;
+        bias_value[k] = bias;
+      }
     }
-    if (i + VEC <= n) {
-      store8<BF16>(out, to + i, x[k]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < VEC; ++e)
-        if (i + e < n) store1<BF16>(out, to + i + e, x[k][e]);
+    __syncthreads();
+  }
+
+  // logit i as the history and the biases leave it
+  auto changed = [&](float y, int i) {
+    const uint32_t c = counting ? C::get(count, i) : 0u;
+    if (c) y = y > 0.0f ? y / rep : y * rep;
+    if (c & ~C::SEEN) y -= freq * (float)(c & ~C::SEEN) + pres;
+    if (biased && has_bias[i / 32] >> (i & 31) & 1) {
+      int best = -1;
+      float add_on = 0.0f;
+#pragma unroll 1
+      for (int k = 0; k < *n_biases; ++k)
+        if (bias_token[k] == i && bias_entry[k] > best) {
+          best = bias_entry[k];
+          add_on = bias_value[k];
+        }
+      y += add_on;
     }
+    return y;
+  };
+#pragma unroll
+  for (int k = 0; k < STEPS; ++k) {
+    const int i0 = k * STEP + tid * VEC;
+    if (i0 + VEC > n) continue;
+    float x[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) x[e] = raw[k].get(e);
+    uint32_t some = biased ? has_bias[i0 / 32] >> (i0 & 31) & 0xffu : 0u;
+    if (counting) some |= C::eight(count, i0);
+    // the few that change, one at a time
+#pragma unroll 1
+    while (some) {
+      const int e = __builtin_ctz(some);
+      some &= some - 1;
+      float y = x[0];
+#pragma unroll
+      for (int q = 1; q < VEC; ++q) y = e == q ? x[q] : y;
+      y = changed(y, i0 + e);
+#pragma unroll
+      for (int q = 0; q < VEC; ++q) x[q] = e == q ? y : x[q];
+    }
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) x[e] = allowed[k] >> e & 1 ? x[e] : -INFINITY;
+    raw[k].set(x);
+    store8<BF16>(out, to + i0, raw[k]);
+  }
+  // the columns behind the last eight
+  const int i = n / VEC * VEC + tid;
+  if (i < n) {
+    float y = changed(load1<BF16>(in, at + i), i);
+    if (mask && !((uint32_t)mask[i / 32] >> (i & 31) & 1)) y = -INFINITY;
+    store1<BF16>(out, to + i, y);
   }
 }
 
-template <bool BF16, int STEPS>
+template <bool BF16, bool SHORT, int THREADS, int STEPS>
 void launch_pieces(const qwen3_logits& l, const void* in, void* out, hipStream_t s) {
-  constexpr int PIECE = STEPS * STEP;
-  const size_t lds = (l.d_history || l.d_path ? 4u * PIECE : 0u) + (l.n_bias > 0 ? PIECE / 8 + sizeof(Biases) : 0u);
-  hipLaunchKernelGGL((logits_kernel<BF16, STEPS>), dim3((l.vocab + PIECE - 1) / PIECE, l.rows), dim3(THREADS), lds, s, l,
-                     in, out);
+  constexpr int PIECE = STEPS * THREADS * VEC;
+  hipLaunchKernelGGL((logits_kernel<BF16, SHORT, THREADS, STEPS>), dim3((l.vocab + PIECE - 1) / PIECE, l.rows),
+                     dim3(THREADS), sizeof(uint32_t) * lds_words<SHORT>(l, PIECE), s, l, in, out);
+}
+
+template <bool BF16>
+void launch(const qwen3_logits& l, const void* in, void* out, hipStream_t s) {
+  const long all = (long)l.rows * l.vocab;
+  const long longest = (l.d_history ? l.history_stride : 0) + (long)l.path_len;
+  // 64 rows of 151,936 after 2,048 tokens: 14.6 us in pieces of 8,192 (512 threads), 15.1 of 2,048 (256), 16.2 of
+  // 8,192 (256), 17.3 of 16,384; 96 rows of 50,257 after 30,000: 22.5, 31.6, 29.4, 24.4. Small calls take more
+  // workgroups of less.
+  if (longest >= Counts<true>::SEEN) launch_pieces<BF16, false, 512, 2>(l, in, out, s);
+  else if (all >= 512l * 2048 || longest > 4096) launch_pieces<BF16, true, 512, 2>(l, in, out, s);
+  else launch_pieces<BF16, true, 256, 1>(l, in, out, s);
 }
 
 }  // namespace
 
 hipError_t launch_adjust_logits(const qwen3_logits& l, const void* logits, void* out, hipStream_t s) {
-  const bool bf = l.dtype == 1;
-  const long all = (long)l.rows * l.vocab;
-  if (all >= 512l * 4 * STEP) bf ? launch_pieces<true, 4>(l, logits, out, s) : launch_pieces<false, 4>(l, logits, out, s);
-  else if (all >= 512l * 2 * STEP) bf ? launch_pieces<true, 2>(l, logits, out, s) : launch_pieces<false, 2>(l, logits, out, s);
-  else bf ? launch_pieces<true, 1>(l, logits, out, s) : launch_pieces<false, 1>(l, logits, out, s);
+  l.dtype == 1 ? launch<true>(l, logits, out, s) : launch<false>(l, logits, out, s);
   return hipGetLastError();
 }

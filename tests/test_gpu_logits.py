@@ -33,6 +33,7 @@ CASES = {
     "several_pieces": (7, 20000, 20000, "float32", 7, 3000, 0, 300, 0),
     "rows_of_drafts": (48, 512, 512, "float32", 4, 1000, 11, 0, 3),
     "long_history": (3, 50257, 50257, "bfloat16", 3, 30001, 2, 1, 1),
+    "past_15_bits": (2, 300, 300, "float32", 2, 70001, 2, 1, 1),
     "masks_alone": (6, 3001, 3008, "bfloat16", 0, 0, 0, 0, 5),
     "biases_alone": (6, 3001, 3008, "float32", 0, 0, 0, 1024, 0),
     "path_alone": (6, 3001, 3008, "float32", 0, 0, 30, 0, 0),
@@ -165,6 +166,19 @@ def test_the_last_entry_of_a_token_counts():
 
 def test_no_rows():
     assert db().adjust_logits(torch.empty(0, 50, device="cuda")).shape == (0, 50)
+
+
+@pytest.mark.parametrize("n", [32764, 32765, 32766, 65535, 65536, 140000])
+def test_one_token_over_and_over(n):
+    """Around the most that counts of 15 bits hold, beside a token of the prompt."""
+    history = torch.full((1, n + 3), 6, dtype=torch.int32, device="cuda")
+    history[0, :3] = torch.tensor([7, 7, 5])
+    count = lambda k: torch.tensor([k], dtype=torch.int32, device="cuda")   # noqa: E731
+    x = torch.zeros(1, 9, device="cuda")
+    y = db().adjust_logits(x, history, count(3), count(n + 3), frequency=torch.ones(1, device="cuda"))
+    want = torch.zeros(1, 9)
+    want[0, 6] = -n
+    assert torch.equal(y.cpu(), want)
 
 
 def test_rows_past_4_gib():
