@@ -158,14 +158,14 @@ gpt2_status qwen3_tree_attention(const qwen3_cache* c, const qwen3_tree* t, cons
   const size_t seqs = 4ul * c->n_seq;
   const struct { const void* p; size_t bytes; } in[] = {
       {d_qkv, qkv}, {d_starts, seqs + 4}, {d_mask, d_mask ? 4 * n * t->mask_words : 0}, {c->d_pages, pages_bytes(*c)},
-      {c->d_table, seqs * c->max_pages}, {c->d_lens, seqs}, {d_workspace, need}};
+      {c->d_table, seqs * c->max_pages}, {c->d_lens, seqs}, {c->d_refs, 4ul * c->n_pages}, {d_workspace, need}};
   for (const auto& i : in)
     if (i.p && (overlap(d_out, out, i.p, i.bytes) || (d_lse && overlap(d_lse, lse, i.p, i.bytes))))
       return refuse("out or lse overlaps another buffer");
   if (d_lse && overlap(d_out, out, d_lse, lse)) return refuse("out or lse overlaps another buffer");
   a.pages = static_cast<const bf16_t*>(c->d_pages) +
             (size_t)t->layer * c->n_pages * 2 * c->n_kv_head * c->page_size * c->head_dim;
-  a.table = c->d_table; a.lens = c->d_lens; a.starts = d_starts; a.mask = d_mask;
+  a.table = c->d_table; a.lens = c->d_lens; a.refs = c->d_refs; a.starts = d_starts; a.mask = d_mask;
   a.qkv = static_cast<const bf16_t*>(d_qkv);
   a.out = static_cast<bf16_t*>(d_out);
   a.lse = d_lse;

@@ -460,11 +460,11 @@ struct TreeArgs {
   int H, Hkv, hd, ps, n_pages, n_seq, max_pages;
   int n_rows, max_new, mask_words;
   const bf16_t* pages;    // the layer's
-  const int32_t *table, *lens, *starts, *mask;
+  const int32_t *table, *lens, *refs, *starts, *mask;
   const bf16_t* qkv;
   bf16_t* out;
   float* lse;
-  int32_t* plan;          // workspace: n_seq + 2 int32, then partial results
+  int32_t* plan;          // workspace: n_seq + 4 int32, then partial results
   float* part;
 };
 // workspace bytes: the plan, then the partial results, which begin at *part_at; 0: out of range

@@ -5,12 +5,12 @@
 // token, for one key/value head. Keys are walked in tiles: the cached ones
 // through the page table, then the sequence's new ones from the rows themselves,
 // masked by the rows' words or by order. One walk of a block of rows over all its
-// tiles is a segment; segments of all sequences, heads and blocks follow one
-// another in one line of tiles, which is cut into equal shares, one a worker,
-// whatever the lengths are. They are on the device, so each worker finds its
-// share from them by itself; with more than 64 sequences a launch before sums
-// them up. A segment that is cut leaves partial results (fp32 O, maximum, sum)
-// that a second launch joins, in order, so runs repeat bit for bit.
+// tiles is a segment. Lengths are on the device, so workers find what they do from
+// them by themselves (with more than 64 sequences a launch before sums them up):
+// where segments are few each is dealt to some workers in equal pieces; otherwise
+// segments follow one another in one line of tiles, which is cut into equal
+// shares. A segment of several workers leaves partial results (fp32 O, maximum,
+// sum) that a second launch joins, in order, so runs repeat bit for bit.
 //
 // A workgroup's four waves are RB blocks of 32 rows times 4/RB groups that walk a
 // share's tiles in turn and merge at a segment's end. With one block of rows and
@@ -18,9 +18,9 @@
 //
 // A page's tile rows come through a buffer descriptor that ends with the
 // sequence's last token, so that what a page holds behind it reads as zeros, and
-// with nothing where the table names no page. Elements of drafted tokens' values
-// that are not finite are taken out of the product and added for the rows that
-// see them only.
+// with nothing where the table names no page. Tiles of drafted tokens whose values
+// are not all finite go without the matrix product, token by token, so that they
+// reach the rows that see them only.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -39,11 +39,14 @@ struct Walk {
   static constexpr int TB = KT * HD * 2;        // bytes of a tile of keys
   static constexpr int STAGES = 2;
   static constexpr int RING = STAGES * 2 * TB;  // of a group
-  static constexpr int KEEP = HD * 32 * 4 + 512;   // a wave's O, maxima and sums
+  static constexpr int DT = HD / 32, PER = DT > GROUPS ? DT / GROUPS : 1;   // blocks of 32 columns of O; of a group, merging
+  // of a wave's O for the others, maxima and sums
+  static constexpr int KEEP = (DT - (GROUPS * PER > DT ? 0 : PER)) * 4096 + 512;
   static constexpr int LEAST = 4;               // tiles of a share; segments of no more are never cut
+  static constexpr int WHOLE = 4 * GROUPS;      // ... nor dealt of these
   static constexpr int TEAMS = 256 * (RB == 1 ? 1 : 2);   // workgroups that run at a time
   static constexpr int MOST = RB == 1 ? 4 * TEAMS : TEAMS;   // shares
-  static_assert((GROUPS - 1) * RB * KEEP <= GROUPS * RING, "the groups' results fit their tiles' space");
+  static_assert(GROUPS == 1 || 4 * KEEP <= GROUPS * RING, "the groups' results fit their tiles' space");
 };
 // Rows of a partial result, and its floats: O [rows][hd], maxima, sums.
 __host__ DEV int part_rows(const TreeArgs& a, int rows) {
@@ -92,73 +95,115 @@ DEV int wave_scan(int v) {
   return add_dpp<0x143, 0xc>(v);
 }
 
-// plan[s]: tiles before sequence s, s <= n_seq; plan[n_seq + 1]: segments
+// How the work is divided.
+//  dealt  a segment of t tiles goes to pieces_of(t, share) workers; a sequence's
+//         base is the number of workers before it
+//  line   worker w has tiles w share.. of the line of all segments, a cut nearer
+//         than `slack` to a segment's end going there (segments of LEAST tiles
+//         are never cut, and few tiles are left on one side of a cut); a
+//         sequence's base is the number of tiles before it
+//  solo   line, every wave a worker of its own
+enum Division { DEALT, LINE, SOLO };
+typedef int Cuts __attribute__((ext_vector_type(4)));   // division, share, slack
+template <class W>
+DEV int pieces_of(int t, int share) {
+  return t <= W::WHOLE ? 1 : (t + share - 1) / share;
+}
+// workers(share): the workers that segments dealt in pieces of `share` tiles take
+template <class W, class Fn>
+DEV Cuts cuts_of(int total, int segments, int longest, Fn workers) {
+  const int even = max(W::WHOLE / 2, (total + W::TEAMS - 1) / W::TEAMS);
+  int deal = segments <= W::TEAMS && longest <= W::WHOLE ? even : 0;
+  // (up to three in eight more tiles than with equal shares cost less than workers with parts of two segments: 16
+  // trees of 24 drafts over 1,000 to 3,001 tokens)
+#pragma unroll
+  for (int k = 3; k >= 0; --k) {
+    const int share = even + (even * k + 7) / 8;
+    if (segments <= W::TEAMS && workers(share) <= W::TEAMS) deal = share;
+  }
+  const bool solo = W::GROUPS == 4 && segments > W::TEAMS && total > 8 * W::TEAMS;
+  const int shares = solo ? W::MOST : W::TEAMS, share = max(W::LEAST, (total + shares - 1) / shares);
+  const int slack = max(W::LEAST / 2, share <= 2 * W::LEAST ? share / 2 : share / 8);
+  return Cuts{deal ? DEALT : solo ? SOLO : LINE, deal ? deal : share, slack, 0};
+}
+
+DEV int wave_total(int v) { return __builtin_amdgcn_readlane(wave_scan(v), 63); }
+DEV int wave_max(int v) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v = max(v, __shfl_xor(v, o));
+  return __builtin_amdgcn_readfirstlane(v);
+}
+
+// The plan, for the launches behind: bases of the sequences and their sum, then
+// the cuts.
+DEV void store_cuts(const TreeArgs& a, int sum, const Cuts& c) {
+  a.plan[a.n_seq] = sum;
+  a.plan[a.n_seq + 1] = c.x;
+  a.plan[a.n_seq + 2] = c.y;
+  a.plan[a.n_seq + 3] = c.z;
+}
+
 template <class W>
 __global__ __launch_bounds__(64) void tree_plan_kernel(TreeArgs a) {
   const int lane = threadIdx.x;
-  int before = 0, segments = 0;
+  auto over = [&](auto f) {   // the sum over the sequences
+    int sum = 0;
+    for (int s = lane; s < a.n_seq; s += 64) sum += f(seq_of<W>(a, s));
+    return wave_total(sum);
+  };
+  int most = 0;
+  for (int s = lane; s < a.n_seq; s += 64) {
+    const Seq q = seq_of<W>(a, s);
+    if (q.blocks) most = max(most, q.t);
+  }
+  const Cuts c = cuts_of<W>(over([&](const Seq& q) { return q.t * q.blocks * a.Hkv; }),
+                            over([&](const Seq& q) { return q.blocks * a.Hkv; }), wave_max(most), [&](int share) {
+                              return over([&](const Seq& q) { return pieces_of<W>(q.t, share) * q.blocks * a.Hkv; });
+                            });
+  int before = 0;
   for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
-    int u = 0, n = 0;
+    int u = 0;
     if (s0 + lane < a.n_seq) {
       const Seq q = seq_of<W>(a, s0 + lane);
-      n = q.blocks * a.Hkv;
-      u = q.t * n;
+      u = (c.x == DEALT ? pieces_of<W>(q.t, c.y) : q.t) * q.blocks * a.Hkv;
     }
     const int x = wave_scan(u);
     if (s0 + lane < a.n_seq) a.plan[s0 + lane] = before + x - u;
     before += __builtin_amdgcn_readlane(x, 63);
-    segments += __builtin_amdgcn_readlane(wave_scan(n), 63);
   }
-  if (lane == 0) {
-    a.plan[a.n_seq] = before;
-    a.plan[a.n_seq + 1] = segments;
-  }
+  if (lane == 0) store_cuts(a, before, c);
 }
 
-// How the line is cut: whether every wave is a worker, a share's tiles, and how
-// near a segment's end a cut goes there instead (segments of LEAST tiles are
-// never cut, and few tiles are left on one side of a cut).
-struct Cuts {
-  bool solo;
-  int share, slack;
-};
-template <class W>
-DEV Cuts cuts_of(int total, int segments) {
-  Cuts c;
-  c.solo = W::GROUPS == 4 && segments > W::TEAMS && total > 8 * W::TEAMS;
-  const int shares = c.solo ? W::MOST : W::TEAMS;
-  c.share = max(W::LEAST, (total + shares - 1) / shares);
-  c.slack = c.share <= 2 * W::LEAST ? c.share / 2 : max(W::LEAST / 2, c.share / 8);
-  return c;
-}
-
-// The line of tiles. Up to 64 sequences: lane s has sequence s and the tiles
-// before it. More: they are in plan.
+// What a worker knows of it all. Up to 64 sequences: lane s has sequence s. More:
+// the plan was made before.
 template <class W>
 struct Line {
-  int base, len, start, n, total, segments;
+  int base, len, start, n, sum;
   bool planned;
   Cuts cuts;
   DEV void init(const TreeArgs& a) {
     const int lane = threadIdx.x & 63;
     planned = a.n_seq > 64;
     if (planned) {
-      total = __builtin_amdgcn_readfirstlane(a.plan[a.n_seq]);
-      segments = __builtin_amdgcn_readfirstlane(a.plan[a.n_seq + 1]);
-    } else {
-      Seq q{};
-      if (lane < a.n_seq) q = seq_of<W>(a, lane);
-      len = q.len;
-      start = q.start;
-      n = q.n;
-      const int u = q.t * q.blocks * a.Hkv, x = wave_scan(u);
-      base = x - u;
-      total = __builtin_amdgcn_readlane(x, 63);
-      segments = __builtin_amdgcn_readlane(wave_scan(q.blocks * a.Hkv), 63);
+      sum = __builtin_amdgcn_readfirstlane(a.plan[a.n_seq]);
+      cuts.x = __builtin_amdgcn_readfirstlane(a.plan[a.n_seq + 1]);
+      cuts.y = __builtin_amdgcn_readfirstlane(a.plan[a.n_seq + 2]);
+      cuts.z = __builtin_amdgcn_readfirstlane(a.plan[a.n_seq + 3]);
+      return;
     }
-    cuts = cuts_of<W>(total, segments);
+    Seq q{};
+    if (lane < a.n_seq) q = seq_of<W>(a, lane);
+    len = q.len;
+    start = q.start;
+    n = q.n;
+    const int each = q.blocks * a.Hkv;
+    cuts = cuts_of<W>(wave_total(q.t * each), wave_total(each), wave_max(each ? q.t : 0),
+                      [&](int share) { return wave_total(pieces_of<W>(q.t, share) * each); });
+    const int u = (cuts.x == DEALT ? pieces_of<W>(q.t, cuts.y) : q.t) * each, x = wave_scan(u);
+    base = x - u;
+    sum = __builtin_amdgcn_readlane(x, 63);
   }
-  // the sequence that has tile p < total, and the tiles before it
+  // the sequence that has tile (worker) p < sum, and what is before it
   DEV int find(const TreeArgs& a, int p, int* before) const {
     const int lane = threadIdx.x & 63;
     if (!planned) {
@@ -183,16 +228,26 @@ struct Line {
     return seq_from<W>(a, __builtin_amdgcn_readfirstlane(q.len), __builtin_amdgcn_readfirstlane(q.start),
                        __builtin_amdgcn_readfirstlane(q.n));
   }
-  // where share w begins
+  // where share w of the line begins
   DEV int bound(const TreeArgs& a, int w) const {
-    const int p = w * cuts.share;   // below total + share
-    if (p >= total) return total;
+    const int p = w * cuts.y;   // below sum + share
+    if (p >= sum) return sum;
     int before;
     const int s = find(a, p, &before);
     const int t = seq(a, s).t, from = before + (p - before) / t * t;
-    return p - from <= cuts.slack ? from : from + t - p <= cuts.slack ? from + t : p;
+    return p - from <= cuts.z ? from : from + t - p <= cuts.z ? from + t : p;
   }
 };
+
+// dma16 past the caches, of what nobody else reads soon: pieces of one block of rows
+// whose first page has one holder. One token over 131,071: 103 -> 95 us a pass; pages
+// that 64 sequences share would take 316 us so instead of 276.
+DEV void dma16_once(v4i32 rsrc, uint32_t voff, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(lds_base)), "v"(voff), "s"(rsrc)
+               : "memory", "m0");
+}
 
 // Keys and values of one segment, tile by tile into a group's ring.
 template <int HD, int RB>
@@ -207,9 +262,10 @@ struct Keys {
   size_t head;              // bytes of the heads before this one
   int len, n, tc, lps;
   int win, ids;             // the lane's entry of the table, pages win..win+63
+  int refs;                 // sequences that have the piece's first page; 0 where other rows walk it too
   uint64_t seen;            // of the last tile issued: keys that are there
 
-  DEV void init(const TreeArgs& args, int s, const Seq& q, int j) {
+  DEV void init(const TreeArgs& args, int s, const Seq& q, int j, int f0) {
     a = &args;
     table = args.table + (size_t)s * args.max_pages;
     const int slots = args.H + 2 * args.Hkv;
@@ -222,7 +278,10 @@ struct Keys {
     n = q.n;
     tc = q.tc;
     lps = 31 - __builtin_clz(args.ps);
-    win = -64;
+    win = f0 * W::KT >> lps;
+    ids = table[min(win + (int)(threadIdx.x & 63), args.max_pages - 1)];
+    const int page = __builtin_amdgcn_readfirstlane(ids);
+    refs = RB == 1 && q.blocks == 1 && (unsigned)page < (unsigned)args.n_pages ? args.refs[page] : 0;
   }
 
   // the lane's part of load i of 16 rows that are `stride` bytes apart
@@ -231,7 +290,7 @@ struct Keys {
     return (uint32_t)row * stride + (uint32_t)c * 16u;
   }
   // by the waves of a group, `wave` of RB
-  DEV void issue(int f, lds_char_t* st, int wave) {
+  DEV void issue(int f, lds_char_t* st, int wave, bool once) {
     constexpr int SIXTEENS = W::KT / 16;
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));   // offsets are made again for each tile: kept, they would leave too few registers
@@ -255,6 +314,14 @@ struct Keys {
         const char* k = reinterpret_cast<const char*>(a->pages) + (size_t)(there ? page_of(key) : 0) * page_bytes + head +
                         (size_t)(key & (a->ps - 1)) * HD * 2;
         const v4i32 rk = make_rsrc(k, (uint32_t)there * HD * 2), rv = make_rsrc(k + v_bytes, (uint32_t)there * HD * 2);
+        if (RB == 1 && once) {
+#pragma unroll
+          for (int i = 0; i < PER; ++i) {
+            dma16_once(rk, offset(i, lane, HD * 2), lds_addr(st + (q * PER + i) * 1024));
+            dma16_once(rv, offset(i, lane, HD * 2), lds_addr(st + W::TB + (q * PER + i) * 1024));
+          }
+          continue;
+        }
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
           dma16(rk, offset(i, lane, HD * 2), lds_addr(st + (q * PER + i) * 1024));
@@ -282,32 +349,16 @@ struct Keys {
 };
 
 DEV bool special(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
-// Of 32 rows of values, those with an element that is not finite.
+// Whether an element of 32 rows of values is not finite.
 template <int HD>
-DEV uint32_t not_finite(const lds_char_t* vs, int lane) {
-  constexpr int U = HD / 8;
-  uint32_t bad = 0;
+DEV bool not_finite(const lds_char_t* vs, int lane) {
+  bool hit = false;
 #pragma unroll 4
-  for (int i = 0; i < U / 2; ++i) {
+  for (int i = 0; i < HD / 16; ++i) {
     const v4u32 x = *reinterpret_cast<const lds_v4u32_t*>(vs + (i * 64 + lane) * 16);
-    const uint64_t hit = __ballot(special(x.x) || special(x.y) || special(x.z) || special(x.w));
-    if (hit) {
-#pragma unroll
-      for (int r = 0; r < 64 / U; ++r)
-        if (hit >> (r * U) & ((1ull << U) - 1)) bad |= 1u << (i * (64 / U) + r);
-    }
+    hit |= special(x.x) || special(x.y) || special(x.z) || special(x.w);
   }
-  return bad;
-}
-// ... and without them.
-DEV bf16x8 finite(bf16x8 v) {
-  v4u32 x = __builtin_bit_cast(v4u32, v);
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    if ((x[k] & 0x7f80u) == 0x7f80u) x[k] &= 0xffff0000u;
-    if ((x[k] & 0x7f800000u) == 0x7f800000u) x[k] &= 0xffffu;
-  }
-  return __builtin_bit_cast(bf16x8, x);
+  return __ballot(hit) != 0;
 }
 
 DEV float inverse(float l) { return l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l; }   // a row that sees nothing: 0
@@ -327,34 +378,50 @@ __global__ __launch_bounds__(256, RB == 1 ? 1 : 2) void tree_kernel(TreeArgs a) 
   line.init(a);
   if (blockIdx.x == 0 && wave == 0 && !line.planned) {   // for the launch that joins
     if (lane < a.n_seq) a.plan[lane] = line.base;
-    if (lane == 0) {
-      a.plan[a.n_seq] = line.total;
-      a.plan[a.n_seq + 1] = line.segments;
-    }
+    if (lane == 0) store_cuts(a, line.sum, line.cuts);
   }
-  const bool solo = line.cuts.solo;
+  const bool solo = line.cuts.x == SOLO, dealt = line.cuts.x == DEALT;
   const int me = solo ? blockIdx.x * 4 + wave : blockIdx.x;
   const int first = solo ? 0 : group, step = solo ? 1 : W::GROUPS;
-  if ((long)me * line.cuts.share >= line.total) return;
-  const int end = line.bound(a, me + 1);
-  for (int p = line.bound(a, me); p < end;) {
+  int p, end;
+  if (dealt) {
+    p = me;
+    end = min(me + 1, line.sum);
+  } else {
+    if ((long)me * line.cuts.y >= line.sum) return;
+    p = line.bound(a, me);
+    end = line.bound(a, me + 1);
+  }
+  while (p < end) {
     int before;
     const int s = line.find(a, p, &before);
     const Seq q = line.seq(a, s);
-    const int seg = (p - before) / q.t, block = seg / a.Hkv, j = seg - block * a.Hkv;
-    const int from = before + seg * q.t;
-    const int f0 = p - from, f1 = min(end - from, q.t);
-    p = from + f1;
+    int seg, f0, f1;
+    if (dealt) {
+      const int n = pieces_of<W>(q.t, line.cuts.y);
+      seg = (p - before) / n;
+      const int k = p - before - seg * n;
+      const int least = q.t / n, more = q.t - least * n;   // tiles of a piece; pieces that have one more
+      f0 = k * least + min(k, more);
+      f1 = f0 + least + (k < more);
+      p = end;
+    } else {
+      seg = (p - before) / q.t;
+      const int from = before + seg * q.t;
+      f0 = p - from;
+      f1 = min(end - from, q.t);
+      p = from + f1;
+    }
+    const int block = seg / a.Hkv, j = seg - block * a.Hkv;
     // a block of rows without a mask needs the new tokens up to its last only
     const int last = min(((block + 1) * W::ROWS - 1) / G, q.n - 1);
     const int f_end = a.mask ? f1 : min(f1, q.tc + last / KT + 1);
 
     Keys<HD, RB> keys;
-    keys.init(a, s, q, j);
+    keys.init(a, s, q, j, f0);
     auto stage = [&](int it) { return ring + it % W::STAGES * 2 * W::TB; };
-    if (f0 + first < f_end) keys.issue(f0 + first, stage(0), rw);
+    if (f0 + first < f_end) keys.issue(f0 + first, stage(0), rw, false);
     uint64_t next_seen = keys.seen;
-
     const int row = block * W::ROWS + 32 * rw + lq;
     const bool on = row < q.n * G;
     const int r = min(row, q.n * G - 1), i = r / G, h = j * G + r - i * G;
@@ -375,7 +442,9 @@ __global__ __launch_bounds__(256, RB == 1 ? 1 : 2) void tree_kernel(TreeArgs a) 
       if constexpr (RB > 1) block_barrier();
       const uint64_t there = next_seen;
       if (f + step < f_end) {
-        keys.issue(f + step, stage(it + 1), rw);
+        int refs = keys.refs;
+        asm volatile("" : "+v"(refs));   // not waited for before
+        keys.issue(f + step, stage(it + 1), rw, __builtin_amdgcn_readfirstlane(refs) == 1);
         next_seen = keys.seen;
       }
       if (f >= f_end) continue;
@@ -385,7 +454,7 @@ __global__ __launch_bounds__(256, RB == 1 ? 1 : 2) void tree_kernel(TreeArgs a) 
         const lds_char_t* Ks = stage(it) + sub * 64 * HD;
         const lds_char_t* Vs = Ks + W::TB;
         // the keys that this lane's row sees
-        uint32_t mine = (uint32_t)(there >> (32 * sub)), bad = 0;
+        uint32_t mine = (uint32_t)(there >> (32 * sub));
         const bool drafted = f >= q.tc;
         if (drafted) {
           const int d0 = (f - q.tc) * KT + 32 * sub;
@@ -394,7 +463,7 @@ __global__ __launch_bounds__(256, RB == 1 ? 1 : 2) void tree_kernel(TreeArgs a) 
         }
         if (__ballot(mine != 0) == 0) continue;
         const bool all = __ballot(mine != ~0u) == 0;
-        if (drafted && !all) bad = not_finite<HD>(Vs, lane);
+        const bool bad = drafted && !all && not_finite<HD>(Vs, lane);
 
         floatx16 x;
         zero(x);
@@ -432,27 +501,18 @@ __global__ __launch_bounds__(256, RB == 1 ? 1 : 2) void tree_kernel(TreeArgs a) 
           rsum += w;
         }
         l_run += sum32(rsum);
-        auto add_values = [&](auto clean) {
+        if (!bad) {
 #pragma unroll
           for (int hh = 0; hh < 2; ++hh) {
             const bf16x8 pf = acc_slots(x, hh);
 #pragma unroll
-            for (int d = 0; d < S::DT; ++d) {
-              bf16x8 v = read_tr<HD>(Vs, 32 * d, 16 * hh, lane);
-              if constexpr (decltype(clean)::value) v = finite(v);
-              o[d] = mfma32(v, pf, o[d]);
-            }
+            for (int d = 0; d < S::DT; ++d) o[d] = mfma32(read_tr<HD>(Vs, 32 * d, 16 * hh, lane), pf, o[d]);
           }
-        };
-        if (bad == 0) {
-          add_values(std::false_type{});
           continue;
         }
-        add_values(std::true_type{});
-        // what was left out, one token after another
-        while (bad) {
-          const int k = __builtin_ctz(bad);
-          bad &= bad - 1;
+        // one token after another, for the rows that see it (0 times infinity would reach the others)
+#pragma unroll 1
+        for (int k = 0; k < 32; ++k) {
           float w = 0.0f;
 #pragma unroll
           for (int e = 0; e < 16; ++e) w = (k & ~4) == acc_row(e, 0) ? x[e] : w;
@@ -466,51 +526,71 @@ __global__ __launch_bounds__(256, RB == 1 ? 1 : 2) void tree_kernel(TreeArgs a) 
                   uint2, *reinterpret_cast<const LDS_AS floatx2*>(Vs + unit<HD>(k, 4 * d + c) * 16 + 8 * g));
               const float y[4] = {lo_f(v.x), hi_f(v.x), lo_f(v.y), hi_f(v.y)};
 #pragma unroll
-              for (int e = 0; e < 4; ++e) o[d][4 * c + e] += w * (sees & !isfinite(y[e]) ? y[e] : 0.0f);
+              for (int e = 0; e < 4; ++e) o[d][4 * c + e] += w * (sees ? y[e] : 0.0f);
               __builtin_amdgcn_sched_barrier(0);   // one read at a time: this path keeps few registers
             }
         }
       }
     }
 
+    // columns 32 d.. of O that this wave has in the end
+    auto has = [&](int d) { return W::GROUPS == 1 || solo || d / W::PER == group; };
     if constexpr (W::GROUPS > 1) {
       if (!solo) {
-        // the other groups' results through LDS, joined in order
+        // the groups' results through LDS, joined in order, each by the group that has its columns
         __syncthreads();
-        lds_char_t* keep = (lds_char_t*)smem_raw + ((group - 1) * RB + rw) * W::KEEP + lane * 16;
-        if (group > 0) {
+        auto kept = [&](int of) { return (lds_char_t*)smem_raw + (of * RB + rw) * W::KEEP; };
+        auto column = [&](int of, int d) { return kept(of) + 512 + (d - (d / W::PER > of ? W::PER : 0)) * 4096 + lane * 16; };
+        const int groups = min(W::GROUPS, max(f_end - f0, 1));   // that had a tile
+        if (group < groups) {
+          *reinterpret_cast<LDS_AS floatx2*>(kept(group) + lane * 8) = floatx2{m_run, l_run};
 #pragma unroll
           for (int d = 0; d < S::DT; ++d)
+            if (d / W::PER != group) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
-              *reinterpret_cast<lds_v4f32_t*>(keep + (d * 4 + c) * 1024) =
-                  v4f32{o[d][4 * c], o[d][4 * c + 1], o[d][4 * c + 2], o[d][4 * c + 3]};
-          *reinterpret_cast<LDS_AS floatx2*>(keep + S::DT * 4096 - lane * 8) = floatx2{m_run, l_run};
+              for (int c = 0; c < 4; ++c)
+                *reinterpret_cast<lds_v4f32_t*>(column(group, d) + c * 1024) =
+                    v4f32{o[d][4 * c], o[d][4 * c + 1], o[d][4 * c + 2], o[d][4 * c + 3]};
+            }
         }
         __syncthreads();
-        if (group == 0) {
+        float m = -INFINITY, l = 0.0f, weight[W::GROUPS];
 #pragma unroll
-          for (int k = 1; k < W::GROUPS; ++k) {
-            const lds_char_t* other = keep + k * RB * W::KEEP;
-            const floatx2 ml = *reinterpret_cast<const LDS_AS floatx2*>(other + S::DT * 4096 - lane * 8);
-            const float m = fmaxf(m_run, ml.x);
-            const float w0 = m_run == -INFINITY ? 0.0f : fast_exp2(m_run - m);
-            const float w1 = ml.x == -INFINITY ? 0.0f : fast_exp2(ml.x - m);
+        for (int k = 0; k < W::GROUPS; ++k) {
+          weight[k] = -INFINITY;
+          if (k < groups) {
+            weight[k] = reinterpret_cast<const LDS_AS floatx2*>(kept(k) + lane * 8)->x;
+            m = fmaxf(m, weight[k]);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < W::GROUPS; ++k)
+          if (k < groups) {
+            const float lk = reinterpret_cast<const LDS_AS floatx2*>(kept(k) + lane * 8)->y;
             // (sums of rows that met a NaN have no maximum, but count)
-            l_run = (m_run == -INFINITY ? l_run : l_run * w0) + (ml.x == -INFINITY ? ml.y : ml.y * w1);
-            m_run = m;
+            l += weight[k] == -INFINITY ? lk : lk * fast_exp2(weight[k] - m);
+            weight[k] = weight[k] == -INFINITY ? 0.0f : fast_exp2(weight[k] - m);
+          }
+        m_run = m;
+        l_run = l;
 #pragma unroll
-            for (int d = 0; d < S::DT; ++d)
+        for (int d = 0; d < S::DT; ++d) {
+          if (d / W::PER != group) continue;
+          const floatx16 own = o[d];
+          zero(o[d]);
 #pragma unroll
-              for (int c = 0; c < 4; ++c) {
-                const v4f32 y = *reinterpret_cast<const lds_v4f32_t*>(other + (d * 4 + c) * 1024);
+          for (int k = 0; k < W::GROUPS; ++k) {
+            if (k >= groups) continue;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[d][4 * c + e] = o[d][4 * c + e] * w0 + y[e] * w1;
-              }
+            for (int c = 0; c < 4; ++c) {
+              v4f32 y = {own[4 * c], own[4 * c + 1], own[4 * c + 2], own[4 * c + 3]};
+              if (k != d / W::PER) y = *reinterpret_cast<const lds_v4f32_t*>(column(k, d) + c * 1024);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[d][4 * c + e] += y[e] * weight[k];
+            }
           }
         }
         __syncthreads();   // the rings are the next segment's
-        if (group > 0) continue;
       }
     } else {
       __syncthreads();
@@ -521,24 +601,28 @@ __global__ __launch_bounds__(256, RB == 1 ? 1 : 2) void tree_kernel(TreeArgs a) 
       bf16_t* out = a.out + (token * a.H + h) * HD;
 #pragma unroll
       for (int d = 0; d < S::DT; ++d)
+        if (has(d)) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-          *reinterpret_cast<uint2*>(out + 32 * d + 8 * c + 4 * g) =
-              make_uint2(pack2(o[d][4 * c] * inv, o[d][4 * c + 1] * inv),
-                         pack2(o[d][4 * c + 2] * inv, o[d][4 * c + 3] * inv));
-      if (g == 0 && a.lse) a.lse[(size_t)h * a.n_rows + token] = (m_run + log2f(l_run)) * LN2;
+          for (int c = 0; c < 4; ++c)
+            *reinterpret_cast<uint2*>(out + 32 * d + 8 * c + 4 * g) =
+                make_uint2(pack2(o[d][4 * c] * inv, o[d][4 * c + 1] * inv),
+                           pack2(o[d][4 * c + 2] * inv, o[d][4 * c + 3] * inv));
+        }
+      if (g == 0 && has(0) && a.lse) a.lse[(size_t)h * a.n_rows + token] = (m_run + log2f(l_run)) * LN2;
       continue;
     }
-    // a share has at most two cut segments: one that begins in it, one that does not
+    // a share of the line has at most two cut segments: one that begins in it, one that does not
     const int prows = part_rows(a, W::ROWS), pr = 32 * rw + lq;
-    float* part = a.part + (2 * (size_t)me + (f0 == 0)) * part_floats(a, W::ROWS, HD);
+    float* part = a.part + (dealt ? (size_t)me : 2 * (size_t)me + (f0 == 0)) * part_floats(a, W::ROWS, HD);
 #pragma unroll
     for (int d = 0; d < S::DT; ++d)
+      if (has(d)) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-        *reinterpret_cast<float4*>(part + (size_t)pr * HD + 32 * d + 8 * c + 4 * g) =
-            make_float4(o[d][4 * c], o[d][4 * c + 1], o[d][4 * c + 2], o[d][4 * c + 3]);
-    if (g == 0) {
+        for (int c = 0; c < 4; ++c)
+          *reinterpret_cast<float4*>(part + (size_t)pr * HD + 32 * d + 8 * c + 4 * g) =
+              make_float4(o[d][4 * c], o[d][4 * c + 1], o[d][4 * c + 2], o[d][4 * c + 3]);
+      }
+    if (g == 0 && has(0)) {
       part[(size_t)prows * HD + pr] = m_run;
       part[(size_t)prows * HD + prows + pr] = l_run;
     }
@@ -564,22 +648,31 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : 64 * WPR) void tree_join_kernel(Tr
     if (b) s = s0 + 63 - __builtin_clzll(b);
   }
   if (s < 0) return;
-  const int total = a.plan[a.n_seq], segments = a.plan[a.n_seq + 1], before = a.plan[s];
+  const int before = a.plan[s];
+  const Cuts cuts = {a.plan[a.n_seq + 1], a.plan[a.n_seq + 2], a.plan[a.n_seq + 3], 0};
   const Seq q = seq_of<W>(a, s);
   const int i = token - q.start;
   if (i < 0 || i >= q.n) return;
-  const Cuts cuts = cuts_of<W>(total, segments);
   const int j = h / G, r = i * G + h - j * G, block = r / W::ROWS, row = r - block * W::ROWS;
-  const int from = before + (block * a.Hkv + j) * q.t;
-  // cuts w0..w1 lie inside the segment, so shares w0 - 1..w1 have its parts
-  const int w0 = (from + cuts.slack) / cuts.share + 1, w1 = (from + q.t - cuts.slack - 1) / cuts.share;
-  if (w1 < w0) return;
-  const int parts = w1 - w0 + 2;
   const int prows = part_rows(a, W::ROWS);
   const size_t floats = part_floats(a, W::ROWS, HD);
-  const float* part0 = a.part + 2 * (size_t)(w0 - 1) * floats;
-  // part k's place: the first begins in its share, the others do not
-  auto place = [&](int k) { return part0 + (2 * (size_t)k + (k == 0)) * floats; };
+  int parts;
+  const float* part0;
+  const bool dealt = cuts.x == DEALT;
+  if (dealt) {
+    parts = pieces_of<W>(q.t, cuts.y);
+    if (parts < 2) return;
+    part0 = a.part + (size_t)(before + (block * a.Hkv + j) * parts) * floats;
+  } else {
+    const int from = before + (block * a.Hkv + j) * q.t;
+    // cuts w0..w1 lie inside the segment, so shares w0 - 1..w1 have its parts
+    const int w0 = (from + cuts.z) / cuts.y + 1, w1 = (from + q.t - cuts.z - 1) / cuts.y;
+    if (w1 < w0) return;
+    parts = w1 - w0 + 2;
+    part0 = a.part + 2 * (size_t)(w0 - 1) * floats;
+  }
+  // part k's place: of the line's, the first begins in its share, the others do not
+  auto place = [&](int k) { return part0 + (dealt ? (size_t)k : 2 * (size_t)k + (k == 0)) * floats; };
   // this wave's parts
   const int k_begin = (int)((long)parts * wave / WPR) * (WPR > 1), k_end = WPR > 1 ? (int)((long)parts * (wave + 1) / WPR) : parts;
   float m = -INFINITY;
@@ -673,7 +766,7 @@ size_t tree_workspace(const TreeArgs& a, size_t* part_at) {
     using W = Walk<decltype(hd)::value, decltype(rb)::value>;
     double segment;
     if (most_tiles<W>(a, &segment) > 2e9) return 0;   // tiles are counted in 32 bits
-    *part_at = (((size_t)a.n_seq + 2) * sizeof(int32_t) + 255) / 256 * 256;
+    *part_at = (((size_t)a.n_seq + 4) * sizeof(int32_t) + 255) / 256 * 256;
     return *part_at + (segment > W::LEAST ? 2 * (size_t)W::MOST * part_floats(a, W::ROWS, W::HEAD) * sizeof(float) : 0);
   });
 }
@@ -686,7 +779,7 @@ hipError_t launch_tree(const TreeArgs& a, hipStream_t s) {
     double segment;
     const double tiles = most_tiles<W>(a, &segment);
     if (a.n_seq > 64) hipLaunchKernelGGL((tree_plan_kernel<W>), dim3(1), dim3(64), 0, s, a);
-    const unsigned teams = (unsigned)std::min((double)W::TEAMS, std::ceil(tiles / W::LEAST));
+    const unsigned teams = (unsigned)std::min((double)W::TEAMS, tiles);
     hipLaunchKernelGGL((tree_kernel<HD, RB>), dim3(teams), dim3(256), 0, s, a);
     if (segment > W::LEAST) {
       const long rows = (long)a.n_rows * a.H;
