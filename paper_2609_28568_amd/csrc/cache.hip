@@ -17,18 +17,13 @@ namespace {
 
 constexpr int BOOK = 1024;   // threads of the one workgroup that keeps the books
 constexpr int WAVES = BOOK / 64;
+struct __attribute__((packed, aligned(4))) Four { int32_t r[4]; };
 
-// Exclusive prefix sum of v over the workgroup, in thread order; *total: the sum.
-// `parts`: WAVES ints of LDS, free again after a barrier.
-DEV int block_scan(int v, int* parts, int* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int x = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(x, o);
-    if (lane >= o) x += y;
-  }
-  if (lane == 63) parts[wave] = x;
+// Exclusive prefix sum of v over the workgroup's waves, in their order (v the
+// wave's own); *total: the sum. `parts`: WAVES ints of LDS of their own.
+DEV int waves_before(int v, int* parts, int* total) {
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) parts[wave] = v;
   __syncthreads();
   int before = 0, all = 0;
 #pragma unroll
@@ -38,7 +33,59 @@ DEV int block_scan(int v, int* parts, int* total) {
     all += p;
   }
   *total = all;
-  return before + x - v;
+  return before;
+}
+// ... over its threads.
+DEV int threads_before(int v, int* parts, int* total) {
+  const int lane = threadIdx.x & 63;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  return waves_before(__builtin_amdgcn_readlane(x, 63), parts, total) + x - v;
+}
+
+// The pages of a wave's run, four a lane, 256 a step: f(first of the lane's four,
+// a bit for each of them that someone holds, bits that are pages).
+template <class Fn>
+DEV void each_page(const CacheArgs& c, Fn f) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int run = ((c.n_pages + WAVES * 256 - 1) / (WAVES * 256)) * 256, p1 = min((wave + 1) * run, c.n_pages);
+  for (int p0 = wave * run; p0 < p1; p0 += 256) {
+    const int p = p0 + 4 * lane;
+    uint32_t held = 0, there = 0;
+    int r[4] = {0, 0, 0, 0};
+    if (p + 4 <= p1) {
+      const Four q = *reinterpret_cast<const Four*>(c.refs + p);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) r[k] = q.r[k];
+      there = 15;
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (p + k < p1) {
+          r[k] = c.refs[p + k];
+          there |= 1u << k;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) held |= r[k] != 0 ? 1u << k : 0u;
+    f(p, held & there, there);
+  }
+}
+// How many of a lane's four pages that `bits` names there are in the lanes before; *all: in the wave.
+DEV int lanes_before(uint32_t bits, int* all) {
+  int before = 0, sum = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint64_t b = __ballot(bits >> k & 1);
+    before += __popcll(b & ((1ull << (threadIdx.x & 63)) - 1));
+    sum += __popcll(b);
+  }
+  *all = sum;
+  return before;
 }
 
 DEV int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
@@ -106,11 +153,12 @@ __global__ __launch_bounds__(BOOK) void append_book_kernel(CacheArgs c, AppendAr
   const int tid = threadIdx.x;
   if (tid == 0) copies = 0;
 
-  // free pages of this thread's run
-  const int per = (c.n_pages + BOOK - 1) / BOOK, p0 = min(tid * per, c.n_pages), p1 = min(p0 + per, c.n_pages);
-  int nfree = 0;
-#pragma unroll 4
-  for (int p = p0; p < p1; ++p) nfree += c.refs[p] == 0;
+  int nfree = 0;   // of the wave's run of pages
+  each_page(c, [&](int, uint32_t held, uint32_t there) {
+    int n;
+    lanes_before(there & ~held, &n);
+    nfree += n;
+  });
 
   const int each = (c.n_seq + BOOK - 1) / BOOK;
   int need = 0, over = 0;
@@ -132,15 +180,16 @@ __global__ __launch_bounds__(BOOK) void append_book_kernel(CacheArgs c, AppendAr
     rec[s] = make_int4(d.len, d.n, page, -1);
   }
   int total, nfrees, overs;
-  const int before = block_scan(need, parts[0], &total);
-  const int rank0 = block_scan(nfree, parts[1], &nfrees);
-  block_scan(over, parts[2], &overs);
+  const int before = threads_before(need, parts[0], &total);
+  int rank = waves_before(nfree, parts[1], &nfrees);
+  threads_before(over, parts[2], &overs);
   const int missing = max(0, total - nfrees) + overs;
-  if (tid == 0) {
-    *c.missing = missing;
-    head[0] = missing == 0;
+  if (tid == 0) *c.missing = missing;
+  if (missing) {   // nothing to move
+    for (int s = tid; s < c.n_seq; s += BOOK) rec[s] = make_int4(0, 0, -1, -1);
+    if (tid == 0) head[0] = 0;
+    return;
   }
-  if (missing) return;
   for (int k = 0; k < each; ++k) {
     const int s = tid * each + k;
     if (s >= c.n_seq) break;
@@ -149,11 +198,18 @@ __global__ __launch_bounds__(BOOK) void append_book_kernel(CacheArgs c, AppendAr
     c.lens[s] = r.x + r.y;
     if (r.z >= 0) copying[atomicAdd(&copies, 1)] = s;
   }
-  int rank = rank0;
-  for (int p = p0; p < p1 && rank < total; ++p)
-    if (c.refs[p] == 0) freed[rank++] = p;
+  each_page(c, [&](int p, uint32_t held, uint32_t there) {
+    int n, at = rank + lanes_before(there & ~held, &n);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if ((there & ~held) >> k & 1) {
+        if (at < total) freed[at] = p + k;
+        ++at;
+      }
+    rank += n;
+  });
   __syncthreads();
-  if (tid == 0) head[1] = copies;
+  if (tid == 0) head[0] = copies;
   for (int i = tid; i < total; i += BOOK) {
     int lo = 0, hi = c.n_seq - 1;   // the first sequence whose end lies past i
     while (lo < hi) {
@@ -179,10 +235,8 @@ DEV size_t page_at(const CacheArgs& c, int layer, int page) {   // in elements
 // Tokens into their places, a wave `tok` tokens of one sequence and layer, and
 // behind those blocks the shared pages' tokens, a wave one head of one page.
 __global__ __launch_bounds__(64) void append_move_kernel(CacheArgs c, AppendArgs a, int tok, int groups, unsigned nt) {
-  const int32_t* head = c.scratch;
   const int4* rec = reinterpret_cast<const int4*>(c.scratch + CACHE_HEADER);
   const int lane = threadIdx.x;
-  if (!head[0]) return;
   const int hu = c.hd / 8, units = 2 * c.Hkv * hu;   // 16-byte units of a head, of a token
   if (blockIdx.x < nt) {
     const int layer = blockIdx.y;
@@ -215,12 +269,16 @@ __global__ __launch_bounds__(64) void append_move_kernel(CacheArgs c, AppendArgs
       }
 #pragma unroll
       for (int k = 0; k < FLIGHT; ++k)
-        if (to[k]) *reinterpret_cast<uint4*>(to[k]) = v[k];
+        if (to[k]) {
+          // (prompts of a batch, 600 MB: 143 us through the caches, 136 past them)
+          if (tok > 1) st_stream(reinterpret_cast<uint4*>(to[k]), v[k]);
+          else *reinterpret_cast<uint4*>(to[k]) = v[k];
+        }
     }
     return;
   }
   const int32_t* copying = c.scratch + CACHE_HEADER + 4 * c.n_seq;
-  const int layer = blockIdx.y, n = head[1] * 2 * c.Hkv;
+  const int layer = blockIdx.y, n = c.scratch[0] * 2 * c.Hkv;
   for (int i = blockIdx.x - nt; i < n; i += gridDim.x - nt) {
     const int s = copying[i / (2 * c.Hkv)], h = i % (2 * c.Hkv);
     const int4 r = rec[s];
@@ -240,23 +298,36 @@ __global__ __launch_bounds__(BOOK) void compact_book_kernel(CacheArgs c) {
   int32_t* holes = c.scratch + CACHE_HEADER + 4 * c.n_seq;   // the k-th move's target
   int32_t* from = holes + c.n_pages;                         // ... and source
   const int tid = threadIdx.x;
-  const int per = (c.n_pages + BOOK - 1) / BOOK, p0 = min(tid * per, c.n_pages), p1 = min(p0 + per, c.n_pages);
-  int mine = 0, used, moves, nholes;
-#pragma unroll 4
-  for (int p = p0; p < p1; ++p) mine += c.refs[p] != 0;
-  const int before = block_scan(mine, parts[0], &used);   // pages in use below this thread's run
-  // of pages below `used`, those not in use; of pages from there on, those in use
-  const int below = clampi(used - p0, 0, p1 - p0);
-  int low = 0;
-  for (int p = p0; p < p0 + below; ++p) low += c.refs[p] != 0;
-  int hole = block_scan(below - low, parts[1], &nholes);
-  int move = block_scan(mine - low, parts[2], &moves);
-  (void)before;
-  for (int p = p0; p < p1; ++p) {
-    const bool on = c.refs[p] != 0;
-    if (p < used && !on) holes[hole++] = p;
-    if (p >= used && on) from[move++] = p;
-  }
+  int mine = 0, used, nholes, moves;
+  each_page(c, [&](int, uint32_t held, uint32_t) {
+    int n;
+    lanes_before(held, &n);
+    mine += n;
+  });
+  waves_before(mine, parts[0], &used);   // pages in use
+  // of pages below `used` those that are free, of the others those in use
+  auto below = [&](int p) { return p >= used ? 0u : p + 4 <= used ? 15u : (1u << (used - p)) - 1; };
+  int hole = 0, move = 0;
+  each_page(c, [&](int p, uint32_t held, uint32_t there) {
+    int n;
+    lanes_before(there & ~held & below(p), &n);
+    hole += n;
+    lanes_before(held & ~below(p), &n);
+    move += n;
+  });
+  hole = waves_before(hole, parts[1], &nholes);
+  move = waves_before(move, parts[2], &moves);
+  each_page(c, [&](int p, uint32_t held, uint32_t there) {
+    const uint32_t h = there & ~held & below(p), m = held & ~below(p);
+    int nh, nm, at = hole + lanes_before(h, &nh), to = move + lanes_before(m, &nm);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (h >> k & 1) holes[at++] = p + k;
+      if (m >> k & 1) from[to++] = p + k;
+    }
+    hole += nh;
+    move += nm;
+  });
   if (tid == 0) {
     head[0] = moves;
     head[1] = used;
@@ -300,7 +371,8 @@ __global__ __launch_bounds__(256) void compact_move_kernel(CacheArgs c) {
     const int n = min(4, (units - u0) / 256);
     uint4 v[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = q < n ? src[q * 256 + threadIdx.x] : make_uint4(0, 0, 0, 0);
+    for (int q = 0; q < 4; ++q)   // (past the caches: 178 MB of pages 53 -> 48 us a pass)
+      v[q] = q < n ? ld_stream(src + q * 256 + threadIdx.x) : make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int q = 0; q < 4; ++q)
       if (q < n) dst[q * 256 + threadIdx.x] = v[q];

@@ -13,7 +13,7 @@ import ctypes
 import struct
 
 from .binding import i32, on_stream
-from .qwen3_binding import _check, _device_rows, _ptr, lib as _lib_qwen3
+from .qwen3_binding import _check, _device_rows, lib as _lib_qwen3
 
 
 class Cache(ctypes.Structure):
@@ -96,7 +96,8 @@ class PagedCache:
             setattr(c, "d_" + name, getattr(self, name).data_ptr())
         self._c, self._ref = c, ctypes.byref(c)
         self._stream = torch.cuda.current_stream(pages.device).cuda_stream
-        self._trees = {}
+        self._n_seq, self._index = n_seq, pages.get_device()
+        self._trees, self._heads = {}, {}
 
     @classmethod
     def empty(cls, n_layer, n_pages, n_kv_head, page_size, head_dim, n_seq, max_pages, device="cuda"):
@@ -107,34 +108,46 @@ class PagedCache:
         return cls(pages, new((n_seq, max_pages), -1), new((n_seq,), 0), new((n_pages,), 0), new((1,), 0))
 
     def _run(self, fn, *args):
-        def call(*args):
-            if args[-1] != self._stream:   # the scratch is another stream's: it stays until this one is done with it
-                self.scratch.record_stream(self.torch.cuda.current_stream(self.pages.device))
-            return fn(self._ref, *args)
-        _check(on_stream(self.pages.device, call, *args))
+        torch, index = self.torch, self._index
+        stream = torch._C._cuda_getCurrentRawStream(index)
+        if stream != self._stream:   # the scratch is another stream's: it stays until this one is done with it
+            self.scratch.record_stream(torch.cuda.current_stream(index))
+        if torch.cuda.current_device() == index:
+            _check(fn(self._ref, *args, stream))
+        else:
+            with torch.cuda.device(index):
+                _check(fn(self._ref, *args, stream))
+
+    def _given(self, t, name, shape, dtype):
+        torch = self.torch
+        if not (type(t) is torch.Tensor and t.dtype is dtype and t.shape == shape and t.get_device() == self._index
+                and t.is_contiguous()):
+            _device_rows(t, name, dtype, self.pages, shape)
+        return t.data_ptr()
 
     def _ints(self, t, name, shape):
-        return _device_rows(t, name, self.torch.int32, self.pages, shape)
+        return self._given(t, name, shape, self.torch.int32)
 
     def fork(self, src, keep=None):
         """Sequence s becomes the first keep[s] tokens (None: all) of what
         sequence src[s] was; src[s] -1: it is freed (qwen3_cache_fork)."""
-        n = self._c.n_seq
-        self._ints(src, "src", (n,))
-        if keep is not None:
-            self._ints(keep, "keep", (n,))
-        self._run(lib().qwen3_cache_fork, src.data_ptr(), _ptr(keep))
+        n = (self._n_seq,)
+        self._run(lib().qwen3_cache_fork, self._ints(src, "src", n), None if keep is None else self._ints(keep, "keep", n))
 
     def _rows(self, qkv, layers):
-        """(n_head, rows) of q | k | v rows of `layers` layers."""
-        c = self._c
-        _device_rows(qkv, "q | k | v", self.torch.bfloat16, self.pages)
-        if qkv.dim() != (2 if layers is None else 3) or (layers is not None and qkv.shape[0] != layers):
-            raise ValueError("rows of q | k | v are [rows, (n_head + 2 n_kv_head) head_dim], of every layer for append")
-        n_head = qkv.shape[-1] // c.head_dim - 2 * c.n_kv_head
-        if n_head < 1 or qkv.shape[-1] % c.head_dim:
-            raise ValueError("rows of q | k | v are (n_head + 2 n_kv_head) head_dim wide")
-        return i32(n_head), i32(qkv.shape[-2])
+        """(n_head, rows, address) of q | k | v rows, of `layers` layers or (0) of one."""
+        shape = tuple(qkv.shape)
+        got = self._heads.get((shape, layers))
+        if got is None:
+            if len(shape) != (3 if layers else 2) or (layers and shape[0] != layers):
+                raise ValueError("rows of q | k | v are [rows, (n_head + 2 n_kv_head) head_dim], of every layer for append")
+            n_head = shape[-1] // self._c.head_dim - 2 * self._c.n_kv_head
+            if n_head < 1 or shape[-1] % self._c.head_dim:
+                raise ValueError("rows of q | k | v are (n_head + 2 n_kv_head) head_dim wide")
+            if len(self._heads) >= 256:
+                self._heads.clear()
+            got = self._heads[shape, layers] = i32(n_head), i32(shape[-2])
+        return (*got, self._given(qkv, "q | k | v", qkv.shape, self.torch.bfloat16))
 
     def append(self, qkv, starts, max_new, counts=None, path=None):
         """Keys and values of new tokens, of all layers (qwen3_cache_append):
@@ -143,25 +156,20 @@ class PagedCache:
         counts[s] (None: all), or those that path int32 [n_seq, max_new] names.
         `short` then holds the number of pages that were missing; unless it is
         0 nothing was appended."""
-        c = self._c
         if qkv.dim() == 2:
             qkv = qkv[None]
-        n_head, rows = self._rows(qkv, c.n_layer)
-        max_new = i32(max_new)
-        self._ints(starts, "starts", (c.n_seq + 1,))
-        if counts is not None:
-            self._ints(counts, "counts", (c.n_seq,))
-        if path is not None:
-            self._ints(path, "path", (c.n_seq, max_new))
-        self._run(lib().qwen3_cache_append, qkv.data_ptr(), n_head, rows, rows * qkv.shape[2], starts.data_ptr(),
-                  _ptr(counts), _ptr(path), max_new)
+        n_head, rows, at = self._rows(qkv, self._c.n_layer)
+        max_new, n = i32(max_new), self._n_seq
+        self._run(lib().qwen3_cache_append, at, n_head, rows, rows * qkv.shape[2], self._ints(starts, "starts", (n + 1,)),
+                  None if counts is None else self._ints(counts, "counts", (n,)),
+                  None if path is None else self._ints(path, "path", (n, max_new)), max_new)
 
     def compact(self):
         """Moves the pages in use to the lowest numbers (qwen3_cache_compact)."""
         self._run(lib().qwen3_cache_compact)
 
     def _tree(self, n_head, rows, max_new, layer, words):
-        """The call's description and workspace bytes, made once per shape."""
+        """The call's description, workspace bytes and the result's width, made once per shape."""
         key = n_head, rows, max_new, layer, words
         got = self._trees.get(key)
         if got is None:
@@ -169,7 +177,7 @@ class PagedCache:
             _check(lib().qwen3_tree_size(self._ref, ctypes.byref(t), ctypes.byref(n)))
             if len(self._trees) >= 256:
                 self._trees.clear()
-            got = self._trees[key] = ctypes.byref(t), n.value
+            got = self._trees[key] = ctypes.byref(t), n.value, n_head * self._c.head_dim
         return got
 
     def attention(self, qkv, starts, max_new, mask=None, layer=0, out=None, lse=None):
@@ -179,24 +187,24 @@ class PagedCache:
         a mask in order, with mask int32 [rows, words] (tree_mask) as its bits
         say. Sequence s's rows are starts[s]..starts[s + 1] - 1, max_new at
         most."""
-        torch, c = self.torch, self._c
-        n_head, rows = self._rows(qkv, None)
-        self._ints(starts, "starts", (c.n_seq + 1,))
-        words = 0
+        torch = self.torch
+        n_head, rows, at = self._rows(qkv, 0)
+        first = self._ints(starts, "starts", (self._n_seq + 1,))
+        words = bits = 0
         if mask is not None:
             if mask.dim() != 2:
                 raise ValueError("a mask is [rows, words]")
             words = i32(mask.shape[1])
-            self._ints(mask, "mask", (rows, words))
-        tree, nbytes = self._tree(n_head, rows, i32(max_new), i32(layer), words)
-        shapes = (rows, n_head * c.head_dim), (n_head, rows)
-        out = (qkv.new_empty(shapes[0]) if out is None
-               else _device_rows(out, "out", torch.bfloat16, self.pages, shapes[0]))
-        lse = (qkv.new_empty(shapes[1], dtype=torch.float32) if lse is None
-               else _device_rows(lse, "lse", torch.float32, self.pages, shapes[1]))
+            bits = self._ints(mask, "mask", (rows, words))
+        tree, nbytes, width = self._tree(n_head, rows, i32(max_new), i32(layer), words)
+        if out is None:
+            out = torch.empty(rows, width, dtype=torch.bfloat16, device=qkv.device)
+        if lse is None:
+            lse = torch.empty(n_head, rows, dtype=torch.float32, device=qkv.device)
         work = torch.empty(nbytes, dtype=torch.uint8, device=qkv.device)
-        _check(on_stream(self.pages.device, lib().qwen3_tree_attention, self._ref, tree, qkv.data_ptr(),
-                         starts.data_ptr(), _ptr(mask), out.data_ptr(), lse.data_ptr(), work.data_ptr(), nbytes))
+        _check(on_stream(qkv.device, lib().qwen3_tree_attention, self._ref, tree, at, first, bits or None,
+                         self._given(out, "out", (rows, width), torch.bfloat16),
+                         self._given(lse, "lse", (n_head, rows), torch.float32), work.data_ptr(), nbytes))
         return out, lse
 
 
