@@ -106,6 +106,44 @@ gpt2_status qwen3_tree_attention(const qwen3_cache* c, const qwen3_tree* t,
                                  float* d_lse, void* d_workspace,
                                  size_t workspace_bytes, void* hip_stream);
 
+/* The rows' positions, int32 [n_rows]: a sequence's tokens in the cache, plus the
+ * new tokens that the row sees besides itself (in order: those before it; with
+ * a mask: its set bits less one); 0 for rows of no sequence. For
+ * qwen3_rotary_forward, before the rows go into the attention. */
+gpt2_status qwen3_tree_positions(const qwen3_cache* c, const qwen3_tree* t,
+                                 const int32_t* d_starts,
+                                 const int32_t* d_mask, int32_t* d_positions,
+                                 void* hip_stream);
+
+/* The cache in the model's forward, from the next qwen3_forward on: its B*T
+ * tokens are the rows of qwen3_tree_attention (c's sequences; n_layer, n_kv_head
+ * and head_dim the model's), rows of no sequence are padding whose results mean
+ * nothing. Attention of layer l is over the cache's layer l. Positions are those
+ * of qwen3_tree_positions, worked out by every forward, unless
+ * qwen3_set_positions gives others. The forward takes no targets and no
+ * backward follows it; with a config whose loss_from is 0,
+ * qwen3_logits_info has the logits of every row. d_starts and d_mask (or NULL) are read by every forward,
+ * the caller's to keep, like the cache's buffers; c itself is copied.
+ * d_workspace: qwen3_set_cache_size bytes, 256-byte aligned, the caller's to
+ * keep while the cache is in use, by graphs too. c NULL goes back to the
+ * forward without a cache. INVALID_ARG for what is not as said here, and while a
+ * layout is set (qwen3_set_layout). */
+gpt2_status qwen3_set_cache_size(const qwen3_model* m, const qwen3_cache* c,
+                                 int32_t max_new, size_t* bytes_out);
+gpt2_status qwen3_set_cache(qwen3_model* m, const qwen3_cache* c,
+                            const int32_t* d_starts, const int32_t* d_mask,
+                            int32_t mask_words, int32_t max_new,
+                            void* d_workspace, size_t workspace_bytes);
+/* qwen3_cache_append of the last forward's rows to the cache that it read, on
+ * the model's stream. STATE without such a forward. */
+gpt2_status qwen3_keep_tokens(qwen3_model* m, const int32_t* d_counts,
+                              const int32_t* d_path, int32_t max_new);
+/* Where the last forward's logits are: bf16 [rows][vocab] at *offset_bytes of
+ * the activations, the positions with loss in order. STATE unless the last
+ * forward had no targets (with targets their gradients are there). */
+gpt2_status qwen3_logits_info(const qwen3_model* m, size_t* offset_bytes,
+                              int32_t* rows);
+
 /* Logits as the choice of a token wants them. For every row r with history row
  * h = d_row_seq[r] (NULL: r), x its logits and, of token v,
  *   seen:  v is among the first d_lens[h] tokens of d_history[h], or in d_path[r];

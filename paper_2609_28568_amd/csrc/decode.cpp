@@ -2,8 +2,7 @@
 // of logits: checks of the arguments.
 #include <hip/hip_runtime.h>
 
-#include "../../include/qwen3_decode.h"
-#include "kernels.h"
+#include "decode.h"
 #include "prefix.h"
 
 namespace {
@@ -45,6 +44,23 @@ const char* cache_check(const qwen3_cache* c, bool sizes_only = false) {
   return nullptr;
 }
 
+const char* heads_check(const qwen3_cache& c, int32_t n_head, int32_t n_rows) {
+  if (n_head < 1 || n_head > 4096 || n_head % c.n_kv_head) return "n_head must be a multiple of n_kv_head, 4096 at most";
+  if (n_rows < 0 || n_rows >= 1 << 28) return "n_rows out of range";
+  return nullptr;
+}
+
+// Whether a call that changes the cache writes into a buffer: its books, and its pages if `pages`.
+bool writes(const qwen3_cache& c, const void* p, size_t bytes, bool pages) {
+  const size_t n = 4ul * c.n_seq;
+  return overlap(p, bytes, c.d_table, n * c.max_pages) || overlap(p, bytes, c.d_lens, n) ||
+         overlap(p, bytes, c.d_refs, 4ul * c.n_pages) || overlap(p, bytes, c.d_short, 4) ||
+         overlap(p, bytes, c.d_scratch, sizeof(int32_t) * cache_scratch_ints(c.n_seq, c.n_pages)) ||
+         (pages && overlap(p, bytes, c.d_pages, pages_bytes(c)));
+}
+
+}  // namespace
+
 CacheArgs cache_args(const qwen3_cache& c) {
   CacheArgs a{};
   a.L = c.n_layer; a.Hkv = c.n_kv_head; a.hd = c.head_dim; a.ps = c.page_size;
@@ -55,10 +71,9 @@ CacheArgs cache_args(const qwen3_cache& c) {
   return a;
 }
 
-const char* heads_check(const qwen3_cache& c, int32_t n_head, int32_t n_rows) {
-  if (n_head < 1 || n_head > 4096 || n_head % c.n_kv_head) return "n_head must be a multiple of n_kv_head, 4096 at most";
-  if (n_rows < 0 || n_rows >= 1 << 28) return "n_rows out of range";
-  return nullptr;
+const bf16_t* cache_layer(const qwen3_cache& c, int layer) {
+  return static_cast<const bf16_t*>(c.d_pages) +
+         (size_t)layer * c.n_pages * 2 * c.n_kv_head * c.page_size * c.head_dim;
 }
 
 const char* tree_check(const qwen3_cache* c, const qwen3_tree* t, bool sizes_only, TreeArgs* a) {
@@ -73,10 +88,31 @@ const char* tree_check(const qwen3_cache* c, const qwen3_tree* t, bool sizes_onl
   a->n_rows = t->n_rows; a->max_new = t->max_new < t->n_rows ? t->max_new : t->n_rows;
   if (a->max_new < 1) a->max_new = 1;
   a->mask_words = t->mask_words;
+  if (!sizes_only) {
+    a->pages = cache_layer(*c, t->layer);
+    a->table = c->d_table; a->lens = c->d_lens; a->refs = c->d_refs;
+  }
   return nullptr;
 }
 
-}  // namespace
+const char* append_check(const qwen3_cache* c, const AppendArgs& a) {
+  if (const char* why = cache_check(c)) return why;
+  if (const char* why = heads_check(*c, a.H, a.n_rows)) return why;
+  if (a.max_new < 1 || (long)a.max_new * c->n_seq >= 1l << 25) return "max_new out of range";
+  if (!a.starts || (!a.qkv && a.n_rows > 0)) return "null argument";
+  if (a.path && !a.counts) return "a path needs counts";
+  if (!aligned(a.qkv, 16) || !aligned(a.starts, 4) || !aligned(a.counts, 4) || !aligned(a.path, 4))
+    return "a pointer is not aligned";
+  if (a.layer_stride % 8 || a.layer_stride > 1ul << 40) return "layer_stride must be a multiple of 8, 2^40 at most";
+  const size_t row = (size_t)(a.H + 2 * c->n_kv_head) * c->head_dim;
+  const size_t all = a.n_rows ? ((c->n_layer - 1) * a.layer_stride + a.n_rows * row) * sizeof(bf16_t) : 0;
+  const size_t n = 4ul * c->n_seq;
+  const struct { const void* p; size_t bytes; } in[] = {
+      {a.qkv, all}, {a.starts, n + 4}, {a.counts, n}, {a.path, n * a.max_new}};
+  for (const auto& i : in)
+    if (i.p && writes(*c, i.p, i.bytes, true)) return "an input overlaps what the call writes";
+  return nullptr;
+}
 
 extern "C" {
 
@@ -91,34 +127,16 @@ gpt2_status qwen3_cache_fork(const qwen3_cache* c, const int32_t* d_src, const i
   if (const char* why = cache_check(c)) return refuse(why);
   if (!d_src) return refuse("d_src is NULL");
   if (!aligned(d_src, 4) || !aligned(d_keep, 4)) return refuse("a pointer is not aligned");
-  const size_t n = 4ul * c->n_seq, table = n * c->max_pages, refs = 4ul * c->n_pages;
   for (const int32_t* p : {d_src, d_keep})
-    if (p && (overlap(p, n, c->d_table, table) || overlap(p, n, c->d_lens, n) || overlap(p, n, c->d_refs, refs)))
-      return refuse("d_src or d_keep overlaps what the call writes");
+    if (p && writes(*c, p, 4ul * c->n_seq, false)) return refuse("d_src or d_keep overlaps what the call writes");
   return done(launch_cache_fork(cache_args(*c), d_src, d_keep, static_cast<hipStream_t>(hip_stream)));
 }
 
 gpt2_status qwen3_cache_append(const qwen3_cache* c, const void* d_qkv, int32_t n_head, int32_t n_rows,
                                size_t layer_stride, const int32_t* d_starts, const int32_t* d_counts,
                                const int32_t* d_path, int32_t max_new, void* hip_stream) {
-  if (const char* why = cache_check(c)) return refuse(why);
-  if (const char* why = heads_check(*c, n_head, n_rows)) return refuse(why);
-  if (max_new < 1 || (long)max_new * c->n_seq >= 1l << 25) return refuse("max_new out of range");
-  if (!d_starts || (!d_qkv && n_rows > 0)) return refuse("null argument");
-  if (d_path && !d_counts) return refuse("a path needs counts");
-  if (!aligned(d_qkv, 16) || !aligned(d_starts, 4) || !aligned(d_counts, 4) || !aligned(d_path, 4))
-    return refuse("a pointer is not aligned");
-  if (layer_stride % 8 || layer_stride > 1ul << 40) return refuse("layer_stride must be a multiple of 8, 2^40 at most");
-  const size_t row = (size_t)(n_head + 2 * c->n_kv_head) * c->head_dim;
-  const size_t all = n_rows ? ((c->n_layer - 1) * layer_stride + n_rows * row) * sizeof(bf16_t) : 0;
-  if (overlap(d_qkv, all, c->d_pages, pages_bytes(*c))) return refuse("the rows overlap the pages");
-  const size_t n = 4ul * c->n_seq, refs = 4ul * c->n_pages;
-  const struct { const int32_t* p; size_t bytes; } in[] = {{d_starts, n + 4}, {d_counts, n}, {d_path, n * max_new}};
-  for (const auto& i : in)
-    if (i.p && (overlap(i.p, i.bytes, c->d_table, n * c->max_pages) || overlap(i.p, i.bytes, c->d_lens, n) ||
-                overlap(i.p, i.bytes, c->d_refs, refs)))
-      return refuse("an input overlaps what the call writes");
-  AppendArgs a{static_cast<const bf16_t*>(d_qkv), n_head, n_rows, max_new, layer_stride, d_starts, d_counts, d_path};
+  const AppendArgs a{static_cast<const bf16_t*>(d_qkv), n_head, n_rows, max_new, layer_stride, d_starts, d_counts, d_path};
+  if (const char* why = append_check(c, a)) return refuse(why);
   return done(launch_cache_append(cache_args(*c), a, static_cast<hipStream_t>(hip_stream)));
 }
 
@@ -163,15 +181,31 @@ gpt2_status qwen3_tree_attention(const qwen3_cache* c, const qwen3_tree* t, cons
     if (i.p && (overlap(d_out, out, i.p, i.bytes) || (d_lse && overlap(d_lse, lse, i.p, i.bytes))))
       return refuse("out or lse overlaps another buffer");
   if (d_lse && overlap(d_out, out, d_lse, lse)) return refuse("out or lse overlaps another buffer");
-  a.pages = static_cast<const bf16_t*>(c->d_pages) +
-            (size_t)t->layer * c->n_pages * 2 * c->n_kv_head * c->page_size * c->head_dim;
-  a.table = c->d_table; a.lens = c->d_lens; a.refs = c->d_refs; a.starts = d_starts; a.mask = d_mask;
+  a.starts = d_starts;
+  a.mask = d_mask;
   a.qkv = static_cast<const bf16_t*>(d_qkv);
   a.out = static_cast<bf16_t*>(d_out);
   a.lse = d_lse;
   a.plan = static_cast<int32_t*>(d_workspace);
   a.part = reinterpret_cast<float*>(static_cast<char*>(d_workspace) + at);
   return done(launch_tree(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+gpt2_status qwen3_tree_positions(const qwen3_cache* c, const qwen3_tree* t, const int32_t* d_starts,
+                                 const int32_t* d_mask, int32_t* d_positions, void* hip_stream) {
+  TreeArgs a;
+  if (const char* why = tree_check(c, t, false, &a)) return refuse(why);
+  if (d_mask && (t->mask_words < 1 || t->mask_words > 1 << 20)) return refuse("mask_words out of range");
+  if (t->n_rows == 0) return GPT2_OK;
+  if (!d_starts || !d_positions) return refuse("null argument");
+  if (!aligned(d_starts, 4) || !aligned(d_mask, 4) || !aligned(d_positions, 4)) return refuse("a pointer is not aligned");
+  const size_t out = 4ul * t->n_rows;
+  if (overlap(d_positions, out, d_starts, 4ul * c->n_seq + 4) || overlap(d_positions, out, c->d_lens, 4ul * c->n_seq) ||
+      (d_mask && overlap(d_positions, out, d_mask, out * t->mask_words)))
+    return refuse("the positions overlap an input");
+  a.starts = d_starts;
+  a.mask = d_mask;
+  return done(launch_tree_positions(a, d_positions, static_cast<hipStream_t>(hip_stream)));
 }
 
 gpt2_status qwen3_adjust_logits(const qwen3_logits* l, const void* d_logits, void* d_out, void* hip_stream) {

@@ -469,6 +469,8 @@ struct TreeArgs {
 };
 // workspace bytes: the plan, then the partial results, which begin at *part_at; 0: out of range
 size_t tree_workspace(const TreeArgs& a, size_t* part_at);
+// positions [n_rows] of the rows in their sequences (of lens, starts, mask only)
+hipError_t launch_tree_positions(const TreeArgs& a, int32_t* positions, hipStream_t s);
 hipError_t launch_tree(const TreeArgs& a, hipStream_t s);
 
 struct qwen3_logits;

@@ -21,6 +21,7 @@
 #include <vector>
 
 #include "../../include/qwen3_prompt.h"
+#include "decode.h"
 #include "kernels.h"
 #include "prefix.h"
 #include "probe.h"
@@ -291,6 +292,14 @@ const char* validate(const qwen3_config* c) {
 
 }  // namespace
 
+// A cache in the forward: its description, the attention's arguments (layer 0),
+// and where the rows' positions go.
+struct CacheUse {
+  qwen3_cache c;
+  TreeArgs args;
+  int32_t* positions;
+};
+
 struct qwen3_model {
   qwen3_config cfg;
   Dims d;
@@ -308,6 +317,9 @@ struct qwen3_model {
   RotaryArgs rotary{}, rotary_used{};
   // likewise the layout (null: B sequences of T tokens)
   std::shared_ptr<qwen3_prefix> layout, layout_used;
+  // likewise the cache (starts null: none)
+  CacheUse cache{}, cache_used{};
+  bool forwarded = false;   // a forward has run
   std::string err;
   ProbeSet<QWEN3_K_COUNT> probes;
 
@@ -543,8 +555,18 @@ PrefixArgs prefix_args(qwen3_model* m, const AttnArgs& aa) {
   return a;
 }
 
+TreeArgs tree_args(const qwen3_model* m, const AttnArgs& aa, int l) {
+  TreeArgs a = m->cache_used.args;
+  a.pages = cache_layer(m->cache_used.c, l);
+  a.qkv = aa.qkv;
+  a.out = aa.out;
+  a.lse = aa.lse;
+  return a;
+}
+
 double attn_fwd_flops(const qwen3_model* m) {
   const Dims& d = m->d;
+  if (m->cache_used.args.starts) return 0.0;   // the lengths are on the device
   if (m->layout_used) return 4.0 * d.H * d.hd * m->layout_used->pairs;
   // causal: q.k and p.v over the key positions j <= i only
   return 4.0 * d.B * d.H * d.hd * ((double)d.T * (d.T + 1) / 2.0);
@@ -807,8 +829,16 @@ gpt2_status qwen3_forward(qwen3_model* m, const int32_t* d_inputs, const int32_t
   const int BT = (int)d.BT, BTL = (int)d.BTL;
   const int FWD = QWEN3_K_GEMM_FWD, NORM = QWEN3_K_NORM, OTHER = QWEN3_K_OTHER;
   const double rowb = 2.0 * d.BT * d.C;   // bytes of one bf16 [BT, C] activation
+  const bool cached = m->cache.args.starts;
+  if (cached && d_targets) return fail(m, GPT2_ERR_INVALID_ARG, "a forward over a cache takes no targets");
   m->layout_used = m->layout;
   m->rotary_used = m->rotary;
+  m->cache_used = m->cache;
+  if (cached && !m->rotary.positions) {
+    const int32_t sections[] = {d.hd / 2};
+    if (gpt2_status st = positions_of(m, m->cache.positions, 1, sections, 0, &m->rotary_used)) return st;
+    TRY(m->run(OTHER, 0.0, 4.0 * d.BT, [&] { return launch_tree_positions(m->cache.args, m->cache.positions, m->stream); }));
+  }
   if (m->layout && !m->rotary.positions) {
     const int32_t sections[] = {d.hd / 2};
     if (gpt2_status st = positions_of(m, m->layout->positions, 1, sections, 0, &m->rotary_used)) return st;
@@ -842,6 +872,7 @@ gpt2_status qwen3_forward(qwen3_model* m, const int32_t* d_inputs, const int32_t
                                     d.H, d.Hkv, d.hd, m->cfg.rms_eps, m->stream);
     }));
     TRY(m->run(QWEN3_K_ATTN_FWD, attn_fwd_flops(m), 0.0, [&] {
+      if (m->cache_used.args.starts) return launch_tree(tree_args(m, aa, l), m->stream);
       return m->layout_used ? launch_prefix_fwd(prefix_args(m, aa), m->stream) : launch_attention_fwd(aa, m->stream);
     }));
     Slices sl;
@@ -886,6 +917,7 @@ gpt2_status qwen3_forward(qwen3_model* m, const int32_t* d_inputs, const int32_t
   bf16_t* logits = m->ab(m->act.logits);
   TRY(gemm(m, FWD, mnk2(BTL, d.V, d.C), BTL, d.V, d.C, xf, d.C, 0, m->base(B_EMBED), d.C, 0, EPI_BF16, logits, d.V));
   m->have_targets = d_targets != nullptr;
+  m->forwarded = true;
   if (d_targets) {
     const float inv_n = 1.0f / (float)d.BTL;   // mean over the positions with loss
     TRY(m->run(QWEN3_K_CROSS_ENTROPY, 0.0, 4.0 * d.BTL * d.V + 12.0 * d.BT, [&] {
@@ -1071,6 +1103,7 @@ gpt2_status qwen3_set_layout(qwen3_model* m, int32_t prefix_len, int32_t n_seq, 
     m->layout.reset();
     return GPT2_OK;
   }
+  if (m->cache.args.starts) return fail(m, GPT2_ERR_INVALID_ARG, "a cache is set");
   if (m->d.B != 1) return fail(m, GPT2_ERR_INVALID_ARG, "a layout takes a model of one row of tokens, B = 1");
   const qwen3_prefix_config c{m->d.H, m->d.Hkv, m->d.hd, prefix_len, n_seq, 1};
   const std::string why = prefix_check(&c, seq_lens);
@@ -1085,6 +1118,75 @@ gpt2_status qwen3_set_layout(qwen3_model* m, int32_t prefix_len, int32_t n_seq, 
   return GPT2_OK;
 } catch (const std::bad_alloc&) {
   return no_memory(m);
+}
+
+gpt2_status qwen3_set_cache_size(const qwen3_model* m, const qwen3_cache* c, int32_t max_new, size_t* bytes_out) {
+  if (!m) return fail(nullptr, GPT2_ERR_INVALID_ARG, "null model");
+  qwen3_model* mm = const_cast<qwen3_model*>(m);
+  if (!bytes_out) return fail(mm, GPT2_ERR_INVALID_ARG, "bytes_out is NULL");
+  const Dims& d = m->d;
+  const qwen3_tree t{d.H, (int32_t)d.BT, max_new, 0, 0};
+  TreeArgs a;
+  if (const char* why = tree_check(c, &t, true, &a)) return fail(mm, GPT2_ERR_INVALID_ARG, why);
+  if (c->n_layer != d.L || c->n_kv_head != d.Hkv || c->head_dim != d.hd)
+    return fail(mm, GPT2_ERR_INVALID_ARG, "the cache's layers, heads or head_dim are not the model's");
+  size_t at;
+  const size_t bytes = tree_workspace(a, &at);
+  if (!bytes) return fail(mm, GPT2_ERR_INVALID_ARG, "the sequences are too many or too long");
+  *bytes_out = align_up(bytes) + align_up((size_t)d.BT * sizeof(int32_t));
+  return GPT2_OK;
+}
+
+gpt2_status qwen3_set_cache(qwen3_model* m, const qwen3_cache* c, const int32_t* d_starts, const int32_t* d_mask,
+                            int32_t mask_words, int32_t max_new, void* d_workspace, size_t workspace_bytes) {
+  if (!m) return fail(nullptr, GPT2_ERR_INVALID_ARG, "null model");
+  if (!c) {
+    m->cache = CacheUse{};
+    return GPT2_OK;
+  }
+  size_t need = 0, at = 0;
+  if (gpt2_status st = qwen3_set_cache_size(m, c, max_new, &need)) return st;
+  if (m->layout) return fail(m, GPT2_ERR_INVALID_ARG, "a layout is set");
+  const qwen3_tree t{m->d.H, (int32_t)m->d.BT, max_new, 0, mask_words};
+  CacheUse use{};
+  if (const char* why = tree_check(c, &t, false, &use.args)) return fail(m, GPT2_ERR_INVALID_ARG, why);
+  if (!d_starts) return fail(m, GPT2_ERR_INVALID_ARG, "null starts");
+  if (d_mask && (mask_words < 1 || mask_words > 1 << 20)) return fail(m, GPT2_ERR_INVALID_ARG, "mask_words out of range");
+  if (reinterpret_cast<uintptr_t>(d_starts) % 4 || reinterpret_cast<uintptr_t>(d_mask) % 4)
+    return fail(m, GPT2_ERR_INVALID_ARG, "a pointer is not aligned");
+  if (!d_workspace || reinterpret_cast<uintptr_t>(d_workspace) % 256 || workspace_bytes < need)
+    return fail(m, GPT2_ERR_INVALID_ARG,
+                "the workspace is NULL, not 256-byte aligned, or smaller than qwen3_set_cache_size says");
+  use.c = *c;
+  use.args.starts = d_starts;
+  use.args.mask = d_mask;
+  const size_t tree = align_up(tree_workspace(use.args, &at));
+  use.args.plan = static_cast<int32_t*>(d_workspace);
+  use.args.part = reinterpret_cast<float*>(static_cast<char*>(d_workspace) + at);
+  use.positions = reinterpret_cast<int32_t*>(static_cast<char*>(d_workspace) + tree);
+  m->cache = use;
+  return GPT2_OK;
+}
+
+gpt2_status qwen3_keep_tokens(qwen3_model* m, const int32_t* d_counts, const int32_t* d_path, int32_t max_new) {
+  if (!m) return fail(nullptr, GPT2_ERR_INVALID_ARG, "null model");
+  if (!m->forwarded || !m->cache_used.args.starts) return fail(m, GPT2_ERR_STATE, "no forward over a cache");
+  const Dims& d = m->d;
+  const CacheUse& use = m->cache_used;
+  const AppendArgs a{m->ab(m->act.packed), d.H, (int)d.BT, max_new, m->act.s_packed / sizeof(bf16_t), use.args.starts,
+                     d_counts, d_path};
+  if (const char* why = append_check(&use.c, a)) return fail(m, GPT2_ERR_INVALID_ARG, why);
+  TRY(m->run(QWEN3_K_OTHER, 0.0, 0.0, [&] { return launch_cache_append(cache_args(use.c), a, m->stream); }));
+  return GPT2_OK;
+}
+
+gpt2_status qwen3_logits_info(const qwen3_model* m, size_t* offset_bytes, int32_t* rows) {
+  if (!m) return fail(nullptr, GPT2_ERR_INVALID_ARG, "null model");
+  if (!m->forwarded || m->have_targets)
+    return fail(const_cast<qwen3_model*>(m), GPT2_ERR_STATE, "no forward without targets");
+  if (offset_bytes) *offset_bytes = m->act.logits;
+  if (rows) *rows = (int32_t)m->d.BTL;
+  return GPT2_OK;
 }
 
 gpt2_status qwen3_muon_size(const qwen3_config* cfg, size_t* bytes_out) {

@@ -741,6 +741,32 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : 64 * WPR) void tree_join_kernel(Tr
   if (c == 0 && a.lse) a.lse[(size_t)h * a.n_rows + token] = (m + log2f(l)) * LN2;
 }
 
+// A row's place in its sequence: behind the cached tokens and the new ones that it
+// sees besides itself.
+__global__ __launch_bounds__(256) void tree_positions_kernel(TreeArgs a, int32_t* positions) {
+  const int row = blockIdx.x * 256 + threadIdx.x;
+  if (row >= a.n_rows) return;
+  int lo = 0, hi = a.n_seq;   // sequences that begin at or before the row
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (a.starts[mid] <= row) lo = mid + 1;
+    else hi = mid;
+  }
+  int position = 0;
+  if (lo > 0) {
+    const int start = clampi(a.starts[lo - 1], 0, a.n_rows), end = clampi(a.starts[lo], start, a.n_rows);
+    if (row >= start && row < end) {
+      int before = row - start;
+      if (a.mask) {
+        before = -1;
+        for (int k = 0; k < a.mask_words; ++k) before += __popc(a.mask[(size_t)row * a.mask_words + k]);
+      }
+      position = clampi(a.lens[lo - 1], 0, a.max_pages * a.ps) + max(before, 0);
+    }
+  }
+  positions[row] = position;
+}
+
 template <int V>
 using Int = std::integral_constant<int, V>;
 
@@ -769,6 +795,12 @@ size_t tree_workspace(const TreeArgs& a, size_t* part_at) {
     *part_at = (((size_t)a.n_seq + 4) * sizeof(int32_t) + 255) / 256 * 256;
     return *part_at + (segment > W::LEAST ? 2 * (size_t)W::MOST * part_floats(a, W::ROWS, W::HEAD) * sizeof(float) : 0);
   });
+}
+
+hipError_t launch_tree_positions(const TreeArgs& a, int32_t* positions, hipStream_t s) {
+  if (a.n_rows < 1) return hipSuccess;
+  hipLaunchKernelGGL(tree_positions_kernel, dim3((a.n_rows + 255) / 256), dim3(256), 0, s, a, positions);
+  return hipGetLastError();
 }
 
 hipError_t launch_tree(const TreeArgs& a, hipStream_t s) {

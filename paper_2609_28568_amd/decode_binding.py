@@ -56,6 +56,11 @@ def lib():
         "qwen3_cache_compact": [cache, P],
         "qwen3_tree_size": [cache, tree, ctypes.POINTER(SIZE)],
         "qwen3_tree_attention": [cache, tree, P, P, P, P, P, P, SIZE, P],
+        "qwen3_tree_positions": [cache, tree, P, P, P, P],
+        "qwen3_set_cache_size": [P, cache, I32, ctypes.POINTER(SIZE)],
+        "qwen3_set_cache": [P, cache, P, P, I32, I32, P, SIZE],
+        "qwen3_keep_tokens": [P, P, P, I32],
+        "qwen3_logits_info": [P, ctypes.POINTER(SIZE), ctypes.POINTER(I32)],
         "qwen3_adjust_logits": [P, P, P, P],
     }
     for name, args in protos.items():
@@ -206,6 +211,19 @@ class PagedCache:
                          self._given(out, "out", (rows, width), torch.bfloat16),
                          self._given(lse, "lse", (n_head, rows), torch.float32), work.data_ptr(), nbytes))
         return out, lse
+
+
+    def positions(self, starts, rows, mask=None, out=None):
+        """int32 [1, rows]: the rows' places in their sequences, for rotary
+        (qwen3_tree_positions)."""
+        torch = self.torch
+        words, bits = (0, None) if mask is None else (i32(mask.shape[1]), self._ints(mask, "mask", (rows, mask.shape[1])))
+        t = Tree(self._c.n_kv_head, i32(rows), 1, 0, words)
+        if out is None:
+            out = torch.empty(1, rows, dtype=torch.int32, device=self.pages.device)
+        _check(on_stream(self.pages.device, lib().qwen3_tree_positions, self._ref, ctypes.byref(t),
+                         self._ints(starts, "starts", (self._n_seq + 1,)), bits, self._ints(out, "out", (1, rows))))
+        return out
 
 
 def tree_mask(parents, device="cuda"):

@@ -348,6 +348,8 @@ class SharedPrefix:
 class Qwen3:
     """One model instance on a torch-owned set of device buffers."""
 
+    _cache = None   # (cache, starts, mask, workspace) of the next forward
+
     def __init__(self, cfg: Qwen3Config, device="cuda"):
         import torch
         self.torch = torch
@@ -429,7 +431,7 @@ class Qwen3:
         if status != GPT2_ERR_INVALID_ARG:
             # a backward takes its forward's positions and layout, whatever is set in between; those
             # of the forward before stay where this one is refused
-            self._in_use = (self._positions, self._plan)
+            self._in_use = (self._positions, self._plan, self._cache)
         _check(status, self.h)
 
     def backward(self):
@@ -472,6 +474,63 @@ class Qwen3:
         plan = stream_buffer(n.value, self.bufs["workspace"].device, self.stream)
         _check(lib().qwen3_set_layout(self.h, prefix_len, len(lens), c_lens, plan.data_ptr(), n.value), self.h)
         self._plan = plan
+
+    def set_cache(self, cache=None, starts=None, max_new=1, mask=None):
+        """A decode_binding.PagedCache in the forward (qwen3_set_cache), from
+        the next one on: its tokens are new ones of the cache's sequences,
+        sequence s's rows starts[s]..starts[s + 1] - 1, max_new at most, with a
+        mask (tree_mask) or in order; keep_tokens stores them. None: without a
+        cache again. What the current stream has enqueued is done before the
+        model reads the tensors; the cache's own calls are to run on the model's
+        stream, or to be waited for. As with set_layout, graphs captured with a
+        cache are replayed only until another is set."""
+        from . import decode_binding as db
+        if cache is None:
+            _check(db.lib().qwen3_set_cache(self.h, None, None, None, 0, 0, None, 0), self.h)
+            self._cache = None
+            return
+        n = ctypes.c_size_t()
+        rows, like = self.cfg.B * self.cfg.T, self.bufs["workspace"]
+        _device_rows(starts, "starts", self.torch.int32, like, (cache.lens.shape[0] + 1,))
+        words = 0
+        if mask is not None:
+            words = i32(mask.shape[1])
+            _device_rows(mask, "mask", self.torch.int32, like, (rows, words))
+        _check(db.lib().qwen3_set_cache_size(self.h, cache._ref, i32(max_new), ctypes.byref(n)), self.h)
+        work = stream_buffer(n.value, like.device, self.stream)
+        _check(db.lib().qwen3_set_cache(self.h, cache._ref, starts.data_ptr(), _ptr(mask), words, i32(max_new),
+                                        work.data_ptr(), n.value), self.h)
+        now = self.torch.cuda.current_stream(like.device)
+        if now != self.stream:
+            self.stream.wait_stream(now)
+        for t in (starts, mask, cache.pages, cache.table, cache.lens, cache.refs, cache.short, cache.scratch):
+            if t is not None:
+                t.record_stream(self.stream)
+        self._cache = (cache, starts, mask, work)
+
+    def keep_tokens(self, max_new, counts=None, path=None):
+        """PagedCache.append of the last forward's rows to the cache that it
+        read (qwen3_keep_tokens), on the model's stream."""
+        from . import decode_binding as db
+        used = self._in_use and self._in_use[2]
+        n_seq = used[0].lens.shape[0] if used else None
+        for t, name, shape in ((counts, "counts", (n_seq,)), (path, "path", (n_seq, i32(max_new)))):
+            if t is not None:
+                _device_rows(t, name, self.torch.int32, self.bufs["workspace"], None if n_seq is None else shape)
+                now = self.torch.cuda.current_stream(t.device)
+                if now != self.stream:
+                    self.stream.wait_stream(now)
+                t.record_stream(self.stream)
+        _check(db.lib().qwen3_keep_tokens(self.h, _ptr(counts), _ptr(path), i32(max_new)), self.h)
+
+    def logits(self):
+        """The last forward's logits (without targets), bf16 [positions with
+        loss, vocab], in the model's own memory (qwen3_logits_info)."""
+        from . import decode_binding as db
+        at, rows = ctypes.c_size_t(), ctypes.c_int32()
+        _check(db.lib().qwen3_logits_info(self.h, ctypes.byref(at), ctypes.byref(rows)), self.h)
+        n = rows.value * self.cfg.vocab * 2
+        return self.bufs["activations"][at.value:at.value + n].view(self.torch.bfloat16).view(rows.value, self.cfg.vocab)
 
     def muon_step(self, norm_out=None, momentum=0.95, nesterov=True, iterations=5, scale=0.2):
         """Clip and an orthogonalised update with momentum of every adapter

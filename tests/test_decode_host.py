@@ -221,3 +221,33 @@ def test_tree_masks():
     assert m[4:6, 0].tolist() == [1, 2]
     # a chain from token 1 on
     assert m[43].tolist() == [torch.tensor(-2, dtype=torch.int32).item(), 255]
+
+
+# ---- positions, and the cache in the model
+
+@pytest.mark.parametrize("starts,mask,words,out,reason", [
+    (0, None, 0, 1 << 24, "null"), (4096, None, 0, 0, "null"), (4098, None, 0, 1 << 24, "aligned"),
+    (4096, 2, 1, 1 << 24, "aligned"), (4096, None, 0, (1 << 24) + 1, "aligned"), (4096, 1 << 20, 0, 1 << 24, "mask_words"),
+    (4096, None, 0, 4100, "overlap"), (4096, 1 << 20, 2, (1 << 20) + 60, "overlap"),
+    (4096, None, 0, FAR + (2 << 40), "overlap")])
+def test_positions_refuse_arguments(starts, mask, words, out, reason):
+    t = db.Tree(4, 8, 8, 0, words)
+    assert db.lib().qwen3_tree_positions(ctypes.byref(cache()), ctypes.byref(t), starts, mask, out, None) == INVALID
+    assert reason in why()
+
+
+def test_calls_without_a_model():
+    L, n, r = db.lib(), ctypes.c_size_t(), ctypes.c_int32()
+    assert L.qwen3_set_cache_size(None, ctypes.byref(cache()), 1, ctypes.byref(n)) == INVALID
+    assert L.qwen3_set_cache(None, ctypes.byref(cache()), 4096, None, 0, 1, 4096, 1 << 30) == INVALID
+    assert L.qwen3_keep_tokens(None, None, None, 1) == INVALID
+    assert L.qwen3_logits_info(None, ctypes.byref(n), ctypes.byref(r)) == INVALID
+
+
+def test_what_a_call_writes_may_not_be_its_input():
+    """The scratch and the count of missing pages are written too."""
+    L = db.lib()
+    for at in (FAR + (4 << 40), FAR + (5 << 40) + 64):
+        assert L.qwen3_cache_fork(ctypes.byref(cache()), at, None, None) == INVALID and "overlap" in why()
+        assert L.qwen3_cache_append(ctypes.byref(cache()), 4096, 4, 8, 0, at, None, None, 8, None) == INVALID
+        assert "overlap" in why()
