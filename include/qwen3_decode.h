@@ -93,7 +93,7 @@ gpt2_status qwen3_cache_compact(const qwen3_cache* c, void* hip_stream);
  * qwen3_tree_size bytes, 256-byte aligned, scratch until the call's kernels have
  * run: calls that may run at the same time take one each. */
 typedef struct qwen3_tree {
-  int32_t n_head, n_rows;
+  int32_t n_head, n_rows;   /* n_head * n_rows below 2^26 */
   int32_t max_new;       /* no sequence has more new tokens */
   int32_t layer;         /* of the cache */
   int32_t mask_words;    /* not looked at without d_mask */

@@ -80,6 +80,7 @@ const char* tree_check(const qwen3_cache* c, const qwen3_tree* t, bool sizes_onl
   if (const char* why = cache_check(c, sizes_only)) return why;
   if (!t) return "null description";
   if (const char* why = heads_check(*c, t->n_head, t->n_rows)) return why;
+  if ((long)t->n_rows * t->n_head >= 1l << 26) return "n_rows * n_head must stay below 2^26";   // a launch's threads
   if (t->max_new < 1 || t->max_new >= 1 << 28) return "max_new out of range";
   if (t->layer < 0 || t->layer >= c->n_layer) return "layer out of range";
   *a = TreeArgs{};

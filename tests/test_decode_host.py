@@ -109,7 +109,7 @@ def test_sizes():
 
 @pytest.mark.parametrize("over,reason", [
     (dict(n_head=0), "n_head"), (dict(n_head=3), "n_head"), (dict(n_head=8192), "n_head"), (dict(n_rows=-1), "n_rows"),
-    (dict(n_rows=1 << 28), "n_rows"), (dict(max_new=0), "max_new"), (dict(max_new=-1), "max_new"),
+    (dict(n_rows=1 << 28), "n_rows"), (dict(n_rows=1 << 24), "2^26"), (dict(max_new=0), "max_new"), (dict(max_new=-1), "max_new"),
     (dict(layer=-1), "layer"), (dict(layer=2), "layer")])
 def test_tree_descriptions_are_refused(over, reason):
     d = dict(n_head=4, n_rows=8, max_new=8, layer=0, mask_words=0)
@@ -122,7 +122,7 @@ def test_tree_descriptions_are_refused(over, reason):
 
 
 def test_tiles_past_32_bits_are_refused():
-    t, n = db.Tree(4096, 1 << 20, 1 << 20, 0, 0), ctypes.c_size_t()
+    t, n = db.Tree(64, 1 << 19, 1 << 19, 0, 0), ctypes.c_size_t()
     c = cache(n_seq=4096, max_pages=1 << 20, n_kv_head=2)
     assert db.lib().qwen3_tree_size(ctypes.byref(c), ctypes.byref(t), ctypes.byref(n)) == INVALID
     assert "too many or too long" in why()

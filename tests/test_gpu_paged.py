@@ -299,3 +299,166 @@ def test_attention_against_the_definition(name):
     assert torch.equal(y[used], y2[used]) and torch.equal(lse[:, used], lse2[:, used])
     for t in (y2[:starts[0]], y2[starts[-1]:], lse2[:, :starts[0]], lse2[:, starts[-1]:]):
         assert bool((t == 7).all())
+
+
+def test_pages_that_the_table_does_not_name_are_not_seen():
+    """Entries out of range, in the middle and at the end: the tokens there are
+    left out, and the others' weights are those of a softmax without them."""
+    H, Hkv, hd, ps, lens, new, tree, max_new = CASES["single_tokens"]
+    c, x, starts, mask, sees = build("single_tokens")
+    for s, i, page in ((0, 1, -1), (4, 0, c.pages.shape[1]), (4, 3, 2 ** 31 - 1), (5, 2, -2 ** 31), (1, 0, -5)):
+        c.table[s, i] = page
+    y, lse = c.attention(x, ints(starts), max_new, layer=1)
+    torch.cuda.synchronize()
+    table, pages = c.table.cpu().numpy(), c.pages
+    for s, n in enumerate(lens):
+        there = np.array([0 <= table[s, t // ps] < pages.shape[1] for t in range(n)], bool)
+        good = np.where((table[s] >= 0) & (table[s] < pages.shape[1]), table[s], 0)
+        k = torch.from_numpy(good[:-(-n // ps)]).long()
+        kv = f64(pages[1][k.cuda()]).transpose(1, 2, 0, 3, 4).reshape(2, Hkv, -1, hd)[:, :, :n][:, :, there]
+        row = f64(x[starts[s]]).reshape(H + 2 * Hkv, hd)
+        for h in range(H):
+            j = h // (H // Hkv)
+            keys, values = np.vstack([kv[0, j], row[H + j]]), np.vstack([kv[1, j], row[H + Hkv + j]])
+            e = keys @ row[h] / np.sqrt(hd)
+            p = np.exp(e - e.max())
+            want, size = (p @ values) / p.sum(), (p @ np.abs(values)) / p.sum()
+            got = f64(y[starts[s]]).reshape(H, hd)[h]
+            assert np.all(np.abs(got - want) <= R * (np.abs(want) + size) + 2.0 ** -15 * size), (s, h)
+            assert abs(float(lse[h, starts[s]]) - (e.max() + np.log(p.sum()))) < 1e-4
+
+
+@pytest.mark.parametrize("name", ["drafts", "drafts_wide", "drafts_hd64", "drafts_hd64_wide", "drafts_past_64", "chain"])
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
+def test_what_a_token_does_not_see_does_not_reach_it(name, what):
+    """One drafted token of each sequence holds NaN or infinity everywhere: the
+    rows that do not see it stay what they were but for the rounding of their
+    probabilities, those that do are not finite."""
+    H, Hkv, hd, ps, lens, new, tree, max_new = CASES[name]
+    c, x, starts, mask, sees = build(name)
+    y, lse = c.attention(x, ints(starts), max_new, mask=mask)
+    bad = x.clone()
+    touched = torch.zeros(x.shape[0], dtype=torch.bool, device="cuda")
+    for s, k in enumerate(new):
+        at = (3 * s + 1) % k
+        bad[starts[s] + at] = what
+        touched[starts[s]:starts[s + 1]] = torch.from_numpy(sees[s][:, at]).cuda()
+    z, zl = c.attention(bad, ints(starts), max_new, mask=mask)
+    keep = ~touched
+    keep[:starts[0]] = False
+    keep[starts[-1]:] = False
+    assert int(keep.sum()) > 0 and int(touched.sum()) > 0
+    # a tile that holds it goes token by token, with probabilities that are not rounded: 2^-8 of them
+    size = (y[keep].float().abs() + x[:, -Hkv * hd:].float().abs().max() * 2.0 ** -8) * 2.0 ** -7
+    assert bool(((z[keep].float() - y[keep].float()).abs() <= size + 2.0 ** -6).all())
+    assert bool((zl[:, keep] - lse[:, keep]).abs().max() < 1e-5)
+    assert bool(torch.isnan(z[touched].float()).any(1).all())
+
+
+def test_rows_past_max_new_are_left():
+    c, x, starts, mask, sees = build("chain")
+    y, lse = c.attention(x, ints(starts), 129)
+    z, zl = torch.full_like(y, 7), torch.full_like(lse, 7)
+    c.attention(x, ints(starts), 70, out=z, lse=zl)
+    for s in range(3):
+        a, n = starts[s], min(70, starts[s + 1] - starts[s])
+        assert bool(((z[a:a + n].float() - y[a:a + n].float()).abs() < 2.0 ** -5).all())
+        assert bool((z[a + n:starts[s + 1]] == 7).all()) and bool((zl[:, a + n:starts[s + 1]] == 7).all())
+
+
+def test_rows_that_see_nothing():
+    """No cached tokens and masks without a bit: 0, and -infinity."""
+    c = db().PagedCache.empty(1, 4, 2, 16, 64, 3, 2)
+    x = torch.randn(6, 8 * 64, device="cuda").bfloat16()
+    mask = torch.zeros(6, 1, dtype=torch.int32, device="cuda")
+    mask[1] = 2
+    y, lse = c.attention(x, ints([0, 2, 2, 6]), 4, mask=mask)
+    keep = torch.tensor([0, 2, 3, 4, 5], device="cuda")
+    assert bool((y[keep] == 0).all()) and bool((lse[:, keep] == -float("inf")).all())
+    assert torch.equal(y[1].view(2, 2, 64), x[1, 6 * 64:].view(2, 1, 64).expand(2, 2, 64))   # one key: its value
+
+
+def test_two_calls_at_once_and_a_captured_one():
+    """On two streams over one cache, and captured with lengths that change
+    between the replays."""
+    c, x, starts, mask, sees = build("long_drafts")
+    st, n = ints(starts), CASES["long_drafts"][7]
+    want = c.attention(x, st, n, mask=mask)
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    for k in range(6):
+        with torch.cuda.stream(streams[k % 2]):
+            got.append(c.attention(x, st, n, mask=mask))
+    torch.cuda.synchronize()
+    used = slice(starts[0], starts[-1])
+    for y, lse in got:
+        assert torch.equal(y[used], want[0][used]) and torch.equal(lse[:, used], want[1][:, used])
+    out = tuple(torch.zeros_like(t) for t in want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.attention(x, st, n, mask=mask, out=out[0], lse=out[1])
+    full = c.lens.clone()
+    for cut in (0, 1, 700, 5000, 3):
+        c.lens.copy_((full - cut).clamp(min=0))
+        graph.replay()
+        y, lse = c.attention(x, st, n, mask=mask)
+        torch.cuda.synchronize()
+        assert torch.equal(y[used], out[0][used]) and torch.equal(lse[:, used], out[1][:, used]), cut
+
+
+def test_pages_past_4_gib():
+    """A sequence's pages at both ends of 9 GiB of them: appended, read, copied on
+    a fork, moved together; the same bits as in a small cache."""
+    layers, Hkv, hd, ps, n_pages = 2, 4, 128, 64, 36864
+    pages = torch.empty(layers, n_pages, 2, Hkv, ps, hd, dtype=torch.bfloat16, device="cuda")
+    assert pages[0].numel() * 2 > 1 << 32
+    refs = torch.ones(n_pages, dtype=torch.int32, device="cuda")
+    free = [0, 1, 20000, 36000, 36001, 36002, 36860, 36861, 36862, 36863]
+    refs[free] = 0   # the others belong to a sequence that is not looked at
+    one = lambda v: torch.full((1,), v, dtype=torch.int32, device="cuda")   # noqa: E731
+    big = db().PagedCache(pages, torch.full((3, n_pages), -1, dtype=torch.int32, device="cuda"), ints([0, 0, 0]), refs, one(0))
+    small = db().PagedCache.empty(layers, 12, Hkv, ps, hd, 3, 12)
+    x = torch.randn(layers, 300, (8 + 2 * Hkv) * hd, device="cuda").bfloat16()
+    q = torch.randn(3, (8 + 2 * Hkv) * hd, device="cuda").bfloat16()
+    for c in (big, small):
+        c.append(x, ints([0, 290, 290, 290]), 290)      # 5 pages
+        c.fork(ints([0, 0, -1]))
+        c.append(x, ints([290, 295, 300, 300]), 10)     # two copies of the last page
+        assert c.short.item() == 0
+    assert big.table[0, :5].tolist() == free[:4] + [free[5]] and big.table[1, 4].item() == free[6]
+    for layer in range(layers):
+        a, b = (c.attention(q, ints([0, 1, 2, 3]), 1, layer=layer) for c in (big, small))
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    # only the sequences that are looked at are left, and move to the front
+    held = torch.zeros_like(refs)
+    held.index_add_(0, big.table[:2, :5].flatten().long(), torch.ones(10, dtype=torch.int32, device="cuda"))
+    big.refs.copy_(held)
+    big.compact()
+    assert big.table[:2, :5].max().item() == 5 and int((big.refs > 0).sum()) == 6
+    for layer in range(layers):
+        a, b = (c.attention(q, ints([0, 1, 2, 3]), 1, layer=layer) for c in (big, small))
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_the_largest_number_of_sequences():
+    """4,096 sequences forked from one, a token each stored and read."""
+    n = 4096
+    c = db().PagedCache.empty(1, n + 4, 1, 16, 64, n, 2)
+    x = torch.randn(1, 21, 3 * 64, device="cuda").bfloat16()
+    c.append(x, ints([0] + [21] * n), 21)
+    c.fork(ints([0] * n))
+    assert c.refs[:2].tolist() == [n, n]
+    q = torch.randn(1, n, 3 * 64, device="cuda").bfloat16()
+    st = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    y, lse = c.attention(q[0], st, 1)
+    c.append(q, st, 1)
+    assert c.short.item() == 0 and c.lens.tolist() == [22] * n and c.refs[:2].tolist() == [n, 0]
+    assert sorted(c.table[:, 1].tolist()) == list(range(2, n + 2)) and c.table[5, 1].item() == 7
+    # a sequence's new token is seen from the cache as it was from its row
+    e = torch.zeros(n, 3 * 64, device="cuda").bfloat16()
+    e[:, :64] = q[0, :, :64]
+    mask = torch.zeros(n, 1, dtype=torch.int32, device="cuda")
+    z, zl = c.attention(e, st, 1, mask=mask)
+    # the same probabilities, rounded to bf16 in another tile, and the result rounded
+    assert bool(((z.float() - y.float()).abs() <= 2.0 ** -6 * (1 + y.float().abs())).all())
+    assert float((zl - lse).abs().max()) < 1e-5
