@@ -80,19 +80,19 @@ DEV Seq seq_of(const TreeArgs& a, int s) {
                      min(clampi(a.starts[s + 1], start, a.n_rows) - start, a.max_new));
 }
 
-// v plus v of the lane that CTRL names, in the rows of ROWS
+// v of the lane that CTRL names, in the rows of ROWS; 0 elsewhere
 template <int CTRL, int ROWS>
-DEV int add_dpp(int v) {
-  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, true);
+DEV int dpp(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, true);
 }
 // over the lanes up to each: shifts within rows of 16, then rows' last lanes to the rows behind
 DEV int wave_scan(int v) {
-  v = add_dpp<0x111, 0xf>(v);
-  v = add_dpp<0x112, 0xf>(v);
-  v = add_dpp<0x114, 0xf>(v);
-  v = add_dpp<0x118, 0xf>(v);
-  v = add_dpp<0x142, 0xa>(v);
-  return add_dpp<0x143, 0xc>(v);
+  v += dpp<0x111, 0xf>(v);
+  v += dpp<0x112, 0xf>(v);
+  v += dpp<0x114, 0xf>(v);
+  v += dpp<0x118, 0xf>(v);
+  v += dpp<0x142, 0xa>(v);
+  return v + dpp<0x143, 0xc>(v);
 }
 
 // How the work is divided.
@@ -105,9 +105,10 @@ DEV int wave_scan(int v) {
 //  solo   line, every wave a worker of its own
 enum Division { DEALT, LINE, SOLO };
 typedef int Cuts __attribute__((ext_vector_type(4)));   // division, share, slack
+// (about t / share: the hardware's reciprocal will do, as all take the same)
 template <class W>
 DEV int pieces_of(int t, int share) {
-  return t <= W::WHOLE ? 1 : (t + share - 1) / share;
+  return t <= W::WHOLE ? 1 : max(1, (int)((float)(t + share - 1) * __builtin_amdgcn_rcpf((float)share)));
 }
 // workers(share): the workers that segments dealt in pieces of `share` tiles take
 template <class W, class Fn>
@@ -128,10 +129,13 @@ DEV Cuts cuts_of(int total, int segments, int longest, Fn workers) {
 }
 
 DEV int wave_total(int v) { return __builtin_amdgcn_readlane(wave_scan(v), 63); }
-DEV int wave_max(int v) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) v = max(v, __shfl_xor(v, o));
-  return __builtin_amdgcn_readfirstlane(v);
+DEV int wave_max(int v) {   // of values that are not negative
+  v = max(v, dpp<0x111, 0xf>(v));
+  v = max(v, dpp<0x112, 0xf>(v));
+  v = max(v, dpp<0x114, 0xf>(v));
+  v = max(v, dpp<0x118, 0xf>(v));
+  v = max(v, dpp<0x142, 0xa>(v));
+  return __builtin_amdgcn_readlane(max(v, dpp<0x143, 0xc>(v)), 63);
 }
 
 // The plan, for the launches behind: bases of the sequences and their sum, then
@@ -263,7 +267,9 @@ struct Keys {
   int len, n, tc, lps;
   int win, ids;             // the lane's entry of the table, pages win..win+63
   int refs;                 // sequences that have the piece's first page; 0 where other rows walk it too
+  uint64_t named;           // of the window: entries that are pages
   uint64_t seen;            // of the last tile issued: keys that are there
+  uint32_t base;            // the lane's byte offset in 16 rows of a page, first load
 
   DEV void init(const TreeArgs& args, int s, const Seq& q, int j, int f0) {
     a = &args;
@@ -278,13 +284,20 @@ struct Keys {
     n = q.n;
     tc = q.tc;
     lps = 31 - __builtin_clz(args.ps);
-    win = f0 * W::KT >> lps;
-    ids = table[min(win + (int)(threadIdx.x & 63), args.max_pages - 1)];
+    base = RB == 1 ? offset(0, threadIdx.x & 63, HD * 2) : 0;
+    look(f0 * W::KT >> lps);
     const int page = __builtin_amdgcn_readfirstlane(ids);
     refs = RB == 1 && q.blocks == 1 && (unsigned)page < (unsigned)args.n_pages ? args.refs[page] : 0;
   }
 
+  DEV void look(int from) {
+    win = from;
+    ids = table[min(win + (int)(threadIdx.x & 63), a->max_pages - 1)];
+    named = __ballot((unsigned)ids < (unsigned)a->n_pages);
+  }
+
   // the lane's part of load i of 16 rows that are `stride` bytes apart
+  static constexpr uint32_t turn(int i) { return HD == 128 ? ((i & 1) << 1 | i >> 1) * 16 : i * 16; }   // load i's against load 0's
   static DEV uint32_t offset(int i, int lane, uint32_t stride) {
     const int u = i * 64 + lane, row = u / U, c = unit<HD>(row, u % U) - row * U;   // the XOR is its own inverse
     return (uint32_t)row * stride + (uint32_t)c * 16u;
@@ -292,21 +305,29 @@ struct Keys {
   // by the waves of a group, `wave` of RB
   DEV void issue(int f, lds_char_t* st, int wave, bool once) {
     constexpr int SIXTEENS = W::KT / 16;
-    int lane = threadIdx.x & 63;
-    asm volatile("" : "+v"(lane));   // offsets are made again for each tile: kept, they would leave too few registers
-    seen = 0;
     if (f < tc) {
       const int p0 = f * W::KT >> lps, p1 = (f * W::KT + W::KT - 1) >> lps;
-      if (p1 >= win + 64 || p0 < win) {
-        win = p0;
-        ids = table[min(p0 + lane, a->max_pages - 1)];
-      }
+      if (p1 >= win + 64 || p0 < win) look(p0);
       auto page_of = [&](int key) { return __builtin_amdgcn_readlane(ids, (key >> lps) - win); };
+      const uint64_t pages = (2ull << (p1 - p0)) - 1;
+      seen = W::KT == 64 ? ~0ull : (1ull << W::KT) - 1;
+      if ((f + 1) * W::KT > len || (named >> (p0 - win) & pages) != pages) {
+        seen = 0;
 #pragma unroll
-      for (int q = 0; q < SIXTEENS; ++q) {
-        const int key = f * W::KT + 16 * q;
-        const int there = (unsigned)page_of(key) < (unsigned)a->n_pages ? clampi(len - key, 0, 16) : 0;
-        seen |= (uint64_t)((1u << there) - 1u) << (16 * q);
+        for (int q = 0; q < SIXTEENS; ++q) {
+          const int key = f * W::KT + 16 * q;
+          const int there = named >> ((key >> lps) - win) & 1 ? clampi(len - key, 0, 16) : 0;
+          seen |= (uint64_t)((1u << there) - 1u) << (16 * q);
+        }
+      }
+      // the loads' offsets are made again for each tile: kept, they would leave too few registers
+      uint32_t at = base;
+      if constexpr (RB == 1) {
+        asm volatile("" : "+v"(at));
+      } else {
+        int lane = threadIdx.x & 63;
+        asm volatile("" : "+v"(lane));
+        at = offset(0, lane, HD * 2);
       }
 #pragma unroll 1
       for (int q = wave; q < SIXTEENS; q += RB) {
@@ -317,19 +338,21 @@ struct Keys {
         if (RB == 1 && once) {
 #pragma unroll
           for (int i = 0; i < PER; ++i) {
-            dma16_once(rk, offset(i, lane, HD * 2), lds_addr(st + (q * PER + i) * 1024));
-            dma16_once(rv, offset(i, lane, HD * 2), lds_addr(st + W::TB + (q * PER + i) * 1024));
+            dma16_once(rk, ((at ^ turn(i)) + i * 1024), lds_addr(st + (q * PER + i) * 1024));
+            dma16_once(rv, ((at ^ turn(i)) + i * 1024), lds_addr(st + W::TB + (q * PER + i) * 1024));
           }
           continue;
         }
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-          dma16(rk, offset(i, lane, HD * 2), lds_addr(st + (q * PER + i) * 1024));
-          dma16(rv, offset(i, lane, HD * 2), lds_addr(st + W::TB + (q * PER + i) * 1024));
+          dma16(rk, ((at ^ turn(i)) + i * 1024), lds_addr(st + (q * PER + i) * 1024));
+          dma16(rv, ((at ^ turn(i)) + i * 1024), lds_addr(st + W::TB + (q * PER + i) * 1024));
         }
       }
     } else {
       const int d0 = (f - tc) * W::KT;
+      int lane = threadIdx.x & 63;
+      asm volatile("" : "+v"(lane));   // likewise
       seen = n - d0 >= 64 ? ~0ull : (1ull << max(n - d0, 0)) - 1;
       if constexpr (W::KT < 64) seen &= (1ull << W::KT) - 1;
 #pragma unroll 1
