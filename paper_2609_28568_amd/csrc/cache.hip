@@ -96,10 +96,9 @@ DEV int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
 __global__ __launch_bounds__(256) void fork_kernel(CacheArgs c, const int32_t* src, const int32_t* keep, int cols) {
   extern __shared__ int32_t old[];
   const int col0 = blockIdx.x * cols, n = c.n_seq * cols;
-  const int32_t kept_pages = c.max_pages;
   for (int i = threadIdx.x; i < n; i += 256) {
     const int col = col0 + i % cols;
-    old[i] = col < kept_pages ? c.table[(size_t)(i / cols) * c.max_pages + col] : -1;
+    old[i] = col < c.max_pages ? c.table[(size_t)(i / cols) * c.max_pages + col] : -1;
   }
   __syncthreads();
   for (int i = threadIdx.x; i < n; i += 256) {
@@ -232,48 +231,35 @@ DEV size_t page_at(const CacheArgs& c, int layer, int page) {   // in elements
   return ((size_t)layer * c.n_pages + page) * (2 * (size_t)c.Hkv * c.ps * c.hd);
 }
 
-// Tokens into their places, a wave `tok` tokens of one sequence and layer, and
-// behind those blocks the shared pages' tokens, a wave one head of one page.
-__global__ __launch_bounds__(64) void append_move_kernel(CacheArgs c, AppendArgs a, int tok, int groups, unsigned nt) {
+// Tokens into their places, a wave one token of one layer, and behind those
+// blocks the shared pages' tokens, a wave one head of one page. Written past the
+// caches: 16 prompts of 1,024, 12 layers of 12 heads of 64, 242 us through them,
+// 229 past them; 8 tokens a wave 275 and 257; one token each of 64, 14 all ways.
+__global__ __launch_bounds__(64) void append_move_kernel(CacheArgs c, AppendArgs a, int most, unsigned nt) {
   const int4* rec = reinterpret_cast<const int4*>(c.scratch + CACHE_HEADER);
   const int lane = threadIdx.x;
   const int hu = c.hd / 8, units = 2 * c.Hkv * hu;   // 16-byte units of a head, of a token
   if (blockIdx.x < nt) {
-    const int layer = blockIdx.y;
-    const int s = blockIdx.x / groups, i0 = (blockIdx.x - s * groups) * tok;
+    const int layer = blockIdx.y, s = blockIdx.x / most, i = blockIdx.x - s * most;
     const int4 r = rec[s];
-    const int n = min(tok, r.y - i0);
-    if (n <= 0) return;
+    if (i >= r.y) return;
     const int b = clampi(a.starts[s], 0, a.n_rows), e = clampi(a.starts[s + 1], b, a.n_rows);
-    const size_t ld = (size_t)(a.H + 2 * c.Hkv) * c.hd;
-    const bf16_t* rows = a.qkv + layer * a.layer_stride + (size_t)a.H * c.hd;
+    const int row = a.path ? a.path[(size_t)s * a.max_new + i] : i;
+    const int pos = r.x + i, page = c.table[(size_t)s * c.max_pages + pos / c.ps];
+    if ((unsigned)row >= (unsigned)(e - b) || (unsigned)page >= (unsigned)c.n_pages) return;
+    const uint4* from = reinterpret_cast<const uint4*>(
+        a.qkv + layer * a.layer_stride + (size_t)(b + row) * (a.H + 2 * c.Hkv) * c.hd + (size_t)a.H * c.hd);
+    uint4* to = reinterpret_cast<uint4*>(c.pages + page_at(c, layer, page) + (size_t)(pos % c.ps) * c.hd);
     constexpr int FLIGHT = 4;
-    const int all = n * units;
-    for (int u0 = lane; u0 < all; u0 += 64 * FLIGHT) {
+    for (int u0 = lane; u0 < units; u0 += 64 * FLIGHT) {
       uint4 v[FLIGHT];
-      bf16_t* to[FLIGHT];
+#pragma unroll
+      for (int k = 0; k < FLIGHT; ++k) v[k] = u0 + 64 * k < units ? from[u0 + 64 * k] : make_uint4(0, 0, 0, 0);
 #pragma unroll
       for (int k = 0; k < FLIGHT; ++k) {
-        const int u = u0 + 64 * k;
-        to[k] = nullptr;
-        v[k] = make_uint4(0, 0, 0, 0);
-        if (u < all) {
-          const int i = u / units, w = u - i * units, h = w / hu;
-          const int row = a.path ? a.path[(size_t)s * a.max_new + i0 + i] : i0 + i;
-          const int pos = r.x + i0 + i, page = c.table[(size_t)s * c.max_pages + pos / c.ps];
-          if ((unsigned)row < (unsigned)(e - b) && (unsigned)page < (unsigned)c.n_pages) {
-            to[k] = c.pages + page_at(c, layer, page) + ((size_t)h * c.ps + pos % c.ps) * c.hd + (w - h * hu) * 8;
-            v[k] = *reinterpret_cast<const uint4*>(rows + (size_t)(b + row) * ld + w * 8);
-          }
-        }
+        const int u = u0 + 64 * k, h = u / hu;
+        if (u < units) st_stream(to + (size_t)h * c.ps * hu + (u - h * hu), v[k]);
       }
-#pragma unroll
-      for (int k = 0; k < FLIGHT; ++k)
-        if (to[k]) {
-          // (prompts of a batch, 600 MB: 143 us through the caches, 136 past them)
-          if (tok > 1) st_stream(reinterpret_cast<uint4*>(to[k]), v[k]);
-          else *reinterpret_cast<uint4*>(to[k]) = v[k];
-        }
     }
     return;
   }
@@ -391,10 +377,10 @@ hipError_t launch_cache_fork(const CacheArgs& c, const int32_t* src, const int32
 
 hipError_t launch_cache_append(const CacheArgs& c, const AppendArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(append_book_kernel, dim3(1), dim3(BOOK), 0, s, c, a);
-  const int tok = a.max_new >= 64 ? 8 : 1, groups = (a.max_new + tok - 1) / tok;
-  const unsigned nt = (unsigned)c.n_seq * groups;
+  const int most = a.path ? a.max_new : std::min(a.max_new, std::max(a.n_rows, 1));   // tokens of a sequence
+  const unsigned nt = (unsigned)c.n_seq * most;
   const unsigned nc = (unsigned)std::min((long)c.n_seq * 2 * c.Hkv, std::max(1l, 2048l / c.L));
-  hipLaunchKernelGGL(append_move_kernel, dim3(nt + nc, c.L), dim3(64), 0, s, c, a, tok, groups, nt);
+  hipLaunchKernelGGL(append_move_kernel, dim3(nt + nc, c.L), dim3(64), 0, s, c, a, most, nt);
   return hipGetLastError();
 }
 

@@ -43,14 +43,15 @@ struct Walk {
   // of a wave's O for the others, maxima and sums
   static constexpr int KEEP = (DT - (GROUPS * PER > DT ? 0 : PER)) * 4096 + 512;
   static constexpr int LEAST = 4;               // tiles of a share; segments of no more are never cut
-  static constexpr int WHOLE = 4 * GROUPS;      // ... nor dealt of these
+  static constexpr int SLACK = LEAST / 2;       // tiles from a segment's end within which a cut goes there
+  static constexpr int WHOLE = 2 * GROUPS > LEAST ? 2 * GROUPS : LEAST;   // ... nor dealt of these
   static constexpr int TEAMS = 256 * (RB == 1 ? 1 : 2);   // workgroups that run at a time
   static constexpr int MOST = RB == 1 ? 4 * TEAMS : TEAMS;   // shares
   static_assert(GROUPS == 1 || 4 * KEEP <= GROUPS * RING, "the groups' results fit their tiles' space");
 };
 // Rows of a partial result, and its floats: O [rows][hd], maxima, sums.
 __host__ DEV int part_rows(const TreeArgs& a, int rows) {
-  const long most = (long)a.max_new * (a.H / a.Hkv);
+  const long most = ((long)a.max_new * (a.H / a.Hkv) + 1) / 2 * 2;   // even: parts begin at multiples of 16 bytes
   return most < rows ? (int)most : rows;
 }
 __host__ DEV size_t part_floats(const TreeArgs& a, int rows, int hd) { return (size_t)part_rows(a, rows) * (hd + 2); }
@@ -98,13 +99,12 @@ DEV int wave_scan(int v) {
 // How the work is divided.
 //  dealt  a segment of t tiles goes to pieces_of(t, share) workers; a sequence's
 //         base is the number of workers before it
-//  line   worker w has tiles w share.. of the line of all segments, a cut nearer
-//         than `slack` to a segment's end going there (segments of LEAST tiles
-//         are never cut, and few tiles are left on one side of a cut); a
-//         sequence's base is the number of tiles before it
+//  line   worker w has tiles w share.. of the line of all segments, a cut within
+//         SLACK of a segment's end going there (so segments of LEAST tiles are
+//         never cut); a sequence's base is the number of tiles before it
 //  solo   line, every wave a worker of its own
 enum Division { DEALT, LINE, SOLO };
-typedef int Cuts __attribute__((ext_vector_type(4)));   // division, share, slack
+typedef int Cuts __attribute__((ext_vector_type(2)));   // division, share
 // (about t / share: the hardware's reciprocal will do, as all take the same)
 template <class W>
 DEV int pieces_of(int t, int share) {
@@ -115,17 +115,19 @@ template <class W, class Fn>
 DEV Cuts cuts_of(int total, int segments, int longest, Fn workers) {
   const int even = max(W::WHOLE / 2, (total + W::TEAMS - 1) / W::TEAMS);
   int deal = segments <= W::TEAMS && longest <= W::WHOLE ? even : 0;
-  // (up to three in eight more tiles than with equal shares cost less than workers with parts of two segments: 16
-  // trees of 24 drafts over 1,000 to 3,001 tokens)
+  // Pieces of up to three in eight more tiles than equal shares cost less than workers with parts of two segments. Of
+  // 16 sequences of 1,000 to 3,001 tokens with 24 drafts each: 42 us with no more, 40 with three in eight, 41 with
+  // eight; of three pieces of prompts 45, 40, 41; all in one line 41 and 44.
 #pragma unroll
   for (int k = 3; k >= 0; --k) {
     const int share = even + (even * k + 7) / 8;
     if (segments <= W::TEAMS && workers(share) <= W::TEAMS) deal = share;
   }
-  const bool solo = W::GROUPS == 4 && segments > W::TEAMS && total > 8 * W::TEAMS;
+  // (single tokens of 64 sequences of 200 to 4,096, 512 segments: 136 us with groups, 100 without; of 64 of 100 to 300:
+  // 38, 25)
+  const bool solo = W::GROUPS == 4 && segments > W::TEAMS;
   const int shares = solo ? W::MOST : W::TEAMS, share = max(W::LEAST, (total + shares - 1) / shares);
-  const int slack = max(W::LEAST / 2, share <= 2 * W::LEAST ? share / 2 : share / 8);
-  return Cuts{deal ? DEALT : solo ? SOLO : LINE, deal ? deal : share, slack, 0};
+  return Cuts{deal ? DEALT : solo ? SOLO : LINE, deal ? deal : share};
 }
 
 DEV int wave_total(int v) { return __builtin_amdgcn_readlane(wave_scan(v), 63); }
@@ -144,7 +146,6 @@ DEV void store_cuts(const TreeArgs& a, int sum, const Cuts& c) {
   a.plan[a.n_seq] = sum;
   a.plan[a.n_seq + 1] = c.x;
   a.plan[a.n_seq + 2] = c.y;
-  a.plan[a.n_seq + 3] = c.z;
 }
 
 template <class W>
@@ -192,7 +193,6 @@ struct Line {
       sum = __builtin_amdgcn_readfirstlane(a.plan[a.n_seq]);
       cuts.x = __builtin_amdgcn_readfirstlane(a.plan[a.n_seq + 1]);
       cuts.y = __builtin_amdgcn_readfirstlane(a.plan[a.n_seq + 2]);
-      cuts.z = __builtin_amdgcn_readfirstlane(a.plan[a.n_seq + 3]);
       return;
     }
     Seq q{};
@@ -239,7 +239,7 @@ struct Line {
     int before;
     const int s = find(a, p, &before);
     const int t = seq(a, s).t, from = before + (p - before) / t * t;
-    return p - from <= cuts.z ? from : from + t - p <= cuts.z ? from + t : p;
+    return p - from <= W::SLACK ? from : from + t - p <= W::SLACK ? from + t : p;
   }
 };
 
@@ -672,7 +672,7 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : 64 * WPR) void tree_join_kernel(Tr
   }
   if (s < 0) return;
   const int before = a.plan[s];
-  const Cuts cuts = {a.plan[a.n_seq + 1], a.plan[a.n_seq + 2], a.plan[a.n_seq + 3], 0};
+  const Cuts cuts = {a.plan[a.n_seq + 1], a.plan[a.n_seq + 2]};
   const Seq q = seq_of<W>(a, s);
   const int i = token - q.start;
   if (i < 0 || i >= q.n) return;
@@ -689,7 +689,7 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : 64 * WPR) void tree_join_kernel(Tr
   } else {
     const int from = before + (block * a.Hkv + j) * q.t;
     // cuts w0..w1 lie inside the segment, so shares w0 - 1..w1 have its parts
-    const int w0 = (from + cuts.z) / cuts.y + 1, w1 = (from + q.t - cuts.z - 1) / cuts.y;
+    const int w0 = (from + W::SLACK) / cuts.y + 1, w1 = (from + q.t - W::SLACK - 1) / cuts.y;
     if (w1 < w0) return;
     parts = w1 - w0 + 2;
     part0 = a.part + 2 * (size_t)(w0 - 1) * floats;
@@ -793,7 +793,9 @@ __global__ __launch_bounds__(256) void tree_positions_kernel(TreeArgs a, int32_t
 template <int V>
 using Int = std::integral_constant<int, V>;
 
-// f(head size, blocks of rows of a workgroup): as many as a sequence's rows fill
+// f(head size, blocks of rows of a workgroup): as many as a sequence's rows fill. 16 sequences of 1,000 to 3,000
+// tokens, heads of 128, with 1, 2, 4 blocks: 24 rows 38, 37, 42 us; 48 rows 52, 40, 44; 96 rows 77, 57, 49; heads of
+// 64: 24 rows 35, 32, 42; 48 rows 51, 36, 46; 100 rows 89, 57, 51.
 template <class Fn>
 auto with_walk(const TreeArgs& a, Fn f) {
   const long rows = (long)a.max_new * (a.H / a.Hkv);
@@ -815,7 +817,7 @@ size_t tree_workspace(const TreeArgs& a, size_t* part_at) {
     using W = Walk<decltype(hd)::value, decltype(rb)::value>;
     double segment;
     if (most_tiles<W>(a, &segment) > 2e9) return 0;   // tiles are counted in 32 bits
-    *part_at = (((size_t)a.n_seq + 4) * sizeof(int32_t) + 255) / 256 * 256;
+    *part_at = (((size_t)a.n_seq + 3) * sizeof(int32_t) + 255) / 256 * 256;
     return *part_at + (segment > W::LEAST ? 2 * (size_t)W::MOST * part_floats(a, W::ROWS, W::HEAD) * sizeof(float) : 0);
   });
 }
@@ -838,7 +840,8 @@ hipError_t launch_tree(const TreeArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((tree_kernel<HD, RB>), dim3(teams), dim3(256), 0, s, a);
     if (segment > W::LEAST) {
       const long rows = (long)a.n_rows * a.H;
-      // a few rows of many parts: 8 waves a row
+      // 8 waves a row where rows are few and their parts many: one token over 131,071 of one key/value head with 8 query
+      // heads 48 us with one wave, 27 with 8, of 8 heads with 16 94 and 92; 16 trees of 24 drafts 40 and 68
       if (rows <= 512) hipLaunchKernelGGL((tree_join_kernel<HD, RB, 8>), dim3((unsigned)rows), dim3(512), 0, s, a);
       else hipLaunchKernelGGL((tree_join_kernel<HD, RB, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
     }
