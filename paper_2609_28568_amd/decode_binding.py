@@ -197,9 +197,7 @@ class PagedCache:
         first = self._ints(starts, "starts", (self._n_seq + 1,))
         words = bits = 0
         if mask is not None:
-            if mask.dim() != 2:
-                raise ValueError("a mask is [rows, words]")
-            words = i32(mask.shape[1])
+            words = mask_words(mask)
             bits = self._ints(mask, "mask", (rows, words))
         tree, nbytes, width = self._tree(n_head, rows, i32(max_new), i32(layer), words)
         if out is None:
@@ -212,18 +210,27 @@ class PagedCache:
                          self._given(lse, "lse", (n_head, rows), torch.float32), work.data_ptr(), nbytes))
         return out, lse
 
-
     def positions(self, starts, rows, mask=None, out=None):
         """int32 [1, rows]: the rows' places in their sequences, for rotary
         (qwen3_tree_positions)."""
         torch = self.torch
-        words, bits = (0, None) if mask is None else (i32(mask.shape[1]), self._ints(mask, "mask", (rows, mask.shape[1])))
+        words, bits = 0, None
+        if mask is not None:
+            words = mask_words(mask)
+            bits = self._ints(mask, "mask", (rows, words))
         t = Tree(self._c.n_kv_head, i32(rows), 1, 0, words)
         if out is None:
             out = torch.empty(1, rows, dtype=torch.int32, device=self.pages.device)
         _check(on_stream(self.pages.device, lib().qwen3_tree_positions, self._ref, ctypes.byref(t),
                          self._ints(starts, "starts", (self._n_seq + 1,)), bits, self._ints(out, "out", (1, rows))))
         return out
+
+
+def mask_words(mask):
+    """Words of a mask's rows; 1 at least, as an empty tensor has no address."""
+    if mask.dim() != 2 or mask.shape[1] < 1:
+        raise ValueError("a mask is [rows, words], a word or more")
+    return i32(mask.shape[1])
 
 
 def tree_mask(parents, device="cuda"):

@@ -494,7 +494,7 @@ class Qwen3:
         _device_rows(starts, "starts", self.torch.int32, like, (cache.lens.shape[0] + 1,))
         words = 0
         if mask is not None:
-            words = i32(mask.shape[1])
+            words = db.mask_words(mask)
             _device_rows(mask, "mask", self.torch.int32, like, (rows, words))
         _check(db.lib().qwen3_set_cache_size(self.h, cache._ref, i32(max_new), ctypes.byref(n)), self.h)
         work = stream_buffer(n.value, like.device, self.stream)

@@ -251,3 +251,12 @@ def test_what_a_call_writes_may_not_be_its_input():
         assert L.qwen3_cache_fork(ctypes.byref(cache()), at, None, None) == INVALID and "overlap" in why()
         assert L.qwen3_cache_append(ctypes.byref(cache()), 4096, 4, 8, 0, at, None, None, 8, None) == INVALID
         assert "overlap" in why()
+
+
+@pytest.mark.parametrize("shape", [(3, 0), (0, 0), (3,), (3, 1, 1)])
+def test_masks_without_words_are_refused(shape):
+    """An empty tensor's address is null, which would mean no mask."""
+    torch = pytest.importorskip("torch")
+    with pytest.raises(ValueError, match="word"):
+        db.mask_words(torch.zeros(*shape, dtype=torch.int32))
+    assert db.mask_words(torch.zeros(0, 2, dtype=torch.int32)) == 2

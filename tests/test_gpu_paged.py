@@ -462,3 +462,40 @@ def test_the_largest_number_of_sequences():
     # the same probabilities, rounded to bf16 in another tile, and the result rounded
     assert bool(((z.float() - y.float()).abs() <= 2.0 ** -6 * (1 + y.float().abs())).all())
     assert float((zl - lse).abs().max()) < 1e-5
+
+
+def test_masks_without_words_are_refused():
+    c = db().PagedCache.empty(1, 4, 1, 16, 64, 2, 4)
+    x, starts = torch.zeros(4, 4 * 64, dtype=torch.bfloat16, device="cuda"), ints([0, 2, 4])
+    for call in (lambda mask: c.attention(x, starts, 2, mask), lambda mask: c.positions(starts, 4, mask)):
+        for mask in (torch.zeros(4, 0, dtype=torch.int32, device="cuda"), ints([0] * 4)):
+            with pytest.raises(ValueError, match="word"):
+                call(mask)
+
+
+@pytest.mark.parametrize("H,Hkv,hd,new,lens", [
+    (8, 8, 128, 1, [37 * s % 391 for s in range(40)]),      # 320 segments: every wave a worker, shares cut
+    (8, 4, 64, 40, [61 * s % 1500 for s in range(70)]),     # planned, two blocks of rows to a workgroup
+    (4, 4, 64, 5, [300, 0, 1, 17, 333, 64])])               # segments that are dealt and some that are whole
+def test_divisions_of_ragged_lengths(H, Hkv, hd, new, lens):
+    """Shares that end anywhere in a segment, segments of nothing, one part and several."""
+    torch.manual_seed(9)
+    n = len(lens)
+    held = [-(-x // 16) for x in lens]
+    pages = torch.randn(1, sum(held) + 1, 2, Hkv, 16, hd, device="cuda").bfloat16()
+    table = torch.full((n, max(held)), -1, dtype=torch.int32)
+    order, at = torch.randperm(sum(held)).int(), 0
+    for s, h in enumerate(held):
+        table[s, :h] = order[at:at + h]
+        at += h
+    refs = torch.ones(sum(held) + 1, dtype=torch.int32)
+    refs[-1] = 0
+    c = db().PagedCache(pages, table.cuda(), ints(lens), refs.cuda(), ints([0]))
+    news = [(7 * s) % (new + 1) for s in range(n)] if new > 1 else [1] * n
+    starts = [sum(news[:s]) for s in range(n + 1)]
+    x = torch.randn(starts[-1], (H + 2 * Hkv) * hd, device="cuda").bfloat16()
+    y, lse = c.attention(x, ints(starts), max(news))
+    again, _ = c.attention(x, ints(starts), max(news))
+    assert torch.equal(y, again)
+    sees = [np.tri(k, dtype=bool) for k in news]
+    check(y, lse, starts, reference(c, x, starts, lens, sees, H, Hkv, hd, 0))
