@@ -121,9 +121,9 @@ gpt2_status qwen3_tree_positions(const qwen3_cache* c, const qwen3_tree* t,
  * nothing. Attention of layer l is over the cache's layer l. Positions are those
  * of qwen3_tree_positions, worked out by every forward, unless
  * qwen3_set_positions gives others. The forward takes no targets and no
- * backward follows it; with a config whose loss_from is 0,
- * qwen3_logits_info has the logits of every row. d_starts and d_mask (or NULL) are read by every forward,
- * the caller's to keep, like the cache's buffers; c itself is copied.
+ * backward follows it; with a config whose loss_from is 0, qwen3_logits_info has
+ * the logits of every row. d_starts and d_mask (or NULL) are read by every
+ * forward, the caller's to keep, like the cache's buffers; c itself is copied.
  * d_workspace: qwen3_set_cache_size bytes, 256-byte aligned, the caller's to
  * keep while the cache is in use, by graphs too. c NULL goes back to the
  * forward without a cache. INVALID_ARG for what is not as said here, and while a
@@ -157,8 +157,8 @@ gpt2_status qwen3_logits_info(const qwen3_model* m, size_t* offset_bytes,
  * [0, n_seq) is a row without a history; a d_row_mask outside [0, n_masks) a row
  * without a mask. d_logits and d_out: bf16 (dtype 1) or fp32 (dtype 0) [rows],
  * rows logits_stride and out_stride elements apart (vocab at least); d_out may
- * be d_logits, with the same stride, and overlaps it in no other way. Columns from vocab on are
- * neither read nor written. */
+ * be d_logits, with the same stride, and overlaps it in no other way. Columns
+ * from vocab on are neither read nor written. */
 typedef struct qwen3_logits {
   int32_t rows, vocab, dtype;
   int64_t logits_stride, out_stride;
