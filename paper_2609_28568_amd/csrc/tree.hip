@@ -116,13 +116,14 @@ template <class W, class Fn>
 DEV Cuts cuts_of(int total, int segments, int longest, Fn workers) {
   const int even = max(W::WHOLE / 2, (total + W::TEAMS - 1) / W::TEAMS);
   int deal = segments <= W::TEAMS && longest <= W::WHOLE ? even : 0;
-  // Pieces of up to three in eight more tiles than equal shares cost less than workers with parts of two segments. Of
-  // 16 sequences of 1,000 to 3,001 tokens with 24 drafts each: 42 us with no more, 40 with three in eight, 41 with
-  // eight; of three pieces of prompts 45, 40, 41; all in one line 41 and 44.
+  // Pieces of up to 14/32 more tiles than equal shares, the fewest that do, cost less than workers with parts of two
+  // segments. Of 16 sequences of 1,000 to 3,001 tokens with 24 drafts each: 42 us with no more, 40 with three in eight,
+  // 41 with eight; of three pieces of prompts 45, 40, 41; all in one line 41 and 44.
+  if (segments <= W::TEAMS) {
+    int k = 15;
 #pragma unroll
-  for (int k = 3; k >= 0; --k) {
-    const int share = even + (even * k + 7) / 8;
-    if (segments <= W::TEAMS && workers(share) <= W::TEAMS) deal = share;
+    for (int step = 8; step; step >>= 1) k -= workers(even + (even * (k - step) + 31) / 32) <= W::TEAMS ? step : 0;
+    if (k < 15) deal = even + (even * k + 31) / 32;
   }
   // (single tokens of 64 sequences of 200 to 4,096, 512 segments: 136 us with groups, 100 without; of 64 of 100 to 300:
   // 38, 25)
