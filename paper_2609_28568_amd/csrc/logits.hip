@@ -4,11 +4,12 @@
 // A workgroup takes a piece of one row. It counts the row's history within the
 // piece in LDS (whole numbers, so their order does not matter), then passes over
 // the logits once, whose loads are under way behind the history's. HBM-bound with
-// many rows (64 rows of 151,936 bf16 after 2,048 tokens 14.5 us, 39 MB: 2.7 TB/s,
+// many rows (64 rows of 151,936 bf16 after 2,048 tokens 13.1 us, 39 MB: 3.0 TB/s,
 // most of it the chain of history, counts and logits that every workgroup runs once);
 // every piece of a row reads the history again, from L2, so pieces are long where
-// histories are (96 rows of 50,257 fp32 after 30,000 21 us). One row takes 3.6 us, a
-// launch and two dependent loads.
+// histories are (96 rows of 50,257 fp32 after up to 30,000 16.2 us, of which some 6 to
+// compare tokens and 3 to count them). One row takes 3.0 us, a launch and two
+// dependent loads.
 #include <algorithm>
 
 #include "../../include/qwen3_decode.h"
@@ -18,44 +19,13 @@
 namespace {
 
 constexpr int VEC = 8;
-// Changed logits of eight that are taken one at a time; with more in some lane, all eight at once. The two rows below at
-// 64 of 151,936 and 96 of 50,257 logits: 14.7 and 19.6 us with 0, 13.4 and 19.5 with 2, 13.3 and 21.4 with 8.
+// Changed logits of eight that are taken one at a time; with more in some lane, all eight at once. 64 rows of 151,936
+// after 2,048 tokens 14.4, 13.1, 13.0 us with 0, 2, 8; 96 of 50,257 after 30,000 17.2, 17.1, 18.7; one row after 200
+// 3.2, 3.2, 3.7.
 constexpr int FEW = 2;
 
-// Counts of a token in 15 bits, two a word, where a history cannot have more of
-// it, otherwise in 31; the bit above says that it was seen in the prompt.
-template <bool SHORT>
-struct Counts {
-  static constexpr int BITS = SHORT ? 16 : 32;
-  static constexpr uint32_t SEEN = 1u << (BITS - 1);
-  static constexpr int words(int piece) { return SHORT ? piece / 2 : piece; }
-  static DEV void add(uint32_t* c, unsigned v) {
-    if constexpr (SHORT) atomicAdd(c + v / 2, 1u << (16 * (v & 1)));
-    else atomicAdd(c + v, 1u);
-  }
-  static DEV void see(uint32_t* c, unsigned v) {
-    if constexpr (SHORT) atomicOr(c + v / 2, SEEN << (16 * (v & 1)));
-    else atomicOr(c + v, SEEN);
-  }
-  static DEV uint32_t get(const uint32_t* c, unsigned v) {
-    if constexpr (SHORT) return c[v / 2] >> (16 * (v & 1)) & 0xffffu;
-    else return c[v];
-  }
-  // of tokens v..v+7
-  static DEV void eight(const uint32_t* c, unsigned v, uint32_t* of) {
-    const uint4 a = reinterpret_cast<const uint4*>(c)[SHORT ? v / 8 : v / 4];
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-    if constexpr (SHORT) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) of[k] = k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xffffu;
-    } else {
-      const uint4 b = reinterpret_cast<const uint4*>(c)[v / 4 + 1];
-      const uint32_t u[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-      for (int k = 0; k < 8; ++k) of[k] = k < 4 ? w[k] : u[k - 4];
-    }
-  }
-};
+// A token's count; the highest bit says that it was seen in the prompt.
+constexpr uint32_t SEEN = 1u << 31;
 
 // Eight logits as they are in memory, where rows begin at any element.
 template <bool BF16>
@@ -101,21 +71,19 @@ struct __attribute__((packed, aligned(4))) Quad { int32_t t[4]; };
 
 // LDS of a workgroup, in words: counts, a bit for each logit with a bias, the
 // biases of the piece (how many, then token, entry and value of each).
-template <bool SHORT>
 __host__ DEV int lds_words(const qwen3_logits& l, int piece) {
-  return (l.d_history || l.d_path ? Counts<SHORT>::words(piece) : 0) + (l.n_bias > 0 ? piece / 32 + 4 + 3 * l.n_bias : 0);
+  return (l.d_history || l.d_path ? piece : 0) + (l.n_bias > 0 ? piece / 32 + 4 + 3 * l.n_bias : 0);
 }
 
 // (waves a SIMD, by the registers: four workgroups a CU)
-template <bool BF16, bool SHORT, int THREADS, int STEPS>
+template <bool BF16, int THREADS, int STEPS>
 __global__ __launch_bounds__(THREADS, 8) void logits_kernel(qwen3_logits l, const void* in, void* out) {
-  using C = Counts<SHORT>;
   constexpr int STEP = THREADS * VEC, PIECE = STEPS * STEP;
   constexpr int AT_ONCE = 4 * THREADS;   // history tokens under way (twice as many: 12.9 -> 13.4 us at 64 rows)
   extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
   const bool counting = l.d_history || l.d_path, biased = l.n_bias > 0;
   uint32_t* count = lds;
-  uint32_t* has_bias = lds + (counting ? C::words(PIECE) : 0);
+  uint32_t* has_bias = lds + (counting ? PIECE : 0);
   int* n_biases = reinterpret_cast<int*>(has_bias + PIECE / 32);
   int *bias_token = n_biases + 4, *bias_entry = bias_token + l.n_bias;
   float* bias_value = reinterpret_cast<float*>(bias_entry + l.n_bias);
@@ -168,7 +136,7 @@ __global__ __launch_bounds__(THREADS, 8) void logits_kernel(qwen3_logits l, cons
   if (counting || biased) {
     if (counting) {
 #pragma unroll
-      for (int i = tid; i < C::words(PIECE) / 4; i += THREADS) reinterpret_cast<uint4*>(count)[i] = make_uint4(0, 0, 0, 0);
+      for (int i = tid; i < PIECE / 4; i += THREADS) reinterpret_cast<uint4*>(count)[i] = make_uint4(0, 0, 0, 0);
     }
     if (biased) {
       for (int i = tid; i < PIECE / 32; i += THREADS) has_bias[i] = 0;
@@ -188,13 +156,13 @@ __global__ __launch_bounds__(THREADS, 8) void logits_kernel(qwen3_logits l, cons
       const int next = i0 + AT_ONCE, i = i0 + 4 * tid;
       if (next < len) quad = load(next);
       if (next <= min(len, prompt)) {
-        four(now, i, [&](unsigned v, int) { C::see(count, v); });
+        four(now, i, [&](unsigned v, int) { atomicOr(count + v, SEEN); });
       } else if (next <= len && i0 >= prompt) {
-        four(now, i, [&](unsigned v, int) { C::add(count, v); });
+        four(now, i, [&](unsigned v, int) { atomicAdd(count + v, 1u); });
       } else {
         four(now, i, [&](unsigned v, int k) {
-          if (k < min(len, prompt)) C::see(count, v);
-          else if (k < len) C::add(count, v);
+          if (k < min(len, prompt)) atomicOr(count + v, SEEN);
+          else if (k < len) atomicAdd(count + v, 1u);
         });
       }
     }
@@ -203,7 +171,7 @@ __global__ __launch_bounds__(THREADS, 8) void logits_kernel(qwen3_logits l, cons
 #pragma unroll 1
       for (int i = tid; i < l.path_len; i += THREADS) {
         const int token = l.d_path[(size_t)row * l.path_len + i];
-        if (piece_has(token)) C::add(count, token - v0);
+        if (piece_has(token)) atomicAdd(count + token - v0, 1u);
       }
     }
 #pragma unroll 1
@@ -226,7 +194,7 @@ __global__ __launch_bounds__(THREADS, 8) void logits_kernel(qwen3_logits l, cons
   // a logit as its token's count leaves it (both quotient and product: a branch would cost more)
   auto counted = [&](float y, uint32_t c) {
     const float less = y / rep, more = y * rep, seen = y > 0.0f ? less : more;
-    const uint32_t times = c & ~C::SEEN;
+    const uint32_t times = c & ~SEEN;
     const float off = times ? freq * (float)times + pres : 0.0f;
     return c ? seen - off : y;
   };
@@ -264,15 +232,16 @@ __global__ __launch_bounds__(THREADS, 8) void logits_kernel(qwen3_logits l, cons
 #pragma unroll
     for (int e = 0; e < VEC; ++e) x[e] = raw[k].get(e);
     if (counting) {
-      uint32_t c[VEC], some = 0;
-      C::eight(count, i0, c);
+      const uint4 *words = reinterpret_cast<const uint4*>(count + i0), lo = words[0], hi = words[1];
+      const uint32_t c[VEC] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+      uint32_t some = 0;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) some |= c[e] ? 1u << e : 0u;
       if (__ballot(__builtin_popcount(some) > FEW) != 0) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) x[e] = counted(x[e], c[e]);
       } else {
-        each(x, some, [&](int e, float y) { return counted(y, C::get(count, i0 + e)); });
+        each(x, some, [&](int e, float y) { return counted(y, count[i0 + e]); });
       }
     }
     if (biased) each(x, has_bias[i0 / 32] >> (i0 & 31) & 0xffu, [&](int e, float y) { return with_bias(y, i0 + e); });
@@ -285,30 +254,29 @@ __global__ __launch_bounds__(THREADS, 8) void logits_kernel(qwen3_logits l, cons
   const int i = n / VEC * VEC + tid;
   if (i < n) {
     float y = load1<BF16>(in, at + i);
-    if (counting) y = counted(y, C::get(count, i));
+    if (counting) y = counted(y, count[i]);
     if (biased && has_bias[i / 32] >> (i & 31) & 1) y = with_bias(y, i);
     if (mask && !((uint32_t)mask[i / 32] >> (i & 31) & 1)) y = -INFINITY;
     store1<BF16>(out, to + i, y);
   }
 }
 
-template <bool BF16, bool SHORT, int THREADS, int STEPS>
+template <bool BF16, int THREADS, int STEPS>
 void launch_pieces(const qwen3_logits& l, const void* in, void* out, hipStream_t s) {
   constexpr int PIECE = STEPS * THREADS * VEC;
-  hipLaunchKernelGGL((logits_kernel<BF16, SHORT, THREADS, STEPS>), dim3((l.vocab + PIECE - 1) / PIECE, l.rows),
-                     dim3(THREADS), sizeof(uint32_t) * lds_words<SHORT>(l, PIECE), s, l, in, out);
+  hipLaunchKernelGGL((logits_kernel<BF16, THREADS, STEPS>), dim3((l.vocab + PIECE - 1) / PIECE, l.rows), dim3(THREADS),
+                     sizeof(uint32_t) * lds_words(l, PIECE), s, l, in, out);
 }
 
 template <bool BF16>
 void launch(const qwen3_logits& l, const void* in, void* out, hipStream_t s) {
   const long all = (long)l.rows * l.vocab;
   const long longest = (l.d_history ? l.history_stride : 0) + (long)l.path_len;
-  // 64 rows of 151,936 after 2,048 tokens: 14.6 us in pieces of 8,192 (512 threads), 15.1 of 2,048 (256), 16.2 of
-  // 8,192 (256), 17.3 of 16,384; 96 rows of 50,257 after 30,000: 22.5, 31.6, 29.4, 24.4. Small calls take more
-  // workgroups of less.
-  if (longest >= Counts<true>::SEEN) launch_pieces<BF16, false, 512, 2>(l, in, out, s);
-  else if (all >= 512l * 2048 || longest > 4096) launch_pieces<BF16, true, 512, 2>(l, in, out, s);
-  else launch_pieces<BF16, true, 256, 1>(l, in, out, s);
+  // Pieces of 8,192 by 512 threads where there is enough work or a long history, of 2,048 by 256 otherwise. 64 rows of
+  // 151,936 after 2,048 tokens, with all adjustments: 13.1 us so, 13.3 in pieces of 2,048, 12.9 of 4,096 (256 threads),
+  // 14.4 of 8,192 (1,024 threads); 96 rows of 50,257 after 30,000: 16.2, 23.1, 18.6, 15.7; one row after 200: 4.0, 3.0.
+  if (all >= 512l * 2048 || longest > 4096) launch_pieces<BF16, 512, 2>(l, in, out, s);
+  else launch_pieces<BF16, 256, 1>(l, in, out, s);
 }
 
 }  // namespace
