@@ -279,14 +279,13 @@ def adjust_logits(logits, history=None, prompt_lens=None, lens=None, repetition=
     device, index = logits.device, logits.get_device()
 
     def given(t, name, dtype, shape):
-        if t is None:
-            return 0
         if not (type(t) is torch.Tensor and t.dtype is dtype and t.shape == shape and t.get_device() == index
                 and t.is_contiguous()):
             _device_rows(t, name, dtype, logits, shape)
         return t.data_ptr()
 
     I, F = torch.int32, torch.float32
+    per_row = (rows,)
     n_seq = stride = path_len = n_bias = n_masks = 0
     if history is not None:
         if history.dim() != 2 or lens is None:
@@ -304,18 +303,21 @@ def adjust_logits(logits, history=None, prompt_lens=None, lens=None, repetition=
         if masks.dim() != 2:
             raise ValueError("masks are [n_masks, ceil(vocab / 32)]")
         n_masks = masks.shape[0]
-    for n in (rows, vocab, n_seq, stride, path_len, n_bias, n_masks):
-        i32(n)
+    i32(max(rows, vocab, n_seq, stride, path_len, n_bias, n_masks))
     # (a packed description: setting 22 fields of a structure takes 3 us)
     desc = _LOGITS.pack(rows, vocab, logits.dtype is torch.bfloat16, logits.stride(0) if rows > 1 else vocab,
                         out.stride(0) if rows > 1 else vocab, n_seq, stride, path_len, n_bias, n_masks,
                         given(history, "history", I, (n_seq, stride)) if stride else 0,
-                        given(prompt_lens, "prompt_lens", I, (n_seq,)), given(lens, "lens", I, (n_seq,)),
-                        given(row_seq, "row_seq", I, (rows,)), given(path, "path", I, (rows, path_len)),
-                        given(repetition, "repetition", F, (rows,)), given(frequency, "frequency", F, (rows,)),
-                        given(presence, "presence", F, (rows,)), given(bias_ids, "bias_ids", I, (rows, n_bias)),
-                        given(bias, "bias", F, (rows, n_bias)),
-                        given(masks, "masks", I, (n_masks, (vocab + 31) // 32)),
-                        given(row_mask, "row_mask", I, (rows,)))
+                        0 if prompt_lens is None else given(prompt_lens, "prompt_lens", I, (n_seq,)),
+                        0 if lens is None else given(lens, "lens", I, (n_seq,)),
+                        0 if row_seq is None else given(row_seq, "row_seq", I, per_row),
+                        0 if path is None else given(path, "path", I, (rows, path_len)),
+                        0 if repetition is None else given(repetition, "repetition", F, per_row),
+                        0 if frequency is None else given(frequency, "frequency", F, per_row),
+                        0 if presence is None else given(presence, "presence", F, per_row),
+                        0 if bias_ids is None else given(bias_ids, "bias_ids", I, (rows, n_bias)),
+                        0 if bias is None else given(bias, "bias", F, (rows, n_bias)),
+                        0 if masks is None else given(masks, "masks", I, (n_masks, (vocab + 31) // 32)),
+                        0 if row_mask is None else given(row_mask, "row_mask", I, per_row))
     _check(on_stream(device, lib().qwen3_adjust_logits, desc, logits.data_ptr(), out.data_ptr()))
     return out
