@@ -676,7 +676,7 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : 64 * WPR) void tree_join_kernel(Tr
   constexpr int LANES = HD / 8, GROUPS = 64 / LANES;
   __shared__ float other[WPR][HD + 2];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, G = a.H / a.Hkv;
-  const long at = WPR == 1 ? (long)blockIdx.x * 4 + wave : blockIdx.x;
+  const long team = (long)blockIdx.y * gridDim.x + blockIdx.x, at = WPR == 1 ? team * 4 + wave : team;
   const int token = (int)(at / a.H), h = (int)(at - (long)token * a.H);
   if (token >= a.n_rows) return;
   // the sequence that has the row: the last one that begins at or before it
@@ -818,6 +818,11 @@ auto with_walk(const TreeArgs& a, Fn f) {
   return rows <= 32 ? f(Int<64>{}, Int<1>{}) : rows <= 64 ? f(Int<64>{}, Int<2>{}) : f(Int<64>{}, Int<4>{});
 }
 
+// `teams` workgroups of 256 threads: a dimension of a grid has less than 2^32 threads, which 2^26 rows reach
+dim3 join_grid(long teams) {
+  return teams < 1l << 24 ? dim3((unsigned)teams) : dim3((unsigned)((teams + 1) / 2), 2);
+}
+
 // Tiles of all sequences at their longest, and of one of their segments.
 template <class W>
 double most_tiles(const TreeArgs& a, double* segment) {
@@ -858,7 +863,7 @@ hipError_t launch_tree(const TreeArgs& a, hipStream_t s) {
       // 8 waves a row where rows are few and their parts many: one token over 131,071 of one key/value head with 8 query
       // heads 48 us with one wave, 27 with 8, of 8 heads with 16 94 and 92; 16 trees of 24 drafts 40 and 68
       if (rows <= 512) hipLaunchKernelGGL((tree_join_kernel<HD, RB, 8>), dim3((unsigned)rows), dim3(512), 0, s, a);
-      else hipLaunchKernelGGL((tree_join_kernel<HD, RB, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
+      else hipLaunchKernelGGL((tree_join_kernel<HD, RB, 1>), join_grid((rows + 3) / 4), dim3(256), 0, s, a);
     }
     return hipGetLastError();
   });

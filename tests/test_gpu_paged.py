@@ -499,3 +499,22 @@ def test_divisions_of_ragged_lengths(H, Hkv, hd, new, lens):
     assert torch.equal(y, again)
     sees = [np.tri(k, dtype=bool) for k in news]
     check(y, lse, starts, reference(c, x, starts, lens, sees, H, Hkv, hd, 0))
+
+
+@pytest.mark.parametrize("n_rows", [2 ** 26 - 1, 2 ** 26 - 3])
+def test_as_many_rows_as_a_call_takes(n_rows):
+    """n_head * n_rows just below 2^26, where the workgroups that join parts have
+    2^32 threads: one token of a sequence of many parts, in the last row."""
+    torch.manual_seed(4)
+    hd, n = 64, 600
+    c = db().PagedCache.empty(1, 40, 1, 16, hd, 1, 40)
+    x = torch.randn(1, n + 1, 3 * hd, device="cuda").bfloat16()
+    c.append(x, ints([0, n]), n)
+    qkv = torch.empty(n_rows, 3 * hd, dtype=torch.bfloat16, device="cuda")
+    qkv[-1] = x[0, n]
+    y, lse = c.attention(qkv, ints([n_rows - 1, n_rows]), 1)
+    small = torch.empty(700, 3 * hd, dtype=torch.bfloat16, device="cuda")   # joined likewise, a wave a row
+    small[-1] = x[0, n]
+    z, zl = c.attention(small, ints([699, 700]), 1)
+    assert torch.equal(y[-1], z[-1]) and torch.equal(lse[:, -1], zl[:, -1])
+    check(y[-1:], lse[:, -1:], [0, 1], reference(c, x[0, n:], [0, 1], [n], [np.ones((1, 1), bool)], 1, 1, hd, 0))
