@@ -135,7 +135,10 @@ gpt2_status qwen3_set_cache(qwen3_model* m, const qwen3_cache* c,
                             int32_t mask_words, int32_t max_new,
                             void* d_workspace, size_t workspace_bytes);
 /* qwen3_cache_append of the last forward's rows to the cache that it read, on
- * the model's stream. STATE without such a forward. */
+ * the model's stream. STATE without such a forward. Of every sequence's rows
+ * that forward computed the first max_new that qwen3_set_cache was given:
+ * without d_path a larger max_new is INVALID_ARG, and a path entry that names a
+ * row behind them is one that is not among the sequence's rows. */
 gpt2_status qwen3_keep_tokens(qwen3_model* m, const int32_t* d_counts,
                               const int32_t* d_path, int32_t max_new);
 /* Where the last forward's logits are: bf16 [rows][vocab] at *offset_bytes of

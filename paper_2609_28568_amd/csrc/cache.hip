@@ -249,7 +249,7 @@ __global__ __launch_bounds__(64) void append_move_kernel(CacheArgs c, AppendArgs
     const int b = clampi(a.starts[s], 0, a.n_rows), e = clampi(a.starts[s + 1], b, a.n_rows);
     const int row = a.path ? a.path[(size_t)s * a.max_new + i] : i;
     const int pos = r.x + i, page = c.table[(size_t)s * c.max_pages + pos / c.ps];
-    if ((unsigned)row >= (unsigned)(e - b) || (unsigned)page >= (unsigned)c.n_pages) return;
+    if ((unsigned)row >= (unsigned)min(e - b, a.max_rows) || (unsigned)page >= (unsigned)c.n_pages) return;
     const uint4* from = reinterpret_cast<const uint4*>(
         a.qkv + layer * a.layer_stride + (size_t)(b + row) * (a.H + 2 * c.Hkv) * c.hd + (size_t)a.H * c.hd);
     uint4* to = reinterpret_cast<uint4*>(c.pages + page_at(c, layer, page) + (size_t)(pos % c.ps) * c.hd);

@@ -451,6 +451,7 @@ struct AppendArgs {
   int H, n_rows, max_new;
   size_t layer_stride;
   const int32_t *starts, *counts, *path;
+  int max_rows = INT32_MAX;   // of a sequence's rows, those that a path may name
 };
 hipError_t launch_cache_append(const CacheArgs& c, const AppendArgs& a, hipStream_t s);
 hipError_t launch_cache_compact(const CacheArgs& c, hipStream_t s);

@@ -1173,8 +1173,11 @@ gpt2_status qwen3_keep_tokens(qwen3_model* m, const int32_t* d_counts, const int
   if (!m->forwarded || !m->cache_used.args.starts) return fail(m, GPT2_ERR_STATE, "no forward over a cache");
   const Dims& d = m->d;
   const CacheUse& use = m->cache_used;
+  // rows behind the forward's max_new have no attention, so their keys and values are nothing to keep
+  if (!d_path && std::min(max_new, (int32_t)d.BT) > use.args.max_new)
+    return fail(m, GPT2_ERR_INVALID_ARG, "max_new is more than the forward over the cache computed");
   const AppendArgs a{m->ab(m->act.packed), d.H, (int)d.BT, max_new, m->act.s_packed / sizeof(bf16_t), use.args.starts,
-                     d_counts, d_path};
+                     d_counts, d_path, use.args.max_new};
   if (const char* why = append_check(&use.c, a)) return fail(m, GPT2_ERR_INVALID_ARG, why);
   TRY(m->run(QWEN3_K_OTHER, 0.0, 0.0, [&] { return launch_cache_append(cache_args(use.c), a, m->stream); }));
   return GPT2_OK;

@@ -510,7 +510,8 @@ class Qwen3:
 
     def keep_tokens(self, max_new, counts=None, path=None):
         """PagedCache.append of the last forward's rows to the cache that it
-        read (qwen3_keep_tokens), on the model's stream."""
+        read (qwen3_keep_tokens), on the model's stream; of a sequence's rows
+        those up to set_cache's max_new can be kept."""
         from . import decode_binding as db
         used = self._in_use and self._in_use[2]
         n_seq = used[0].lens.shape[0] if used else None

@@ -241,3 +241,33 @@ def test_the_model_refuses_caches_that_are_not_its_own():
     a.m.forward(torch.zeros(1, 64, dtype=torch.int32, device="cuda"))
     a.m.keep_tokens(1)
     assert good.lens.tolist() == [0, 0, 0] and good.short.item() == 0
+
+
+def test_only_rows_that_the_forward_computed_are_kept():
+    """A forward of two rows a sequence where one has four: more of them are
+    refused, and a path that names the others leaves their places."""
+    from paper_2609_28568_amd import binding
+    a = Answers(seed=61)
+    a.cache.pages.fill_(7)
+    ids = torch.zeros(1, 64, dtype=torch.int32, device="cuda")
+    ids[0, :5] = ints([3, 4, 5, 6, 7])
+    a.m.set_cache(a.cache, ints([0, 4, 5, 5, 5, 5]), 2)
+    a.m.forward(ids)
+    for n in (3, 4, 64, 1000):
+        with pytest.raises(binding.LibError, match="max_new"):
+            a.m.keep_tokens(n)
+    torch.cuda.synchronize()
+    assert not a.cache.lens.any() and bool((a.cache.pages == 7).all())
+    a.m.keep_tokens(4, ints([4, 2, 0, 0, 0]), ints([[1, 2, 0, 3], [0, 1, -1, -1]] + [[-1] * 4] * 3))
+    torch.cuda.synchronize()
+    assert a.cache.lens.tolist() == [4, 2, 0, 0, 0]
+    left = (a.cache.pages == 7).all(-1)   # [layer, page, 2, head, token]
+    assert not left[:, 0, :, :, [0, 2]].any() and bool(left[:, 0, :, :, [1, 3]].all())   # rows 1 and 0; 2 and 3
+    assert not left[:, 1, :, :, 0].any() and bool(left[:, 1, :, :, 1].all())             # another sequence's row
+    a.m.keep_tokens(2)
+    assert a.cache.lens.tolist() == [6, 3, 0, 0, 0]
+    # as many rows as there are, whatever the call says
+    a.m.set_cache(a.cache, ints([0, 4, 5, 5, 5, 5]), 1000)
+    a.m.forward(ids)
+    a.m.keep_tokens(500)
+    assert a.cache.lens.tolist() == [10, 4, 0, 0, 0] and a.cache.short.item() == 0
