@@ -58,7 +58,8 @@ gpt2_status qwen3_cache_fork(const qwen3_cache* c, const int32_t* d_src,
  * d_path int32 [n_seq][max_new], rows d_starts[s] + d_path[s][i], i <
  * d_counts[s] (a tree's accepted tokens); a path entry that is not among the
  * sequence's rows leaves its token's place in the cache as it was. No sequence
- * takes more than max_new.
+ * takes more than max_new, which is below 2^22, or small enough that n_seq *
+ * max_new is below 2^25; with d_path the latter in any case.
  * Pages are taken from the free ones, the lowest numbers first, for the
  * sequences in their order. Tokens on a last page that others have too are
  * copied to one of its own first. d_short receives the number of pages that

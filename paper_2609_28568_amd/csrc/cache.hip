@@ -234,34 +234,54 @@ DEV size_t page_at(const CacheArgs& c, int layer, int page) {   // in elements
   return ((size_t)layer * c.n_pages + page) * (2 * (size_t)c.Hkv * c.ps * c.hd);
 }
 
-// Tokens into their places, a wave one token of one layer, and behind those
-// blocks the shared pages' tokens, a wave one head of one page. Written past the
+// The sequence that has row `row`: the last one that begins at or before it, -1
+// where none does. By all lanes, in one load of starts, or two past 64 sequences.
+DEV int seq_of_row(const int32_t* starts, int n_seq, int row) {
+  const int lane = threadIdx.x & 63, step = (n_seq + 63) / 64;
+  const int i = lane * step;
+  int s = __popcll(__ballot(i < n_seq && starts[min(i, n_seq)] <= row)) - 1;
+  if (step > 1 && s >= 0) {
+    s *= step;
+    const int j = s + lane;
+    s += __popcll(__ballot(lane < step && j < n_seq && starts[min(j, n_seq)] <= row)) - 1;
+  }
+  return s;
+}
+
+// Tokens into their places, a wave one token of one layer (of the rows, or of
+// the path's entries: a wave each of n_seq * max_new, 63 single tokens beside a
+// piece of 2,048 in 28 layers were 789 us a pass, 81 so), and behind those blocks the shared pages' tokens, a wave one head of one page. Written past the
 // caches: prompts of a batch, 600 MB read and written, 115 us a pass through
 // them, 106 past them (5.3 TB/s); with 8 tokens a wave 143 and 136.
-__global__ __launch_bounds__(64) void append_move_kernel(CacheArgs c, AppendArgs a, int most, unsigned nt) {
+__global__ __launch_bounds__(64) void append_move_kernel(CacheArgs c, AppendArgs a, int items, int nt) {
   const int4* rec = reinterpret_cast<const int4*>(c.scratch + CACHE_HEADER);
   const int lane = threadIdx.x;
   const int hu = c.hd / 8, units = 2 * c.Hkv * hu;   // 16-byte units of a head, of a token
-  if (blockIdx.x < nt) {
-    const int layer = blockIdx.y, s = blockIdx.x / most, i = blockIdx.x - s * most;
-    const int4 r = rec[s];
-    if (i >= r.y) return;
-    const int b = clampi(a.starts[s], 0, a.n_rows), e = clampi(a.starts[s + 1], b, a.n_rows);
-    const int row = a.path ? a.path[(size_t)s * a.max_new + i] : i;
-    const int pos = r.x + i, page = c.table[(size_t)s * c.max_pages + pos / c.ps];
-    if ((unsigned)row >= (unsigned)min(e - b, a.max_rows) || (unsigned)page >= (unsigned)c.n_pages) return;
-    const uint4* from = reinterpret_cast<const uint4*>(
-        a.qkv + layer * a.layer_stride + (size_t)(b + row) * (a.H + 2 * c.Hkv) * c.hd + (size_t)a.H * c.hd);
-    uint4* to = reinterpret_cast<uint4*>(c.pages + page_at(c, layer, page) + (size_t)(pos % c.ps) * c.hd);
-    constexpr int FLIGHT = 4;
-    for (int u0 = lane; u0 < units; u0 += 64 * FLIGHT) {
-      uint4 v[FLIGHT];
+  if ((int)blockIdx.x < nt) {
+    const int layer = blockIdx.y;
+    for (int item = blockIdx.x; item < items; item += nt) {
+      const int s = a.path ? item / a.max_new : seq_of_row(a.starts, c.n_seq, item);
+      if (s < 0) continue;
+      const int4 r = rec[s];
+      const int b = clampi(a.starts[s], 0, a.n_rows), e = clampi(a.starts[s + 1], b, a.n_rows);
+      const int i = a.path ? item - s * a.max_new : item - b;
+      if ((unsigned)i >= (unsigned)r.y) continue;
+      const int row = a.path ? a.path[item] : i;
+      const int pos = r.x + i, page = c.table[(size_t)s * c.max_pages + pos / c.ps];
+      if ((unsigned)row >= (unsigned)min(e - b, a.max_rows) || (unsigned)page >= (unsigned)c.n_pages) continue;
+      const uint4* from = reinterpret_cast<const uint4*>(
+          a.qkv + layer * a.layer_stride + (size_t)(b + row) * (a.H + 2 * c.Hkv) * c.hd + (size_t)a.H * c.hd);
+      uint4* to = reinterpret_cast<uint4*>(c.pages + page_at(c, layer, page) + (size_t)(pos % c.ps) * c.hd);
+      constexpr int FLIGHT = 4;
+      for (int u0 = lane; u0 < units; u0 += 64 * FLIGHT) {
+        uint4 v[FLIGHT];
 #pragma unroll
-      for (int k = 0; k < FLIGHT; ++k) v[k] = u0 + 64 * k < units ? from[u0 + 64 * k] : make_uint4(0, 0, 0, 0);
+        for (int k = 0; k < FLIGHT; ++k) v[k] = u0 + 64 * k < units ? from[u0 + 64 * k] : make_uint4(0, 0, 0, 0);
 #pragma unroll
-      for (int k = 0; k < FLIGHT; ++k) {
-        const int u = u0 + 64 * k, h = u / hu;
-        if (u < units) st_stream(to + (size_t)h * c.ps * hu + (u - h * hu), v[k]);
+        for (int k = 0; k < FLIGHT; ++k) {
+          const int u = u0 + 64 * k, h = u / hu;
+          if (u < units) st_stream(to + (size_t)h * c.ps * hu + (u - h * hu), v[k]);
+        }
       }
     }
     return;
@@ -381,12 +401,12 @@ hipError_t launch_cache_fork(const CacheArgs& c, const int32_t* src, const int32
 
 hipError_t launch_cache_append(const CacheArgs& c, const AppendArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(append_book_kernel, dim3(1), dim3(BOOK), 0, s, c, a);
-  const int most = a.path ? a.max_new : std::min(a.max_new, std::max(a.n_rows, 1));   // tokens of a sequence
-  const unsigned nt = (unsigned)c.n_seq * most;
+  // a grid's dimension has less than 2^32 threads: past 2^20 tokens a layer waves take several
+  const int items = a.path ? c.n_seq * a.max_new : a.n_rows, nt = std::min(items, 1 << 20);
   // heads to copy at most; waves that find none cost 0.5 us, and 16 shared pages in 28 layers 22.4 us with 2,048, 18.3
   // with 8,192
   const unsigned nc = (unsigned)std::min((long)c.n_seq * 2 * c.Hkv, std::max(1l, 8192l / c.L));
-  hipLaunchKernelGGL(append_move_kernel, dim3(nt + nc, c.L), dim3(64), 0, s, c, a, most, nt);
+  hipLaunchKernelGGL(append_move_kernel, dim3(nt + nc, c.L), dim3(64), 0, s, c, a, items, nt);
   return hipGetLastError();
 }
 

@@ -99,7 +99,9 @@ const char* tree_check(const qwen3_cache* c, const qwen3_tree* t, bool sizes_onl
 const char* append_check(const qwen3_cache* c, const AppendArgs& a) {
   if (const char* why = cache_check(c)) return why;
   if (const char* why = heads_check(*c, a.H, a.n_rows)) return why;
-  if (a.max_new < 1 || (long)a.max_new * c->n_seq >= 1l << 25) return "max_new out of range";
+  // (the pages that all sequences may need stay below 2^31)
+  if (a.max_new < 1 || ((a.path || a.max_new >= 1 << 22) && (long)a.max_new * c->n_seq >= 1l << 25))
+    return "max_new out of range";
   if (!a.starts || (!a.qkv && a.n_rows > 0)) return "null argument";
   if (a.path && !a.counts) return "a path needs counts";
   if (!aligned(a.qkv, 16) || !aligned(a.starts, 4) || !aligned(a.counts, 4) || !aligned(a.path, 4))

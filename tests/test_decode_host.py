@@ -260,3 +260,15 @@ def test_masks_without_words_are_refused(shape):
     with pytest.raises(ValueError, match="word"):
         db.mask_words(torch.zeros(*shape, dtype=torch.int32))
     assert db.mask_words(torch.zeros(0, 2, dtype=torch.int32)) == 2
+
+
+@pytest.mark.parametrize("n_seq,max_new,path,reason", [
+    (4096, 8192, None, None), (4096, (1 << 22) - 1, None, None), (1, (1 << 25) - 1, None, None), (8, (1 << 22) - 1, None, None),
+    (8, 1 << 22, None, "max_new"), (1, 1 << 25, None, "max_new"), (4096, 8191, 1 << 21, None), (4096, 8192, 1 << 21, "max_new")])
+def test_appends_of_one_long_piece_among_many_sequences(n_seq, max_new, path, reason):
+    """Without a path the rows bound the work, not n_seq * max_new: what is taken
+    gets as far as the overlap of its counts with the cache's lengths."""
+    c = cache(n_seq=n_seq)
+    counts = FAR + (2 << 40)
+    assert db.lib().qwen3_cache_append(ctypes.byref(c), 4096, 4, 8, 0, 1 << 22, counts, path, max_new, None) == INVALID
+    assert (reason or "overlap") in why()

@@ -518,3 +518,23 @@ def test_as_many_rows_as_a_call_takes(n_rows):
     z, zl = c.attention(small, ints([699, 700]), 1)
     assert torch.equal(y[-1], z[-1]) and torch.equal(lse[:, -1], zl[:, -1])
     check(y[-1:], lse[:, -1:], [0, 1], reference(c, x[0, n:], [0, 1], [n], [np.ones((1, 1), bool)], 1, 1, hd, 0))
+
+
+@pytest.mark.parametrize("n_seq,piece,at", [(64, 2048, 63), (200, 3001, 137), (4096, 8192, 2500)])
+def test_one_long_piece_appended_among_single_tokens(n_seq, piece, at):
+    """Every third sequence gets nothing, one a piece, the others a token; rows
+    before the first sequence's and behind the last one's are nobody's."""
+    layers, H, Hkv, hd, ps = 2, 2, 1, 64, 16
+    pages = -(-piece // ps) + 1
+    c = db().PagedCache.empty(layers, pages + n_seq, Hkv, ps, hd, n_seq, pages)
+    m = Model(pages + n_seq, n_seq, pages, ps)
+    new = [0 if s % 3 == 2 else 1 for s in range(n_seq)]
+    new[at] = piece
+    lead = 5
+    starts = (lead + np.concatenate([[0], np.cumsum(new)])).tolist()
+    x = torch.randn(layers, starts[-1] + 3, (H + 2 * Hkv) * hd, generator=torch.Generator().manual_seed(8)).bfloat16()
+    c.append(x.cuda(), ints(starts), piece)
+    value = {(s, i): x[:, starts[s] + i].view(layers, H + 2 * Hkv, hd)[:, H:].reshape(layers, 2, Hkv, hd)
+             for s, k in enumerate(new) for i in range(k)}
+    assert m.append([[(s, i) for i in range(k)] for s, k in enumerate(new)]) == 0 == c.short.item()
+    agree(c, m, value)
