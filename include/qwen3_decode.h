@@ -92,7 +92,10 @@ gpt2_status qwen3_cache_compact(const qwen3_cache* c, void* hip_stream);
  * overlaps an input or the other. Of every sequence's rows the first max_new
  * are computed; other rows are left as they were. d_workspace:
  * qwen3_tree_size bytes, 256-byte aligned, scratch until the call's kernels have
- * run: calls that may run at the same time take one each. */
+ * run: calls that may run at the same time take one each.
+ * The work that the capacities allow is counted in 32 bits: (max_pages *
+ * page_size + max_new + 64) / 32 * (n_head * n_rows / 32 + n_kv_head * n_seq) up
+ * to 2 * 10^9 is taken, what is much beyond is INVALID_ARG. */
 typedef struct qwen3_tree {
   int32_t n_head, n_rows;   /* n_head * n_rows below 2^26 */
   int32_t max_new;       /* no sequence has more new tokens */

@@ -75,6 +75,9 @@ DEV Seq seq_from(const TreeArgs& a, int len, int start, int n) {
   q.blocks = (n * (a.H / a.Hkv) + W::ROWS - 1) / W::ROWS;
   return q;
 }
+// Whether sequence s ends before it begins, which starts must not: nothing is computed then, as the sums of tiles are
+// bounded by rows that belong to one sequence.
+DEV bool falls(const TreeArgs& a, int s) { return a.starts[s + 1] < a.starts[s]; }
 template <class W>
 DEV Seq seq_of(const TreeArgs& a, int s) {
   const int start = clampi(a.starts[s], 0, a.n_rows);
@@ -153,6 +156,12 @@ DEV void store_cuts(const TreeArgs& a, int sum, const Cuts& c) {
 template <class W>
 __global__ __launch_bounds__(64) void tree_plan_kernel(TreeArgs a) {
   const int lane = threadIdx.x;
+  bool bad = false;
+  for (int s = lane; s < a.n_seq; s += 64) bad |= falls(a, s);
+  if (__ballot(bad) != 0) {
+    if (lane == 0) store_cuts(a, 0, Cuts{LINE, W::LEAST});
+    return;
+  }
   auto over = [&](auto f) {   // the sum over the sequences
     int sum = 0;
     for (int s = lane; s < a.n_seq; s += 64) sum += f(seq_of<W>(a, s));
@@ -198,7 +207,11 @@ struct Line {
       return;
     }
     Seq q{};
-    if (lane < a.n_seq) q = seq_of<W>(a, lane);
+    bool bad = false;
+    if (lane < a.n_seq) {
+      q = seq_of<W>(a, lane);
+      bad = falls(a, lane);
+    }
     len = q.len;
     start = q.start;
     n = q.n;
@@ -207,7 +220,7 @@ struct Line {
                       [&](int share) { return wave_total(pieces_of<W>(q.t, share) * each); });
     const int u = (cuts.x == DEALT ? pieces_of<W>(q.t, cuts.y) : q.t) * each, x = wave_scan(u);
     base = x - u;
-    sum = __builtin_amdgcn_readlane(x, 63);
+    sum = __ballot(bad) ? 0 : __builtin_amdgcn_readlane(x, 63);
   }
   // the sequence that has tile (worker) p < sum, and what is before it
   DEV int find(const TreeArgs& a, int p, int* before) const {
@@ -688,6 +701,7 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : 64 * WPR) void tree_join_kernel(Tr
   if (s < 0) return;
   const int before = a.plan[s];
   const Cuts cuts = {a.plan[a.n_seq + 1], a.plan[a.n_seq + 2]};
+  if (a.plan[a.n_seq] == 0) return;
   const Seq q = seq_of<W>(a, s);
   const int i = token - q.start;
   if (i < 0 || i >= q.n) return;
@@ -823,11 +837,14 @@ dim3 join_grid(long teams) {
   return teams < 1l << 24 ? dim3((unsigned)teams) : dim3((unsigned)((teams + 1) / 2), 2);
 }
 
-// Tiles of all sequences at their longest, and of one of their segments.
+// Tiles of all sequences at their longest, and of one of their segments. Blocks of rows are bounded by the rows, too:
+// one piece of a prompt among many single tokens has many, the others have one each.
 template <class W>
 double most_tiles(const TreeArgs& a, double* segment) {
   *segment = std::ceil((double)a.max_pages * a.ps / W::KT) + std::ceil((double)a.max_new / W::KT);
-  return *segment * a.n_seq * a.Hkv * std::ceil((double)a.max_new * (a.H / a.Hkv) / W::ROWS);
+  const double G = a.H / a.Hkv;
+  return *segment * a.Hkv *
+         std::min(a.n_seq * std::ceil(a.max_new * G / W::ROWS), std::floor(a.n_rows * G / W::ROWS) + a.n_seq);
 }
 
 }  // namespace

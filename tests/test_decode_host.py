@@ -272,3 +272,14 @@ def test_appends_of_one_long_piece_among_many_sequences(n_seq, max_new, path, re
     counts = FAR + (2 << 40)
     assert db.lib().qwen3_cache_append(ctypes.byref(c), 4096, 4, 8, 0, 1 << 22, counts, path, max_new, None) == INVALID
     assert (reason or "overlap") in why()
+
+
+def test_tiles_are_bounded_by_the_rows():
+    """4,096 sequences of up to 131,072 tokens, one of them with a piece of a prompt
+    of 4,096: not as if all of them had one."""
+    c, n, L = cache(n_kv_head=8, n_seq=4096, max_pages=8192), ctypes.c_size_t(), db.lib()
+    assert L.qwen3_tree_size(ctypes.byref(c), ctypes.byref(db.Tree(16, 8191, 4096, 0, 0)), ctypes.byref(n)) == 0
+    assert n.value > 0
+    c.max_pages, t = 1 << 15, db.Tree(16, (1 << 22) - 1, 4096, 0, 0)   # 69,632 blocks of 8,256 tiles, 8 heads
+    assert L.qwen3_tree_size(ctypes.byref(c), ctypes.byref(t), ctypes.byref(n)) == INVALID
+    assert "too many or too long" in why()

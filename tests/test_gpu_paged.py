@@ -538,3 +538,56 @@ def test_one_long_piece_appended_among_single_tokens(n_seq, piece, at):
              for s, k in enumerate(new) for i in range(k)}
     assert m.append([[(s, i) for i in range(k)] for s, k in enumerate(new)]) == 0 == c.short.item()
     agree(c, m, value)
+
+
+def pick(c, x, starts, lens, sees, some, heads):
+    """reference() of some sequences: (their rows of an output, starts, the reference) of it."""
+    from types import SimpleNamespace
+    rows = torch.cat([torch.arange(starts[s], starts[s + 1]) for s in some]).cuda()
+    at = np.concatenate([[0], np.cumsum([starts[s + 1] - starts[s] for s in some])]).tolist()
+    part = SimpleNamespace(pages=c.pages, table=c.table[torch.tensor(some, device="cuda")])
+    return rows, at, reference(part, x[rows], at, [lens[s] for s in some], [sees[s] for s in some], *heads, 0)
+
+
+def test_one_long_piece_among_the_most_sequences():
+    """4,096 sequences in a table for 131,072 tokens each, one with a piece of a
+    prompt of 4,096, the others with a token or none: the same bits as in a table
+    that is hardly wider than what they have, and what the definition says."""
+    n, H, Hkv, hd, ps, at, piece = 4096, 16, 8, 128, 16, 1717, 4096
+    torch.manual_seed(12)
+    lens = [37 * s % 90 for s in range(n)]
+    lens[at] = 777
+    held = [-(-k // ps) for k in lens]
+    pages = torch.randn(1, sum(held), 2, Hkv, ps, hd, device="cuda").bfloat16()
+    new = [0 if s % 5 == 4 else 1 for s in range(n)]
+    new[at] = piece
+    starts = np.concatenate([[0], np.cumsum(new)]).tolist()
+    order, x = torch.randperm(sum(held)).int(), torch.randn(starts[-1], (H + 2 * Hkv) * hd, device="cuda").bfloat16()
+    got = []
+    for width in (max(held) + 1, 8192):
+        table, k = torch.full((n, width), -1, dtype=torch.int32), 0
+        for s, h in enumerate(held):
+            table[s, :h] = order[k:k + h]
+            k += h
+        refs = torch.ones(sum(held), dtype=torch.int32, device="cuda")
+        c = db().PagedCache(pages, table.cuda(), ints(lens), refs, ints([0]))
+        got.append(c.attention(x, ints(starts), piece))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    y, lse = got[1]
+    some = list(range(0, n, 41)) + [at - 1, at, at + 1]
+    sees = [None] * n
+    for s in some:
+        sees[s] = np.tri(new[s], dtype=bool)
+    rows, k, ref = pick(c, x, starts, lens, sees, some, (H, Hkv, hd))
+    check(y[rows], lse[:, rows], k, ref)
+
+
+@pytest.mark.parametrize("n_seq", [4, 70])
+def test_starts_that_fall_compute_nothing(n_seq):
+    c = db().PagedCache.empty(1, 8, 1, 16, 64, n_seq, 64)
+    c.lens[1] = 1000   # of no pages: tokens that nobody sees
+    x = torch.randn(40, 3 * 64, device="cuda").bfloat16()
+    out, lse = torch.full((40, 64), 7, dtype=torch.bfloat16, device="cuda"), torch.full((1, 40), 7.0, device="cuda")
+    c.attention(x, ints([0, 20, 10] + [40] * (n_seq - 2)), 40, out=out, lse=lse)
+    torch.cuda.synchronize()
+    assert bool((out == 7).all()) and bool((lse == 7).all())
