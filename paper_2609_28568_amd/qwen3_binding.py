@@ -491,6 +491,8 @@ class Qwen3:
             return
         n = ctypes.c_size_t()
         rows, like = self.cfg.B * self.cfg.T, self.bufs["workspace"]
+        if cache.pages.device != like.device:
+            raise ValueError("the cache must be on the model's device")
         _device_rows(starts, "starts", self.torch.int32, like, (cache.lens.shape[0] + 1,))
         words = 0
         if mask is not None:

@@ -283,3 +283,14 @@ def test_tiles_are_bounded_by_the_rows():
     c.max_pages, t = 1 << 15, db.Tree(16, (1 << 22) - 1, 4096, 0, 0)   # 69,632 blocks of 8,256 tiles, 8 heads
     assert L.qwen3_tree_size(ctypes.byref(c), ctypes.byref(t), ctypes.byref(n)) == INVALID
     assert "too many or too long" in why()
+
+
+def test_a_cache_on_another_device_than_the_model_is_refused():
+    """Its addresses would be another card's."""
+    torch = pytest.importorskip("torch")
+    from types import SimpleNamespace
+    m = qb.Qwen3.__new__(qb.Qwen3)
+    m.bufs, m.cfg = {"workspace": torch.zeros(1)}, SimpleNamespace(B=1, T=64)
+    c = SimpleNamespace(pages=torch.empty(1, 4, 2, 1, 16, 64, device="meta"), lens=torch.zeros(3, dtype=torch.int32, device="meta"))
+    with pytest.raises(ValueError, match="device"):
+        m.set_cache(c, torch.zeros(4, dtype=torch.int32))
