@@ -528,10 +528,17 @@ class Qwen3:
 
     def logits(self):
         """The last forward's logits (without targets), bf16 [positions with
-        loss, vocab], in the model's own memory (qwen3_logits_info)."""
+        loss, vocab], in the model's own memory (qwen3_logits_info). The current
+        stream waits for the model's (but in a capture, whose graph the caller
+        replays behind the forward). The next forward writes over them: what
+        another stream has still to read of them is the caller's to wait for
+        before it."""
         from . import decode_binding as db
         at, rows = ctypes.c_size_t(), ctypes.c_int32()
         _check(db.lib().qwen3_logits_info(self.h, ctypes.byref(at), ctypes.byref(rows)), self.h)
+        now = self.torch.cuda.current_stream(self.bufs["activations"].device)
+        if now != self.stream and not self.torch.cuda.is_current_stream_capturing():
+            now.wait_stream(self.stream)
         n = rows.value * self.cfg.vocab * 2
         return self.bufs["activations"][at.value:at.value + n].view(self.torch.bfloat16).view(rows.value, self.cfg.vocab)
 

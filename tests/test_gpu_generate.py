@@ -271,3 +271,32 @@ def test_only_rows_that_the_forward_computed_are_kept():
     a.m.forward(ids)
     a.m.keep_tokens(500)
     assert a.cache.lens.tolist() == [10, 4, 0, 0, 0] and a.cache.short.item() == 0
+
+
+def test_logits_read_on_another_stream():
+    """The stream that asks for them waits for the forward on the model's stream."""
+    a = Answers(seed=63)
+    a.extend([prompt(20, 1), prompt(3, 2), [], [], []])
+    ids = torch.zeros(1, 64, dtype=torch.int32, device="cuda")
+    starts, other = ints([0, 1, 2, 2, 2, 2]), torch.cuda.Stream()
+    a.m.set_cache(a.cache, starts, 1)
+    got = {}
+    for token in (5, 9):
+        ids[0, :2] = token
+        torch.cuda._sleep(20_000_000)   # the forward is behind this, on the model's stream
+        a.m.forward(ids)
+        with torch.cuda.stream(other):
+            got[token] = a.m.logits()[:2].clone()
+        torch.cuda.current_stream().wait_stream(other)
+        assert torch.equal(a.m.logits()[:2], got[token])
+    assert not torch.equal(got[5], got[9])
+    # captured on that stream, replayed behind forwards
+    graph, out = torch.cuda.CUDAGraph(), torch.empty_like(got[5])
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=other):
+        out.copy_(a.m.logits()[:2])
+    for token in (5, 9, 5):
+        ids[0, :2] = token
+        a.m.forward(ids)
+        graph.replay()
+        assert torch.equal(out, got[token])
