@@ -72,8 +72,10 @@ def lib():
 
 class PagedCache:
     """Keys and values of some sequences on pages that they may share
-    (qwen3_cache_*). Its calls run one after another, on the current stream;
-    the tensors are the caller's to read, and to save and restore."""
+    (qwen3_cache_*). Its calls run one after another, on the current stream,
+    which the caller orders where there are several; the tensors are the
+    caller's to read, and to save and restore, and are not freed before the
+    streams of the calls are done with them."""
 
     def __init__(self, pages, table, lens, refs, short):
         """Over tensors that hold a cache: pages bf16 [n_layer, n_pages, 2,
@@ -100,7 +102,7 @@ class PagedCache:
         for name in ("pages", "table", "lens", "refs", "short", "scratch"):
             setattr(c, "d_" + name, getattr(self, name).data_ptr())
         self._c, self._ref = c, ctypes.byref(c)
-        self._stream = torch.cuda.current_stream(pages.device).cuda_stream
+        self._streams = {torch.cuda.current_stream(pages.device).cuda_stream}   # that the tensors are kept for
         self._n_seq, self._index = n_seq, pages.get_device()
         self._trees, self._heads = {}, {}
 
@@ -115,8 +117,10 @@ class PagedCache:
     def _run(self, fn, *args):
         torch, index = self.torch, self._index
         stream = torch._C._cuda_getCurrentRawStream(index)
-        if stream != self._stream:   # the scratch is another stream's: it stays until this one is done with it
-            self.scratch.record_stream(torch.cuda.current_stream(index))
+        if stream not in self._streams:   # memory of another stream's: it stays until this one is done with it
+            for t in (self.pages, self.table, self.lens, self.refs, self.short, self.scratch):
+                t.record_stream(torch.cuda.current_stream(index))
+            self._streams.add(stream)
         if torch.cuda.current_device() == index:
             _check(fn(self._ref, *args, stream))
         else:
@@ -205,9 +209,9 @@ class PagedCache:
         if lse is None:
             lse = torch.empty(n_head, rows, dtype=torch.float32, device=qkv.device)
         work = torch.empty(nbytes, dtype=torch.uint8, device=qkv.device)
-        _check(on_stream(qkv.device, lib().qwen3_tree_attention, self._ref, tree, at, first, bits or None,
-                         self._given(out, "out", (rows, width), torch.bfloat16),
-                         self._given(lse, "lse", (n_head, rows), torch.float32), work.data_ptr(), nbytes))
+        self._run(lib().qwen3_tree_attention, tree, at, first, bits or None,
+                  self._given(out, "out", (rows, width), torch.bfloat16),
+                  self._given(lse, "lse", (n_head, rows), torch.float32), work.data_ptr(), nbytes)
         return out, lse
 
     def positions(self, starts, rows, mask=None, out=None):
@@ -221,8 +225,8 @@ class PagedCache:
         t = Tree(self._c.n_kv_head, i32(rows), 1, 0, words)
         if out is None:
             out = torch.empty(1, rows, dtype=torch.int32, device=self.pages.device)
-        _check(on_stream(self.pages.device, lib().qwen3_tree_positions, self._ref, ctypes.byref(t),
-                         self._ints(starts, "starts", (self._n_seq + 1,)), bits, self._ints(out, "out", (1, rows))))
+        self._run(lib().qwen3_tree_positions, ctypes.byref(t), self._ints(starts, "starts", (self._n_seq + 1,)), bits,
+                  self._ints(out, "out", (1, rows)))
         return out
 
 

@@ -591,3 +591,33 @@ def test_starts_that_fall_compute_nothing(n_seq):
     c.attention(x, ints([0, 20, 10] + [40] * (n_seq - 2)), 40, out=out, lse=lse)
     torch.cuda.synchronize()
     assert bool((out == 7).all()) and bool((lse == 7).all())
+
+
+def test_a_cache_let_go_while_another_stream_works_on_it():
+    """Its memory is not another tensor's before that stream is done."""
+    n, H, hd = 600, 2, 64
+    x = torch.randn(1, n + 1, (H + 2) * hd, device="cuda").bfloat16()
+    st, one = ints([0, n]), ints([0, 1])
+
+    def use(sleep):
+        c = db().PagedCache.empty(1, 40, 1, 16, hd, 1, 40)
+        torch.cuda.current_stream().synchronize()
+        with torch.cuda.stream(side):
+            if sleep:
+                torch.cuda._sleep(50_000_000)
+            c.append(x, st, n)
+            y = c.attention(x[0, n:], one, 1)
+            p = c.positions(one, 1)
+        shapes = [t.shape for t in (c.pages, c.table, c.lens, c.refs, c.short, c.scratch)]
+        return y, p, shapes
+
+    side = torch.cuda.Stream()
+    (want, lse), place, _ = use(False)
+    torch.cuda.synchronize()
+    (y, l), p, shapes = use(True)
+    # of the same sizes, on the stream that the cache was made on
+    junk = [torch.full(s, 3, dtype=d, device="cuda") for s, d in
+            zip(shapes, [torch.bfloat16] + [torch.int32] * 4 + [torch.uint8]) for _ in range(3)]
+    torch.cuda.synchronize()
+    assert torch.equal(y, want) and torch.equal(l, lse) and torch.equal(p, place) and p.tolist() == [[n]]
+    assert all(bool((t == 3).all()) for t in junk)
