@@ -621,3 +621,139 @@ def test_a_cache_let_go_while_another_stream_works_on_it():
     torch.cuda.synchronize()
     assert torch.equal(y, want) and torch.equal(l, lse) and torch.equal(p, place) and p.tolist() == [[n]]
     assert all(bool((t == 3).all()) for t in junk)
+
+
+# ---- which kernel a call takes, and how it divides its work
+
+def walk(H, Hkv, hd, lens, new, max_new):
+    """(head size, blocks of 32 rows of a workgroup, division, planned): the rules of
+    tree.hip's with_walk and cuts_of, so that the cases below reach what they are for."""
+    G = H // Hkv
+    rb = 1 if max_new * G <= 32 else 2 if max_new * G <= 64 else 4
+    kt, groups, teams = 32 if hd == 128 and rb < 4 else 64, 4 // rb, 256 if rb == 1 else 512
+    whole = max(2 * groups, 4)
+    up = lambda a, b: -(-a // b)   # noqa: E731
+    seqs = [(up(n, kt) + up(k, kt), up(k * G, 32 * rb) * Hkv) for n, k in zip(lens, new) if k]   # tiles, segments
+    total, segments = sum(t * s for t, s in seqs), sum(s for _, s in seqs)
+    even = max(whole // 2, up(total, teams))
+    pieces = lambda share: sum((1 if t <= whole else up(t, share)) * s for t, s in seqs)   # noqa: E731
+    dealt = segments <= teams and (max(t for t, _ in seqs) <= whole or pieces(even + (even * 14 + 31) // 32) <= teams)
+    return hd, rb, "dealt" if dealt else "solo" if rb == 1 and segments > teams else "line", len(lens) > 64
+
+
+def ragged(n, lo, hi, step):
+    return [lo + (step * i) % (hi - lo + 1) for i in range(n)]
+
+
+DIVIDED = {
+    # as CASES, with the walk
+    "dealt_128_2": ((4, 2, 128, 16, [3001, 0, 1700, 333, 64, 2222], [20, 32, 17, 31, 1, 29], True, 32), "dealt"),
+    "dealt_128_2_chain": ((6, 2, 128, 64, [2500, 31, 900], [13, 21, 20], False, 21), "dealt"),
+    "dealt_128_2_planned": ((2, 1, 128, 16, ragged(80, 0, 900, 311), ragged(80, 17, 32, 5), True, 32), "dealt"),
+    "dealt_64_2": ((4, 2, 64, 32, [4000, 1, 1234, 777], [18, 32, 25, 3], True, 32), "dealt"),
+    "dealt_64_2_planned": ((3, 1, 64, 16, ragged(70, 5, 1500, 407), ragged(70, 11, 21, 4), False, 21), "dealt"),
+    "dealt_128_4": ((4, 2, 128, 32, [1800, 77, 640], [130, 40, 65], True, 130), "dealt"),
+    "dealt_128_1_planned": ((4, 1, 128, 16, ragged(90, 0, 1200, 173), [1] * 90, False, 1), "dealt"),
+    "line_128_1": ((6, 3, 128, 16, ragged(48, 950, 1150, 37), [1 + i % 4 for i in range(48)], False, 4), "line"),
+    "line_64_1": ((6, 3, 64, 32, ragged(48, 1900, 2300, 71), [1 + i % 3 for i in range(48)], True, 3), "line"),
+    "line_128_1_planned": ((4, 2, 128, 64, ragged(73, 950, 1150, 53), [1] * 73, False, 1), "line"),
+    "line_64_1_planned": ((4, 2, 64, 16, ragged(73, 1900, 2300, 91), [2] * 73, True, 2), "line"),
+    "line_128_2": ((18, 9, 128, 16, ragged(60, 0, 700, 263), ragged(60, 12, 32, 7), True, 32), "line"),
+    "line_128_2_planned": ((8, 4, 128, 32, ragged(140, 0, 500, 119), ragged(140, 1, 24, 5), False, 24), "line"),
+    "line_64_2": ((18, 9, 64, 64, ragged(60, 0, 1300, 571), ragged(60, 12, 32, 7), False, 32), "line"),
+    "line_64_2_planned": ((8, 4, 64, 16, ragged(140, 0, 900, 313), ragged(140, 1, 24, 5), True, 24), "line"),
+    "line_128_4": ((18, 9, 128, 128, ragged(60, 0, 900, 389), ragged(60, 20, 90, 17), True, 90), "line"),
+    "line_128_4_planned": ((8, 4, 128, 16, ragged(140, 0, 600, 257), ragged(140, 1, 45, 8), False, 45), "line"),
+    "line_64_4": ((18, 9, 64, 16, ragged(60, 0, 1100, 463), ragged(60, 20, 90, 17), False, 90), "line"),
+    "line_64_4_planned": ((8, 4, 64, 32, ragged(140, 0, 800, 337), ragged(140, 1, 45, 8), True, 45), "line"),
+    "solo_128_1_planned": ((8, 4, 128, 16, ragged(120, 0, 700, 97), [i % 3 for i in range(120)], False, 2), "solo"),
+    "solo_64_1": ((20, 10, 64, 64, ragged(50, 0, 1500, 283), [1 + i % 5 for i in range(50)], True, 5), "solo"),
+    # a piece of a prompt among single tokens
+    "mixed": ((4, 2, 128, 16, ragged(64, 200, 2048, 709), [1] * 40 + [700] + [1] * 23, False, 700), "dealt"),
+    "mixed_planned": ((4, 4, 64, 32, ragged(90, 200, 1500, 709), [1] * 70 + [333] + [1] * 19, False, 333), "line"),
+}
+
+
+def test_walks_and_divisions_are_all_reached():
+    got = {k: walk(*c[:3], c[4], c[5], c[7]) for k, c in CASES.items()}
+    for k, (c, division) in DIVIDED.items():
+        got[k] = walk(*c[:3], c[4], c[5], c[7])
+        assert got[k][2] == division, (k, got[k])
+    ways = {(rb, d) for rb in (1, 2, 4) for d in ("dealt", "line")} | {(1, "solo")}
+    assert {(hd, rb, d) for hd, rb, d, _ in got.values()} == {(hd, rb, d) for hd in (64, 128) for rb, d in ways}
+    assert {(rb, d) for _, rb, d, planned in got.values() if planned} == ways
+
+
+@pytest.mark.parametrize("name", list(DIVIDED))
+def test_every_walk_and_division(name, monkeypatch):
+    monkeypatch.setitem(CASES, name, DIVIDED[name][0])
+    test_attention_against_the_definition(name)
+
+
+def test_a_step_of_the_books_captured():
+    """Forking, appending and compacting captured once: every replay, with other
+    arguments and eager calls on another cache in between, as the lists say."""
+    rng, gen = random.Random(5), torch.Generator().manual_seed(5)
+    layers, H, Hkv, hd, ps, n_seq, n_pages, max_pages, rows, width = 2, 2, 1, 64, 16, 6, 60, 9, 64, 7
+    c, m = db().PagedCache.empty(layers, n_pages, Hkv, ps, hd, n_seq, max_pages), Model(n_pages, n_seq, max_pages, ps)
+    other = db().PagedCache.empty(layers, n_pages, Hkv, ps, hd, n_seq, max_pages)
+    x = torch.zeros(layers, rows, (H + 2 * Hkv) * hd, dtype=torch.bfloat16, device="cuda")
+    src, keep, counts = (torch.zeros(n_seq, dtype=torch.int32, device="cuda") for _ in range(3))
+    starts, path = torch.zeros(n_seq + 1, dtype=torch.int32, device="cuda"), ints([[-1] * width] * n_seq)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        c.fork(src, keep)
+        c.append(x, starts, width, counts=counts, path=path)
+        c.append(x, starts, 40)
+        c.compact()
+    value = {}
+    for step in range(12):
+        s, k = [rng.choice((i, i, 0, -1)) for i in range(n_seq)], [rng.choice((10 ** 6, 3, ps, 21)) for _ in range(n_seq)]
+        given = [rng.choice((0, 1, rng.randint(0, 10))) for _ in range(n_seq)]
+        if step % 4 == 1:
+            given[rng.randrange(n_seq)] = 40
+            given = [g if g in (40, 1) else 0 for g in given]
+        st = np.concatenate([[0], np.cumsum(given)]).tolist()
+        assert st[-1] <= rows
+        new = torch.randn(layers, rows, x.shape[2], generator=gen).bfloat16()
+        taken = [sorted(rng.sample(range(g), rng.randint(0, min(g, width)))) for g in given]
+        for t, v in ((src, s), (keep, k), (starts, st), (counts, [len(t) for t in taken]),
+                     (path, [t + [-1] * (width - len(t)) for t in taken])):
+            t.copy_(ints(v))
+        x.copy_(new)
+        graph.replay()
+        other.append(x, starts, 40)   # eager work in between, until the pages are too few
+        torch.cuda.synchronize()
+        name = lambda q, i: (step, q, i)   # noqa: E731
+        for q, g in enumerate(given):
+            for i in range(g):
+                row = new[:, st[q] + i].view(layers, H + 2 * Hkv, hd)[:, H:]
+                value[name(q, i)] = row.reshape(layers, 2, Hkv, hd)
+        m.fork(s, k)
+        m.append([[name(q, i) for i in t] for q, t in enumerate(taken)])
+        assert m.append([[name(q, i) for i in range(g)] for q, g in enumerate(given)]) == c.short.item()
+        m.compact()
+        agree(c, m, value)
+
+
+@pytest.mark.parametrize("name", ["drafts", "drafts_wide", "drafts_hd64", "drafts_hd64_wide", "drafts_past_64", "chain",
+                                  "chain_hd64"])
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
+def test_rows_beside_one_that_is_not_finite_keep_their_bounds(name, what):
+    """Against the definition, of which a token that a row does not see is no part."""
+    H, Hkv, hd, ps, lens, new, tree, max_new = CASES[name]
+    c, x, starts, mask, sees = build(name, seed=5)
+    for s, k in enumerate(new):
+        x[starts[s] + (2 * s + k // 3) % k] = what
+    y, lse = c.attention(x, ints(starts), max_new, mask=mask)
+    ref = reference(c, torch.where(x.isfinite(), x, 0), starts, lens, sees, H, Hkv, hd, 0)
+    n = 0
+    for s, k in enumerate(new):
+        rows = np.flatnonzero(~sees[s][:, (2 * s + k // 3) % k])
+        n += len(rows)
+        out, l, bound = ref[s]
+        at = torch.from_numpy(starts[s] + rows).cuda()
+        assert np.all(np.abs(f64(y[at]) - out[rows]) <= bound[rows]), s
+        assert np.all(np.abs(f64(lse[:, at]) - l[:, rows]) <= 2.0 ** -18 * (1 + np.abs(l[:, rows]))), s
+    assert n > 0
