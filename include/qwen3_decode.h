@@ -30,9 +30,10 @@ extern "C" {
  * Calls on one cache run one after another. Forking, appending and compacting
  * change it (attention does not). */
 typedef struct qwen3_cache {
-  int32_t n_layer, n_kv_head, head_dim;   /* head_dim 64 or 128 */
+  int32_t n_layer, n_kv_head, head_dim;   /* 65535 and 4096 at most; head_dim 64 or 128 */
   int32_t page_size;                      /* 16, 32, 64, 128 or 256 */
-  int32_t n_pages, n_seq, max_pages;      /* pages; sequences, 4096 at most; pages of a sequence */
+  int32_t n_pages, n_seq, max_pages;      /* pages, below 2^28; sequences, 4096 at most; pages of a sequence,
+                                             max_pages * page_size below 2^30 */
   void* d_pages;      /* bf16 [n_layer][n_pages][2: keys, values][n_kv_head][page_size][head_dim], 16-byte aligned */
   int32_t* d_table;   /* [n_seq][max_pages] */
   int32_t* d_lens;    /* [n_seq], tokens of each sequence */
@@ -51,8 +52,9 @@ gpt2_status qwen3_cache_fork(const qwen3_cache* c, const int32_t* d_src,
 
 /* New tokens' keys and values, of every layer, behind those of their sequences.
  * d_qkv: bf16 [n_layer][n_rows] rows q [n_head * head_dim] | k [n_kv_head *
- * head_dim] | v likewise, layers layer_stride elements apart (a multiple of 8),
- * 16-byte aligned, n_head a positive multiple of n_kv_head. Sequence s has rows
+ * head_dim] | v likewise, layers layer_stride elements apart (a multiple of 8,
+ * 2^40 at most), 16-byte aligned, n_head a positive multiple of n_kv_head, 4096
+ * at most, n_rows below 2^28. Sequence s has rows
  * d_starts[s]..d_starts[s+1]-1 (d_starts int32 [n_seq + 1], within 0..n_rows,
  * not falling). It takes the first d_counts[s] of them (NULL: all), or, with
  * d_path int32 [n_seq][max_new], rows d_starts[s] + d_path[s][i], i <
@@ -98,9 +100,9 @@ gpt2_status qwen3_cache_compact(const qwen3_cache* c, void* hip_stream);
  * to 2 * 10^9 is taken, what is much beyond is INVALID_ARG. */
 typedef struct qwen3_tree {
   int32_t n_head, n_rows;   /* n_head * n_rows below 2^26 */
-  int32_t max_new;       /* no sequence has more new tokens */
+  int32_t max_new;       /* no sequence has more new tokens; below 2^28 */
   int32_t layer;         /* of the cache */
-  int32_t mask_words;    /* not looked at without d_mask */
+  int32_t mask_words;    /* 2^20 at most; not looked at without d_mask */
 } qwen3_tree;
 gpt2_status qwen3_tree_size(const qwen3_cache* c, const qwen3_tree* t,
                             size_t* bytes_out);
@@ -167,11 +169,11 @@ gpt2_status qwen3_logits_info(const qwen3_model* m, size_t* offset_bytes,
  * be d_logits, with the same stride, and overlaps it in no other way. Columns
  * from vocab on are neither read nor written. */
 typedef struct qwen3_logits {
-  int32_t rows, vocab, dtype;
-  int64_t logits_stride, out_stride;
-  int32_t n_seq, history_stride;   /* d_history int32 [n_seq][history_stride] */
-  int32_t path_len;                /* d_path int32 [rows][path_len] */
-  int32_t n_bias;                  /* d_bias_ids int32, d_bias fp32 [rows][n_bias] */
+  int32_t rows, vocab, dtype;      /* 65535 rows and a vocab of 2^26 at most */
+  int64_t logits_stride, out_stride;   /* 2^40 at most */
+  int32_t n_seq, history_stride;   /* d_history int32 [n_seq][history_stride], 2^28 at most */
+  int32_t path_len;                /* d_path int32 [rows][path_len], 2^20 at most */
+  int32_t n_bias;                  /* d_bias_ids int32, d_bias fp32 [rows][n_bias], 1024 at most */
   int32_t n_masks;                 /* d_masks int32 [n_masks][ceil(vocab / 32)] */
   const int32_t *d_history, *d_prompt_lens, *d_lens, *d_row_seq, *d_path;
   const float *d_repetition, *d_frequency, *d_presence;   /* [rows] */

@@ -7,10 +7,11 @@
 // pages are taken follows from the counts alone, so results do not depend on
 // which workgroup comes first. Books of a call are one launch of few
 // workgroups, bound by a few dependent memory round trips (forking 16 sequences
-// of 1,500 tokens 2.2 us, appending to them 5.8; finding which of 15 sequences' pages
-// move 3.4); the tokens and pages they name are moved by a second one, bound by
-// HBM (prompts, 600 MB read and written, 92 us: 6.1 TB/s; 178 MB of moved pages
-// 30 us: 5.9 TB/s).
+// of 1,500 tokens 2.0 us, appending to them 5.6; finding which of 15 sequences' pages
+// move 3.4, with some hundred pages; the counts of all pages are passed over two and
+// three times, which with 57,344 of them takes an append 7 us more); the tokens and
+// pages they name are moved by a second one, bound by HBM (prompts, 561 MB read and
+// written, 91 us: 6.2 TB/s; 175 MB of moved pages 30 us: 5.8 TB/s).
 #include <algorithm>
 
 #include "common.h"
@@ -251,7 +252,7 @@ DEV int seq_of_row(const int32_t* starts, int n_seq, int row) {
 // Tokens into their places, a wave one token of one layer (of the rows, or of
 // the path's entries: a wave each of n_seq * max_new, 63 single tokens beside a
 // piece of 2,048 in 28 layers were 789 us a pass, 81 so), and behind those blocks the shared pages' tokens, a wave one head of one page. Written past the
-// caches: prompts of a batch, 600 MB read and written, 115 us a pass through
+// caches: prompts of a batch, 561 MB read and written, 115 us a pass through
 // them, 106 past them (5.3 TB/s); with 8 tokens a wave 143 and 136.
 __global__ __launch_bounds__(64) void append_move_kernel(CacheArgs c, AppendArgs a, int items, int nt) {
   const int4* rec = reinterpret_cast<const int4*>(c.scratch + CACHE_HEADER);
@@ -380,7 +381,7 @@ __global__ __launch_bounds__(256) void compact_move_kernel(CacheArgs c) {
     const int n = min(4, (units - u0) / 256);
     uint4 v[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q)   // (past the caches: 178 MB of pages 53 -> 48 us a pass)
+    for (int q = 0; q < 4; ++q)   // (past the caches: 175 MB of pages 53 -> 48 us a pass)
       v[q] = q < n ? ld_stream(src + q * 256 + threadIdx.x) : make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int q = 0; q < 4; ++q)

@@ -4,12 +4,13 @@
 // A workgroup takes a piece of one row. It counts the row's history within the
 // piece in LDS (whole numbers, so their order does not matter), then passes over
 // the logits once, whose loads are under way behind the history's. HBM-bound with
-// many rows (64 rows of 151,936 bf16 after 2,048 tokens 13.1 us, 39 MB: 3.0 TB/s,
+// many rows (64 rows of 151,936 bf16 after 2,048 tokens 13.1 us a pass, 39 MB: 3.0 TB/s,
 // most of it the chain of history, counts and logits that every workgroup runs once);
 // every piece of a row reads the history again, from L2, so pieces are long where
-// histories are (96 rows of 50,257 fp32 after up to 30,000 16.2 us, of which some 6 to
-// compare tokens and 3 to count them). One row takes 3.0 us, a launch and two
-// dependent loads.
+// histories are (96 rows of 50,257 fp32 after up to 30,000 16.3 us a pass, of which some
+// 6 to compare tokens and 3 to count them). One row takes 3.0 us, a launch and two
+// dependent loads. (Passes of one launch among others; a launch that is traced takes
+// longer.)
 #include <algorithm>
 
 #include "../../include/qwen3_decode.h"

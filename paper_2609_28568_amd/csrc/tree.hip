@@ -406,12 +406,14 @@ DEV float inverse(float l) { return l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l; 
 // attention kernels here; two bf16 halves of P would take the output's error from
 // 2.3e-3 to 1.7e-3 and cost 2 to 6 %), O += V P, all sums in fp32. Loads of the next
 // tile are under way while one is worked on.
-// One new token is bound by HBM: 64 sequences of 200 to 4,096 96 us, 131,071 tokens
-// 87 us, 64 of 2,048 89 us (5.5, 6.2 and 6.0 TB/s; a read-only stream reaches 6.0 to
-// 7.1). 16 trees of 24 drafts over 1,000 to 3,001 tokens take 34 us: pieces of some 12
-// tiles one after another, 1.6 us for 32 keys (0.5 to issue loads, 1.1 for scores and
-// softmax, then the second product beside them), 3 to 4 us of dependent loads before
-// the first (lengths, table, page) and 1 to 2 to merge the groups.
+// One new token is bound by HBM: 64 sequences of 200 to 4,096 95 us, 131,071 tokens
+// 87 us, 64 of 2,048 89 us (5.8, 6.2 and 6.0 TB/s; a read-only stream reaches 6.0 to
+// 7.1). 16 trees of 24 drafts over 1,000 to 3,001 tokens take 33 us: 5 of dependent
+// loads (lengths, cuts, table, page) before the first tile is under way and 2 until it is
+// there, then up to nine tiles of 32 keys a group one after another at 2.3 (0.5 to
+// issue loads, 1.1 for scores and softmax, 0.6 for the second product, beside another
+// workgroup on the compute unit), 1 to merge the groups, 3 to launch and end. Two
+// blocks of rows of heads of 128 take all 256 registers and spill 3, four spill 5.
 template <int HD, int RB>
 __global__ __launch_bounds__(256, RB == 1 ? 1 : 2) void tree_kernel(TreeArgs a) {
   using W = Walk<HD, RB>;
